@@ -561,6 +561,220 @@ atp_status atp_attention_bwd_noalloc(const atp_mesh* mesh, int32_t block_mode, i
                                      const float* lse, const void* d_out, int64_t ld_dout,
                                      void* d_qkv, int64_t ld_dqkv, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Position, cache and cached attention of one device's run of heads.
+ *
+ * What a layer needs around the attention core to be trained with positions
+ * and to answer with: the norms of queries and keys with the position
+ * rotation, a paged cache of keys and values, and the attention that reads
+ * it.  The calls take the device's run of heads itself (atp_attention_heads
+ * gives its first head: pass the buffer at that head's column).
+ *
+ * Head layout of a QKV row: for each of kv_heads key/value heads its `group`
+ * query heads, the key and the value, 128 columns each ([q .. q | k | v];
+ * group 1 is the block of atp_attention_fwd).  Rows of queries and of
+ * attention outputs hold the kv_heads * group query heads in that order.
+ * group is at most ATP_MAX_QUERY_GROUP.
+ *
+ * Lists, lengths and tables live in device memory (int32, 16-byte aligned),
+ * so a step can be captured once and replayed as the lengths grow.  What the
+ * host cannot see is checked by the kernels: a table entry outside
+ * [0, n_pages) holds no tokens, rows and columns stay inside the sizes given
+ * here, and nothing is read or written elsewhere.
+ * ------------------------------------------------------------------------ */
+#define ATP_MAX_QUERY_GROUP 64
+#define ATP_MAX_FORKS 4096
+
+/* What is done to every query and key head row x (128 values), in fp32 and
+ * rounded once:
+ *   u = norm ? w o x / sqrt(mean(x^2) + eps) : x     (w: q_weight or k_weight)
+ *   y = u with the pairs of its first rotary_dims values turned by the angle
+ *       position * inv_freq[i], i = 0 .. rotary_dims / 2 - 1:
+ *       (a, b) -> (a cos - b sin, b cos + a sin)
+ * with pair i = (u[i], u[i + rotary_dims / 2]), or (u[2 i], u[2 i + 1]) when
+ * interleaved.  The angle is formed and reduced in 64 bits.
+ * q_weight, k_weight: bf16 [128], nullable (ones).  inv_freq: fp32
+ * [rotary_dims / 2], radians per position.  rotary_dims: a multiple of 8 up
+ * to 128, 0 for no rotation (inv_freq may be NULL).
+ * Errors: INVALID_ARGUMENT for a NULL struct, negative or non-finite eps, eps
+ * and norm flags out of range, weights without norm, rotary_dims outside [0,
+ * 128], a missing inv_freq; UNSUPPORTED for rotary_dims not a multiple of 8,
+ * misalignment. */
+typedef struct {
+    const void* q_weight;
+    const void* k_weight;
+    const float* inv_freq;
+    float eps;
+    int32_t norm;
+    int32_t rotary_dims;
+    int32_t interleaved;
+} atp_qk_norm_rope;
+
+/* The rows of a QKV block normed and turned: out = the block with its query
+ * and key heads replaced, values copied (the input of atp_attention_fwd).
+ * qkv, out: bf16 [batch*seq, kv_heads * (group + 2) * 128], token rows
+ * sequence-major.  positions: int32 [batch*seq], or NULL for t % seq.  out
+ * may be qkv itself (same pointer and ld; values are then not touched), else
+ * they must not overlap.
+ * Errors: INVALID_ARGUMENT for negative sizes, kv_heads or group < 1, NULL
+ * buffers, overlap; UNSUPPORTED for more than 2^24 tokens, a group above
+ * ATP_MAX_QUERY_GROUP, misalignment. */
+atp_status atp_qk_norm_rope_fwd(int64_t batch, int64_t seq, int32_t kv_heads, int32_t group,
+                                const atp_qk_norm_rope* params, const int32_t* positions,
+                                const void* qkv, int64_t ld_qkv, void* out, int64_t ld_out,
+                                void* stream);
+
+/* Gradient of atp_qk_norm_rope_fwd.  qkv: the forward's input; d_out: the
+ * gradient of its output (what atp_attention_bwd writes); d_qkv receives the
+ * gradient of qkv and may be d_out itself (same pointer and ld), else it must
+ * not overlap it, and never qkv.  With u' = y's gradient turned back and
+ * r = 1 / sqrt(mean(x^2) + eps): dw = sum over rows of u' o x r (fp32 [128]
+ * for the queries, shared by all their heads, and for the keys; nullable,
+ * refused without norm), dx = r (g - x r mean(g o x r)) with g = w o u'.
+ * The sums are formed in a fixed order.  workspace: caller-owned device
+ * memory of atp_qk_norm_rope_workspace_bytes(batch*seq) bytes, scratch;
+ * needed when a weight gradient is asked for.  Errors as
+ * atp_qk_norm_rope_fwd; INVALID_ARGUMENT for a missing or short workspace. */
+atp_status atp_qk_norm_rope_bwd(int64_t batch, int64_t seq, int32_t kv_heads, int32_t group,
+                                const atp_qk_norm_rope* params, const int32_t* positions,
+                                const void* qkv, int64_t ld_qkv, const void* d_out,
+                                int64_t ld_dout, void* d_qkv, int64_t ld_dqkv, float* dq_weight,
+                                float* dk_weight, void* workspace, size_t ws_bytes, void* stream);
+/* 0 for a negative number of tokens. */
+size_t atp_qk_norm_rope_workspace_bytes(int64_t tokens);
+
+/* One layer's cache: bf16 pages[n_pages][2][kv_heads][page_size][128], the
+ * keys then the values of page_size consecutive tokens of one sequence.
+ * page_size: a power of two from 16 to 1024. */
+typedef struct {
+    void* pages;
+    int32_t n_pages, kv_heads, page_size;
+} atp_kv_cache;
+
+/* A batch of n_seqs sequences.  Token i of sequence s is in page
+ * table[s * ld_table + i / page_size] (columns [0, max_pages), at most 2^30
+ * tokens); an entry outside [0, n_pages) is empty.  ctx[s]: tokens cached
+ * before this step.  Rows [cu_new[s], cu_new[s + 1]) of the step's buffers
+ * are the sequence's new tokens (cu_new: n_seqs + 1 ascending values, a
+ * sequence may have none); token j of them goes to place ctx[s] + j of the
+ * cache.  Rows behind cu_new[n_seqs] are padding, neither read nor written.
+ * At most 65536 sequences. */
+typedef struct {
+    int32_t* table;
+    int64_t ld_table;
+    int32_t max_pages, n_seqs;
+    const int32_t* ctx;
+    const int32_t* cu_new;
+} atp_kv_batch;
+
+/* The new tokens of a step: queries normed and turned into q (bf16 [tokens,
+ * kv_heads * group * 128]), keys normed and turned and values as they are into
+ * the cache.  qkv: bf16 [tokens, kv_heads * (group + 2) * 128], the step's rows.
+ * positions: int32 [tokens] (a drafted tree's depths), or NULL for the place
+ * in the cache.  A row whose page is empty or beyond the table is not cached.
+ * kv_heads is the cache's.  Errors as atp_qk_norm_rope_fwd, and those of the
+ * cache and the batch: INVALID_ARGUMENT for NULL structs or members, sizes < 1
+ * (n_seqs < 0), ld_table < max_pages; UNSUPPORTED for page sizes, alignment
+ * and sizes beyond the limits above. */
+atp_status atp_qk_norm_rope_cache(const atp_kv_cache* cache, const atp_kv_batch* batch,
+                                  int64_t tokens, int32_t group, const atp_qk_norm_rope* params,
+                                  const int32_t* positions, const void* qkv, int64_t ld_qkv,
+                                  void* q, int64_t ld_q, void* stream);
+
+/* Pages.  refs[n_pages] counts the table entries that name a page; 0 is
+ * free.  The bookkeeping is one for all layers that share a table; the data
+ * of a layer's cache moves by atp_cache_copy_pages and atp_cache_compact.
+ * Calls that change refs or a table are ordered by their stream: run them on
+ * one stream, or order the streams.
+ *
+ * atp_cache_reserve gives every sequence the pages that its new tokens go to.
+ * An empty entry gets a free page; a page that other sequences hold too
+ * (refs > 1) is replaced by a free one, and when it holds some of the
+ * sequence's cached tokens (the page of place ctx[s] - 1 and ctx[s]) they have
+ * to be copied: copy_src[s], copy_dst[s] name the pages and copy_rows[s] =
+ * ctx[s] % page_size the tokens (-1, -1, 0 for no copy), for
+ * atp_cache_copy_pages on every layer before the next call that gives pages
+ * out.  Pages are given in ascending order to the sequences in ascending
+ * order.  A sequence gets all it needs or nothing: missing[s] is 0, or how
+ * many pages it lacks when the pool (after the sequences before it) or the
+ * table's columns cannot hold it; such a sequence changes nothing, and the
+ * sequences behind it that need pages get none either if it was the pool.
+ * workspace: atp_cache_workspace_bytes(n_pages, n_seqs) bytes, scratch.
+ * missing, copy_src, copy_dst, copy_rows: int32 [n_seqs], written. */
+atp_status atp_cache_reserve(int32_t n_pages, int32_t page_size, int32_t* refs,
+                             const atp_kv_batch* batch, int32_t* missing, int32_t* copy_src,
+                             int32_t* copy_dst, int32_t* copy_rows, void* workspace,
+                             size_t ws_bytes, void* stream);
+/* 0 for sizes below 1 (n_seqs below 0). */
+size_t atp_cache_workspace_bytes(int32_t n_pages, int32_t n_seqs);
+
+/* children[f] becomes a copy of parents[f], f < n_forks: it holds the pages of
+ * the parent's ctx[parent] cached tokens too (no data moves: a shared page is
+ * copied by atp_cache_reserve when one of its holders writes to it).  done[f]
+ * (int32, written) is 0, or 1 for a fork that is refused and changes nothing:
+ * an index outside the batch, a child that is a parent or an earlier child
+ * of the call, or a child whose row still holds pages.  A parent may appear any
+ * number of times.  The lengths (ctx) are the caller's.  n_forks is at most
+ * ATP_MAX_FORKS. */
+atp_status atp_cache_fork(int32_t n_pages, int32_t page_size, int32_t* refs,
+                          const atp_kv_batch* batch, int32_t n_forks, const int32_t* parents,
+                          const int32_t* children, int32_t* done, void* stream);
+
+/* Every sequence with keep[s] >= 0 gives back the pages behind its first
+ * keep[s] tokens (all of them for 0): their entries become -1 and their
+ * reference counts fall by one.  keep: int32 [n_seqs].  ctx and cu_new are not
+ * read. */
+atp_status atp_cache_release(int32_t n_pages, int32_t page_size, int32_t* refs,
+                             const atp_kv_batch* batch, const int32_t* keep, void* stream);
+
+/* For i < n: the first rows[i] tokens (all for rows NULL) of page src[i], keys
+ * and values of every head, are copied to page dst[i].  An entry with rows[i]
+ * <= 0, an index outside the pool or src[i] == dst[i] does nothing.  A page
+ * that is a destination must not appear a second time among src and dst (its
+ * content is undefined then). */
+atp_status atp_cache_copy_pages(const atp_kv_cache* cache, int32_t n, const int32_t* src,
+                                const int32_t* dst, const int32_t* rows, void* stream);
+
+/* Chosen rows behind ctx[s] are moved together: token ctx[s] + keep[cu_keep[s]
+ * + i] goes to place ctx[s] + i, for i < cu_keep[s + 1] - cu_keep[s] (the
+ * accepted path of a drafted tree, or the tokens of a context that are kept).
+ * The indices of a sequence must ascend strictly.  moved (int32 [n_seqs],
+ * nullable) receives the number of rows, or -1 for a sequence that is left
+ * as it was: indices that do not ascend or are negative, or a place without
+ * a page.  cu_keep: int32 [n_seqs + 1]; keep: int32 [n_keep].  The pages
+ * written to must be held by this sequence alone.  cu_new is not read. */
+atp_status atp_cache_compact(const atp_kv_cache* cache, const atp_kv_batch* batch,
+                             const int32_t* cu_keep, const int32_t* keep, int32_t n_keep,
+                             int32_t* moved, void* stream);
+
+/* Attention of the step's new tokens over the cache, which holds them already
+ * (atp_qk_norm_rope_cache): softmax(q k^T / sqrt(128)) v over what each token
+ * sees, in fp32 (weights rounded to bf16 for the product with v).  New token
+ * j of sequence s sees the ctx[s] cached tokens and, of the new ones, 0 .. j
+ * (tree_mask NULL: a decode step, a chunk of a prompt) or those whose bit is
+ * set in its row of tree_mask (uint64 [tokens][mask_words]; bit i % 64 of word
+ * i / 64 is new token i of its sequence, itself included; tokens beyond the
+ * words are not seen).  Whatever a masked or empty place holds does not reach
+ * the result.  A token that sees nothing gets zeros and a log-sum-exp of
+ * -inf.
+ * q, out: bf16 [tokens, kv_heads * group * 128], no overlap.  lse (nullable):
+ * fp32 [kv_heads * group][tokens], the natural log-sum-exp of each row's
+ * scaled scores.  max_new: the most new tokens a sequence is expected to have;
+ * it chooses the kernel's tile, not the result.  workspace: caller-owned,
+ * atp_attention_cache_workspace_bytes(kv_heads, group, max_new) bytes,
+ * scratch.  Long contexts are split over workgroups and joined in a fixed
+ * order: repeats give the same bits; another batch around a sequence can
+ * change its results by fp32 rounding.
+ * Errors as atp_qk_norm_rope_cache; INVALID_ARGUMENT for max_new < 1,
+ * mask_words < 1 with a mask, a short workspace. */
+atp_status atp_attention_cache_fwd(const atp_kv_cache* cache, const atp_kv_batch* batch,
+                                   int64_t tokens, int32_t group, int32_t max_new, const void* q,
+                                   int64_t ld_q, const uint64_t* tree_mask, int32_t mask_words,
+                                   void* out, int64_t ld_out, float* lse, void* workspace,
+                                   size_t ws_bytes, void* stream);
+/* 0 for sizes below 1 or a group above ATP_MAX_QUERY_GROUP. */
+size_t atp_attention_cache_workspace_bytes(int32_t kv_heads, int32_t group, int32_t max_new);
+
 /* Per-kernel timing of the library's own launches.  When enabled, every
  * kernel the library enqueues is bracketed by HIP events on its stream;
  * atp_profile_collect synchronises those events, fills up to `max`

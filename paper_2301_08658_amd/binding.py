@@ -128,6 +128,22 @@ class atp_attn_block_bwd_io(ctypes.Structure):
                 ("partial_dtype", ctypes.c_int32)]
 
 
+class atp_qk_norm_rope(ctypes.Structure):
+    _fields_ = [("q_weight", _vp), ("k_weight", _vp), ("inv_freq", _vp), ("eps", ctypes.c_float),
+                ("norm", ctypes.c_int32), ("rotary_dims", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32)]
+
+
+class atp_kv_cache(ctypes.Structure):
+    _fields_ = [("pages", _vp), ("n_pages", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("page_size", ctypes.c_int32)]
+
+
+class atp_kv_batch(ctypes.Structure):
+    _fields_ = [("table", _vp), ("ld_table", ctypes.c_int64), ("max_pages", ctypes.c_int32),
+                ("n_seqs", ctypes.c_int32), ("ctx", _vp), ("cu_new", _vp)]
+
+
 class atp_kernel_stat(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 64), ("launches", ctypes.c_int64),
                 ("total_ms", ctypes.c_double), ("flops", ctypes.c_double),
@@ -161,8 +177,14 @@ EXPORTS = (
     "atp_attention_fwd", "atp_attention_bwd", "atp_chunked_partial_reduce_bf16",
     "atp_shard_linear_fwd_fused", "atp_block_workspace_path", "atp_block_geometry",
     "atp_attention_heads", "atp_attention_block_fwd", "atp_attention_block_bwd",
-    "atp_attention_bwd_noalloc",
+    "atp_attention_bwd_noalloc", "atp_qk_norm_rope_fwd", "atp_qk_norm_rope_bwd",
+    "atp_qk_norm_rope_workspace_bytes", "atp_qk_norm_rope_cache", "atp_cache_reserve",
+    "atp_cache_workspace_bytes", "atp_cache_fork", "atp_cache_release", "atp_cache_copy_pages",
+    "atp_cache_compact", "atp_attention_cache_fwd", "atp_attention_cache_workspace_bytes",
 )
+ATP_MAX_QUERY_GROUP = 64
+ATP_MAX_FORKS = 4096
+HEAD_DIM = 128
 ATP_NOALLOC_DELTA_MAX = 1 << 20   # values of atp_attention_bwd_noalloc's scratch
 
 _lib = None
@@ -241,6 +263,24 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.atp_attention_bwd_noalloc.argtypes = [mp, i32, i64, i64, i64, i32, _vp, i64, _vp, i64,
                                               _vp, _vp, i64, _vp, i64, _vp]
     lib.atp_attention_bwd_noalloc.restype = i32
+    nrp, kcp, kbp = (ctypes.POINTER(atp_qk_norm_rope), ctypes.POINTER(atp_kv_cache),
+                     ctypes.POINTER(atp_kv_batch))
+    lib.atp_qk_norm_rope_fwd.argtypes = [i64, i64, i32, i32, nrp, _vp, _vp, i64, _vp, i64, _vp]
+    lib.atp_qk_norm_rope_bwd.argtypes = [i64, i64, i32, i32, nrp, _vp, _vp, i64, _vp, i64, _vp,
+                                         i64, _vp, _vp, _vp, sz, _vp]
+    lib.atp_qk_norm_rope_workspace_bytes.argtypes = [i64]
+    lib.atp_qk_norm_rope_cache.argtypes = [kcp, kbp, i64, i32, nrp, _vp, _vp, i64, _vp, i64, _vp]
+    lib.atp_cache_reserve.argtypes = [i32, i32, _vp, kbp, _vp, _vp, _vp, _vp, _vp, sz, _vp]
+    lib.atp_cache_workspace_bytes.argtypes = [i32, i32]
+    lib.atp_cache_fork.argtypes = [i32, i32, _vp, kbp, i32, _vp, _vp, _vp, _vp]
+    lib.atp_cache_release.argtypes = [i32, i32, _vp, kbp, _vp, _vp]
+    lib.atp_cache_copy_pages.argtypes = [kcp, i32, _vp, _vp, _vp, _vp]
+    lib.atp_cache_compact.argtypes = [kcp, kbp, _vp, _vp, i32, _vp, _vp]
+    lib.atp_attention_cache_fwd.argtypes = [kcp, kbp, i64, i32, i32, _vp, i64, _vp, i32, _vp, i64,
+                                            _vp, _vp, sz, _vp]
+    lib.atp_attention_cache_workspace_bytes.argtypes = [i32, i32, i32]
+    for name in EXPORTS[EXPORTS.index("atp_qk_norm_rope_fwd"):]:
+        getattr(lib, name).restype = sz if name.endswith("_bytes") else i32
     hp, dp, cp = (ctypes.POINTER(atp_hcm_layer), ctypes.POINTER(atp_model_dims),
                   ctypes.POINTER(atp_mesh_cost))
     lib.atp_tcomm.argtypes = [dp, i32, i32, ctypes.c_double, ctypes.c_double,
@@ -715,6 +755,210 @@ def atp_attention_bwd_noalloc(m: atp_mesh, block_mode: int, batch: int, seq: int
     _check(load_library().atp_attention_bwd_noalloc(
         ctypes.byref(m), int(block_mode), int(batch), int(seq), int(h), int(heads), qp, ldq, op,
         ldo, _ptr(lse, "lse"), dop, lddo, dqp, lddq, _stream(stream)))
+
+
+def _ints(t: Optional[torch.Tensor], n: int, name: str):
+    """Pointer of a device list of at least n int32 values (None stays NULL)."""
+    return _vec(t, n, torch.int32, name)
+
+
+class qk_norm_rope:
+    """Parameters of the query/key norms with the position rotation
+    (atp_qk_norm_rope in include/atp.h); keeps its tensors alive.  q_weight,
+    k_weight: bf16 [128]; inv_freq: float32 [rotary_dims / 2]."""
+
+    def __init__(self, q_weight=None, k_weight=None, eps: float = 1e-6, inv_freq=None,
+                 rotary_dims: int = 0, interleaved: bool = False, norm: bool = True):
+        self.q_weight, self.k_weight, self.inv_freq = q_weight, k_weight, inv_freq
+        rotary_dims = int(rotary_dims)
+        if rotary_dims > 0 and inv_freq is None:
+            raise ValueError("inv_freq: a rotation needs its frequencies")
+        self.c = atp_qk_norm_rope(
+            _vec(q_weight, HEAD_DIM, torch.bfloat16, "q_weight"),
+            _vec(k_weight, HEAD_DIM, torch.bfloat16, "k_weight"),
+            _vec(inv_freq, max(0, rotary_dims) // 2, torch.float32, "inv_freq"), float(eps),
+            int(norm), rotary_dims, int(interleaved))
+
+    def ref(self):
+        for t, name in ((self.q_weight, "q_weight"), (self.k_weight, "k_weight"),
+                        (self.inv_freq, "inv_freq")):
+            if t is not None:
+                _on_device(t, name)
+        return ctypes.byref(self.c)
+
+
+class kv_cache:
+    """One layer's cache: pages, a contiguous bf16 tensor [n_pages, 2, kv_heads,
+    page_size, 128] (keys, then values)."""
+
+    def __init__(self, pages: torch.Tensor):
+        if pages.dtype != torch.bfloat16:
+            raise TypeError(f"pages: expected torch.bfloat16, got {pages.dtype}")
+        if (pages.dim() != 5 or pages.size(1) != 2 or pages.size(4) != HEAD_DIM or
+                not pages.is_contiguous()):
+            raise ValueError("pages: needs a contiguous [n_pages, 2, kv_heads, page_size, "
+                             f"{HEAD_DIM}] tensor, got {tuple(pages.shape)}")
+        self.pages = pages
+        self.n_pages, _, self.kv_heads, self.page_size, _ = pages.shape
+        self.c = atp_kv_cache(_ptr(pages, "pages"), self.n_pages, self.kv_heads, self.page_size)
+
+    def ref(self):
+        _on_device(self.pages, "pages")
+        return ctypes.byref(self.c)
+
+
+class kv_batch:
+    """A batch of sequences over a cache: table int32 [n_seqs, max_pages], ctx
+    int32 [n_seqs], cu_new int32 [n_seqs + 1] (either may be None for the calls
+    that do not read it).  The tensors are read when a call's kernels run."""
+
+    def __init__(self, table: torch.Tensor, ctx=None, cu_new=None):
+        if table.dtype != torch.int32:
+            raise TypeError(f"table: expected torch.int32, got {table.dtype}")
+        if table.dim() != 2 or (table.size(1) > 1 and table.stride(1) != 1):
+            raise ValueError("table: needs a 2-D row-major tensor")
+        self.table, self.ctx, self.cu_new = table, ctx, cu_new
+        self.n_seqs, self.max_pages = table.shape
+        ld = table.stride(0) if self.n_seqs > 1 else self.max_pages
+        self.c = atp_kv_batch(_ptr(table, "table"), ld, self.max_pages, self.n_seqs,
+                              _ints(ctx, self.n_seqs, "ctx"),
+                              _ints(cu_new, self.n_seqs + 1, "cu_new"))
+
+    def ref(self):
+        for t, name in ((self.table, "table"), (self.ctx, "ctx"), (self.cu_new, "cu_new")):
+            if t is not None:
+                _on_device(t, name)
+        return ctypes.byref(self.c)
+
+
+def atp_qk_norm_rope_fwd(batch: int, seq: int, kv_heads: int, group: int, params: qk_norm_rope,
+                         qkv, out, positions=None, stream=None):
+    """qkv, out: bf16 [batch*seq, kv_heads*(group+2)*128] (out may be qkv);
+    positions: int32 [batch*seq], or None for t % seq."""
+    T, cols = batch * seq, kv_heads * (group + 2) * HEAD_DIM
+    xp, ldx = _mat(qkv, T, cols, torch.bfloat16, "qkv")
+    op, ldo = _mat(out, T, cols, torch.bfloat16, "out")
+    _check(load_library().atp_qk_norm_rope_fwd(
+        int(batch), int(seq), int(kv_heads), int(group), params.ref(),
+        _ints(positions, T, "positions"), xp, ldx, op, ldo, _stream(stream)))
+
+
+def atp_qk_norm_rope_workspace_bytes(tokens: int) -> int:
+    return load_library().atp_qk_norm_rope_workspace_bytes(int(tokens))
+
+
+def atp_qk_norm_rope_bwd(batch: int, seq: int, kv_heads: int, group: int, params: qk_norm_rope,
+                         qkv, d_out, d_qkv, dq_weight=None, dk_weight=None, workspace=None,
+                         positions=None, stream=None):
+    """Gradient of atp_qk_norm_rope_fwd: d_qkv (may be d_out) and, where
+    given, the weights' gradients (float32 [128]; they need a workspace of
+    atp_qk_norm_rope_workspace_bytes(batch*seq) bytes)."""
+    T, cols = batch * seq, kv_heads * (group + 2) * HEAD_DIM
+    xp, ldx = _mat(qkv, T, cols, torch.bfloat16, "qkv")
+    gp, ldg = _mat(d_out, T, cols, torch.bfloat16, "d_out")
+    dp_, ldd = _mat(d_qkv, T, cols, torch.bfloat16, "d_qkv")
+    wsp, wsb = _workspace(workspace)
+    _check(load_library().atp_qk_norm_rope_bwd(
+        int(batch), int(seq), int(kv_heads), int(group), params.ref(),
+        _ints(positions, T, "positions"), xp, ldx, gp, ldg, dp_, ldd,
+        _vec(dq_weight, HEAD_DIM, torch.float32, "dq_weight"),
+        _vec(dk_weight, HEAD_DIM, torch.float32, "dk_weight"), wsp, wsb, _stream(stream)))
+
+
+def atp_qk_norm_rope_cache(cache: kv_cache, batch: kv_batch, tokens: int, group: int,
+                           params: qk_norm_rope, qkv, q, positions=None, stream=None):
+    """The step's rows qkv [tokens, kv_heads*(group+2)*128]: queries into q
+    [tokens, kv_heads*group*128], keys and values into the cache."""
+    xp, ldx = _mat(qkv, tokens, cache.kv_heads * (group + 2) * HEAD_DIM, torch.bfloat16, "qkv")
+    qp, ldq = _mat(q, tokens, cache.kv_heads * group * HEAD_DIM, torch.bfloat16, "q")
+    _check(load_library().atp_qk_norm_rope_cache(
+        cache.ref(), batch.ref(), int(tokens), int(group), params.ref(),
+        _ints(positions, tokens, "positions"), xp, ldx, qp, ldq, _stream(stream)))
+
+
+def atp_cache_workspace_bytes(n_pages: int, n_seqs: int) -> int:
+    return load_library().atp_cache_workspace_bytes(int(n_pages), int(n_seqs))
+
+
+def _refs(refs):
+    if refs is None:
+        raise ValueError("refs: needs the pages' reference counts")
+    return refs.numel(), _ints(refs, refs.numel(), "refs")
+
+
+def atp_cache_reserve(page_size: int, refs, batch: kv_batch, missing, copy_src, copy_dst,
+                      copy_rows, workspace, stream=None):
+    """Pages for every sequence's new tokens; refs: int32 [n_pages]; missing,
+    copy_src, copy_dst, copy_rows: int32 [n_seqs], written."""
+    n, rp = _refs(refs)
+    wsp, wsb = _workspace(workspace)
+    _check(load_library().atp_cache_reserve(
+        n, int(page_size), rp, batch.ref(), _ints(missing, batch.n_seqs, "missing"),
+        _ints(copy_src, batch.n_seqs, "copy_src"), _ints(copy_dst, batch.n_seqs, "copy_dst"),
+        _ints(copy_rows, batch.n_seqs, "copy_rows"), wsp, wsb, _stream(stream)))
+
+
+def atp_cache_fork(page_size: int, refs, batch: kv_batch, parents, children, done, stream=None):
+    """children[f] takes over parents[f]'s pages (int32 lists of one length);
+    done: int32, 0 or 1 (refused) per fork."""
+    n, rp = _refs(refs)
+    forks = parents.numel()
+    _check(load_library().atp_cache_fork(
+        n, int(page_size), rp, batch.ref(), forks, _ints(parents, forks, "parents"),
+        _ints(children, forks, "children"), _ints(done, forks, "done"), _stream(stream)))
+
+
+def atp_cache_release(page_size: int, refs, batch: kv_batch, keep, stream=None):
+    """Gives back the pages behind the first keep[s] >= 0 tokens of sequence s."""
+    n, rp = _refs(refs)
+    _check(load_library().atp_cache_release(n, int(page_size), rp, batch.ref(),
+                                            _ints(keep, batch.n_seqs, "keep"), _stream(stream)))
+
+
+def atp_cache_copy_pages(cache: kv_cache, src, dst, rows=None, stream=None):
+    """The first rows[i] tokens (all for None) of page src[i] to page dst[i]."""
+    n = src.numel()
+    _check(load_library().atp_cache_copy_pages(
+        cache.ref(), n, _ints(src, n, "src"), _ints(dst, n, "dst"), _ints(rows, n, "rows"),
+        _stream(stream)))
+
+
+def atp_cache_compact(cache: kv_cache, batch: kv_batch, cu_keep, keep, moved=None, stream=None):
+    """Moves tokens ctx[s] + keep[cu_keep[s] + i] to places ctx[s] + i; moved:
+    int32 [n_seqs], rows moved or -1 (refused)."""
+    n = keep.numel()
+    _check(load_library().atp_cache_compact(
+        cache.ref(), batch.ref(), _ints(cu_keep, batch.n_seqs + 1, "cu_keep"),
+        _ints(keep, n, "keep"), n, _ints(moved, batch.n_seqs, "moved"), _stream(stream)))
+
+
+def atp_attention_cache_workspace_bytes(kv_heads: int, group: int, max_new: int) -> int:
+    return load_library().atp_attention_cache_workspace_bytes(int(kv_heads), int(group),
+                                                              int(max_new))
+
+
+def atp_attention_cache_fwd(cache: kv_cache, batch: kv_batch, tokens: int, group: int,
+                            max_new: int, q, out, lse=None, tree_mask=None, workspace=None,
+                            stream=None):
+    """Attention of the step's rows q over the cache into out (both bf16
+    [tokens, kv_heads*group*128]); lse: float32 [kv_heads*group, tokens];
+    tree_mask: int64 or uint64 [tokens, words], contiguous; workspace:
+    atp_attention_cache_workspace_bytes(kv_heads, group, max_new) bytes."""
+    cols = cache.kv_heads * group * HEAD_DIM
+    qp, ldq = _mat(q, tokens, cols, torch.bfloat16, "q")
+    op, ldo = _mat(out, tokens, cols, torch.bfloat16, "out")
+    words, mp = 0, None
+    if tree_mask is not None:
+        if tree_mask.dtype not in (torch.int64, torch.uint64):
+            raise TypeError(f"tree_mask: expected 64-bit words, got {tree_mask.dtype}")
+        if tree_mask.dim() != 2 or tree_mask.size(0) < tokens or not tree_mask.is_contiguous():
+            raise ValueError(f"tree_mask: needs a contiguous [{tokens}, words] tensor")
+        words, mp = tree_mask.size(1), _ptr(tree_mask, "tree_mask")
+    wsp, wsb = _workspace(workspace)
+    _check(load_library().atp_attention_cache_fwd(
+        cache.ref(), batch.ref(), int(tokens), int(group), int(max_new), qp, ldq, mp, words, op,
+        ldo, _vec(lse, cache.kv_heads * group * tokens, torch.float32, "lse"), wsp, wsb,
+        _stream(stream)))
 
 
 def _attn_weights(G, w, b, layout: int):

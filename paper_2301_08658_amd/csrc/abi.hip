@@ -15,6 +15,7 @@
 #include <vector>
 
 #include "../../include/atp.h"
+#include "abi_common.h"
 #include "errors.h"
 #include "kernels.h"
 
@@ -774,6 +775,19 @@ atp_status noalloc_scratch(float** out) {
     return ATP_OK;
 }
 }  // namespace
+
+namespace atp {
+namespace abi {
+atp_status check_matrix(const void* p, int64_t rows, int64_t ld, int64_t cols, const char* name) {
+    return check_mat(p, rows, ld, cols, name);
+}
+atp_status check_vector(const void* p, const char* name) { return check_vec(p, name); }
+atp_status run_timed(const char* name, double flops, double bytes, hipStream_t s,
+                     const std::function<hipError_t()>& launch) {
+    return timed(name, flops, bytes, s, launch);
+}
+}  // namespace abi
+}  // namespace atp
 
 // ===========================================================================
 // exported
