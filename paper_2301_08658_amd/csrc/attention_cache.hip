@@ -9,17 +9,21 @@
 // that is cut leaves its pieces' maxima, sums and outputs in the workspace, and
 // join_kernel adds them in order.
 //
-// Inside a workgroup the four waves take 32 keys of every step each, with their
-// own running maximum, sum and output, and meet only at the end of a piece: no
-// barrier stands in the key loop.  A wave's K and V tiles (8 KB each) go straight
+// Few rows (up to 32): the four waves take 32 keys of every step each, with
+// their own running maximum, sum and output, and meet only at the end of a piece:
+// no barrier stands in the key loop.  A wave's K and V tiles (8 KB each) go straight
 // to LDS; K's next tile is asked for as soon as the score products have read this
 // one and V's after the second products, so 8 to 16 KB per wave are under way at
-// any time, 64 to 128 KB per CU.  With few rows the time is the cache's bytes.
+// any time, 64 to 128 KB per CU.  The time is the cache's bytes.
+//
+// Many rows (128 per unit): the waves take 32 rows each and share double-buffered
+// tiles of 64 keys, so every fragment read from LDS feeds two products; the time is
+// the products'.
 //
 // Products (layouts as in attention.hip): a lane of S^T = K Q^T holds row lane %
-// 16 and keys 4 (lane / 16) + e of two 16-key tiles, its probabilities are the
-// right operand of O^T += V^T P^T as they are, and V^T's fragments are transposing
-// LDS reads in the same key order.
+// 16 and keys 4 (lane / 16) + e of 16-key tiles, its probabilities are the right
+// operand of O^T += V^T P^T as they are, and V^T's fragments are transposing LDS
+// reads in the same key order.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -50,6 +54,7 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 // lists that the kernel never writes: uniform reads go through the scalar cache
@@ -83,6 +88,12 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {   // round t
 }
 __device__ __forceinline__ float weight_of(float m, float top) {   // exp2(m - top), 0 for m = -inf
     return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+}
+
+// a / b for a >= 0, b > 0: 64-bit division takes its time
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    if (((a | b) >> 32) == 0) return (uint32_t)a / (uint32_t)b;
+    return a / b;
 }
 
 // A value that is the same in every lane, kept in scalar registers.
@@ -184,7 +195,7 @@ __device__ __forceinline__ Unit unit_at(const Args& a, int s, int64_t start, int
     u.s = s;
     u.q = seq_of(a, s);
     const int64_t head = plan::steps_before(u.q, u.q.blocks, a.rows, causal);
-    u.head = __builtin_amdgcn_readfirstlane((int)((at - start) / head));
+    u.head = __builtin_amdgcn_readfirstlane((int)quotient(at - start, head));
     const int64_t h0 = start + u.head * head;
     u.block = __builtin_amdgcn_readfirstlane(plan::block_of(u.q, at - h0, a.rows, causal));
     u.u0 = uniform(h0 + plan::steps_before(u.q, u.block, a.rows, causal));
@@ -200,12 +211,154 @@ __device__ __forceinline__ int64_t share_index(int bid, int64_t used) {
     return x * base + (x < rem ? x : rem) + bid / kXcds;
 }
 
-// A piece's results in the workspace: BM rows of 128 sums, BM maxima (base 2),
-// BM sums of weights; slot 0 of a share for a unit that began before it, 1 for one
-// that goes on behind it.
+// The workspace: a record of every share, then two slots per share.  The record
+// tells join_kernel of the unit that begins in the share and goes on behind it (last:
+// the share of its last step, -1 for no such unit).  A slot holds a piece's
+// results, BM rows of 128 sums, BM maxima (base 2), BM sums of weights: slot 0 for a
+// unit that began before the share, 1 for the one that goes on behind it.
+struct Record {
+    int last, token, tokens, head;    // token: its first row of the step's buffers
+};
+constexpr int kRecordFloats = kGroups * (int)sizeof(Record) / 4;
 template <int BM>
 __device__ __forceinline__ float* slot_of(float* ws, int64_t share, int slot) {
-    return ws + (share * 2 + slot) * (int64_t)(BM * (D + 2));
+    return ws + kRecordFloats + (share * 2 + slot) * (int64_t)(BM * (D + 2));
+}
+__device__ __forceinline__ void leave_record(const Args& a, int64_t share, const Record& r) {
+    if (threadIdx.x == 0) reinterpret_cast<Record*>(a.ws)[share] = r;
+}
+__device__ __forceinline__ Record record_of(const Args& a, const Unit& u, int64_t per) {
+    const int tok = u.block * a.rows;
+    return Record{(int)quotient(u.u1 - 1, per), u.q.first + tok, min(a.rows, u.q.fresh - tok), u.head};
+}
+
+// Keys below this one are seen by every row of a unit.
+__device__ __forceinline__ int seen_by_all(const Args& a, const Unit& u) {
+    return u.q.ctx + (a.mask == nullptr ? min(u.block * a.rows + 1, u.q.fresh) : 0);
+}
+
+// Bit i: new token `tok` of the unit's sequence (-1: no row) sees key base + i.
+__device__ __forceinline__ uint64_t sees_keys(const Args& a, const Unit& u, int tok, int base) {
+    if (tok < 0) return 0;
+    const int d0 = base - u.q.ctx;              // new token at the first place
+    if (a.mask == nullptr) {
+        const int n = tok + 1 - d0;
+        return n >= 64 ? ~0ull : (n <= 0 ? 0ull : (1ull << n) - 1);
+    }
+    if (d0 <= -64) return ~0ull;
+    const uint64_t* bits = a.mask + (int64_t)(u.q.first + tok) * a.words;
+    if (d0 < 0) return bits[0] << -d0 | ((1ull << -d0) - 1);   // cached tokens, then new ones
+    const int i = d0 >> 6, sh = d0 & 63;
+    uint64_t v = i < a.words ? bits[i] >> sh : 0;
+    if (sh > 0 && i + 1 < a.words) v |= bits[i + 1] << (64 - sh);
+    return v;
+}
+
+// Infinities and NaN among the bf16 values of 16 bytes.
+__device__ __forceinline__ bool any_odd(const u32x4& v) {
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        odd |= (v[e] & 0x7f80u) == 0x7f80u || (v[e] & 0x7f800000u) == 0x7f800000u;
+    return odd;
+}
+__device__ __forceinline__ bool is_odd(uint32_t b) { return (b & 0x7f80u) == 0x7f80u; }
+
+// V^T's fragment of a 32-key slice: two transposing reads 16 rows apart; with
+// `odd`, values that are not finite are left out (0 times them would reach the
+// sums of rows that do not see them).
+__device__ __forceinline__ bf16x8 v_fragment(const uint16_t* p, bool odd) {
+    i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p);
+    i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 16 * D));
+    if (odd) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (is_odd((uint16_t)lo[e])) lo[e] = 0;
+            if (is_odd((uint16_t)hi[e])) hi[e] = 0;
+        }
+    }
+    const i16x8 vv = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    return __builtin_bit_cast(bf16x8, vv);
+}
+// The infinities and NaN that the rows do see: o(row lane % 16, value 16 dt + 4 g +
+// e) += p(row, key) v(key, value) for the 32 keys of a slice, key by key.  pf: the
+// lane's weights, sees: bits of its row.
+__device__ __forceinline__ void add_odd(const uint16_t* vt, const bf16x8& pf, uint32_t sees,
+                                        f32x4 (&o)[8]) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, l16 = lane & 15;
+    const u32x4 pw = __builtin_bit_cast(u32x4, pf);
+    for (int key = 0; key < 32; ++key) {
+        const int i = 4 * (key >> 4) + (key & 3);          // of the holding lane's eight
+        uint32_t word = i < 4 ? (i < 2 ? pw[0] : pw[1]) : (i < 6 ? pw[2] : pw[3]);
+        word = __shfl(word, 16 * ((key & 15) >> 2) + l16);
+        const float p = __uint_as_float(i & 1 ? word & 0xffff0000u : word << 16);
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int col = 16 * dt + 4 * g + e;
+                const uint32_t b = vt[key * D + vpos(key, col >> 3) * 8 + (col & 7)];
+                if (is_odd(b) && (sees >> key & 1)) o[dt][e] += p * __uint_as_float(b << 16);
+            }
+    }
+}
+
+// Softmax of a row's new scores (N 16-key tiles, scaled to base 2): weights in sc,
+// running maximum, sum (the lane's own keys; joined at the end) and output moved.
+template <int N>
+__device__ __forceinline__ void softmax_step(f32x4 (&sc)[N], float scale, float& m, float& l,
+                                             f32x4 (&o)[8]) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        mx = fmaxf(mx, fmaxf(fmaxf(sc[j][0], sc[j][1]), fmaxf(sc[j][2], sc[j][3])));
+    const float mnew = fmaxf(m, row_max4(mx) * scale);
+    // the exponentials' reference moves when a row gains more than kSlack on it;
+    // results differ by rounding only
+    if (__builtin_amdgcn_ballot_w64(mnew > m + kSlack) != 0) {
+        const float alpha = weight_of(m, mnew);
+        l *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) o[dt] *= alpha;
+        m = mnew;
+    }
+    const float msub = m == -INFINITY ? 0.f : m;
+    float rs = 0.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            sc[j][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[j][e], scale, -msub));
+            rs += sc[j][e];
+        }
+    l += rs;
+}
+
+// Weights of a 32-key slice as the products' operand, rounded to bf16 (half a step
+// is 2^-9 of a weight, as in attention.hip; their sum is not rounded).
+__device__ __forceinline__ bf16x8 round_weights(const f32x4& a, const f32x4& b) {
+    return __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]),
+                                            pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])});
+}
+// What that rounding left, rounded in turn: with both products a weight keeps 16
+// bits.
+__device__ __forceinline__ bf16x8 weights_left(const f32x4& a, const f32x4& b, const bf16x8& r) {
+    const u32x4 w = __builtin_bit_cast(u32x4, r);
+    f32x4 x, y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t p = w[e >> 1], q = w[2 + (e >> 1)];
+        x[e] = a[e] - __uint_as_float(e & 1 ? p & 0xffff0000u : p << 16);
+        y[e] = b[e] - __uint_as_float(e & 1 ? q & 0xffff0000u : q << 16);
+    }
+    return round_weights(x, y);
+}
+
+__device__ __forceinline__ float inverse_sum(float l) {   // 0 for a row that saw nothing
+    return l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);       // NaN stays
+}
+__device__ __forceinline__ float log_sum(float m, float l) {
+    return l == 0.f ? -INFINITY : kLn2 * m + logf(l);
 }
 
 template <int RT>
@@ -220,15 +373,18 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
     const bool causal = a.mask == nullptr;
 
     const Line ln = lay_out(a, sums);
-    if (ln.total == 0) return;
     const int64_t per = uniform(plan::share(ln.total, kGroups, kLeastSteps));
-    const int64_t used = uniform((ln.total + per - 1) / per);
-    if (blockIdx.x >= used) return;
+    const int64_t used = uniform(quotient(ln.total + per - 1, per));
+    if (blockIdx.x >= used) {
+        leave_record(a, blockIdx.x, Record{-1, 0, 0, 0});
+        return;
+    }
     const int64_t share = share_index(blockIdx.x, used);
     const int64_t begin = share * per, end = min(begin + per, ln.total);
     int s;
     int64_t start;
     find_seq(a, ln, begin, found, &s, &start);
+    Record record = {-1, 0, 0, 0};
 
     uint16_t* kt = tiles[wave][0];
     uint16_t* vt = tiles[wave][1];
@@ -259,6 +415,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
         const Unit u = unit_at(a, s, start, at);
         const int t0 = (int)(at - u.u0), t1 = (int)(min(end, u.u1) - u.u0);
         const int lim = plan::block_keys(u.q, u.block, a.rows, causal);
+        const int all = seen_by_all(a, u);
         const const_ints table =
             (const_ints)(uintptr_t)(a.batch.table + (int64_t)u.s * a.batch.ld_table);
         const int64_t head0 = ((int64_t)u.head << shift) * D;
@@ -357,34 +514,16 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
             if (next) copy(nxt, base_of(t + 1), 0, kt, true);
 
             // what the rows see of these 32 keys, where that is not everything
-            const bool masked = base + KT > u.q.ctx || base + KT > lim || cur.page[0] < 0 ||
-                                cur.page[1] < 0;
+            const bool masked =
+                base + KT > all || base + KT > lim || cur.page[0] < 0 || cur.page[1] < 0;
             uint32_t sees[RT];
             if (masked) {
                 uint32_t there = (cur.page[0] < 0 ? 0u : 0xffffu) |
                                  (cur.page[1] < 0 ? 0u : 0xffff0000u);
                 if (lim - base < KT) there &= (1u << (lim - base)) - 1;
-                const int d0 = base - u.q.ctx;      // new token at the tile's first place
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
-                    uint32_t w = 0;
-                    if (tok[r] >= 0 && causal) {
-                        const int n = tok[r] + 1 - d0;
-                        w = n >= KT ? ~0u : (n <= 0 ? 0u : (1u << n) - 1);
-                    } else if (tok[r] >= 0) {
-                        const uint64_t* bits =
-                            a.mask + (int64_t)(u.q.first + tok[r]) * a.words;
-                        if (d0 < 0) {               // cached tokens, then new ones
-                            w = d0 <= -KT ? ~0u
-                                          : ((uint32_t)bits[0] << -d0) | ((1u << -d0) - 1);
-                        } else {
-                            const int i = d0 >> 6, sh = d0 & 63;
-                            uint64_t v = i < a.words ? bits[i] >> sh : 0;
-                            if (sh > 32 && i + 1 < a.words) v |= bits[i + 1] << (64 - sh);
-                            w = (uint32_t)v;
-                        }
-                    }
-                    sees[r] = w & there;
+                    sees[r] = (uint32_t)sees_keys(a, u, tok[r], base) & there;
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -392,99 +531,36 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
                             if (!(sees[r] >> (16 * j + 4 * g + e) & 1)) sc[r][j][e] = -INFINITY;
                 }
             }
-            bf16x8 pf[RT];
+            // the products have time to spare here: the weights' second halves too
+            bf16x8 pf[RT], pl[RT];
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                float mx = fmaxf(fmaxf(fmaxf(sc[r][0][0], sc[r][0][1]),
-                                       fmaxf(sc[r][0][2], sc[r][0][3])),
-                                 fmaxf(fmaxf(sc[r][1][0], sc[r][1][1]),
-                                       fmaxf(sc[r][1][2], sc[r][1][3])));
-                mx = row_max4(mx);
-                const float mnew = fmaxf(mrun[r], mx * a.scale_log2);
-                // the exponentials' reference moves when a row gains more than
-                // kSlack on it; results differ by rounding only
-                if (__builtin_amdgcn_ballot_w64(mnew > mrun[r] + kSlack) != 0) {
-                    const float alpha = weight_of(mrun[r], mnew);
-                    lrun[r] *= alpha;
-#pragma unroll
-                    for (int dt = 0; dt < 8; ++dt) o[r][dt] *= alpha;
-                    mrun[r] = mnew;
-                }
-                const float msub = mrun[r] == -INFINITY ? 0.f : mrun[r];
-                float p[2][4], rs = 0.f;
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        p[j][e] = __builtin_amdgcn_exp2f(
-                            __builtin_fmaf(sc[r][j][e], a.scale_log2, -msub));
-                        rs += p[j][e];
-                    }
-                lrun[r] += rs;             // the lane's own keys; joined at the end
-                // the weights are rounded to bf16 for the matrix product (half a step
-                // is 2^-9 of a weight, as in attention.hip); their sum is not
-                const u32x4 pw = {pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]),
-                                  pack_bf16x2(p[1][0], p[1][1]), pack_bf16x2(p[1][2], p[1][3])};
-                pf[r] = __builtin_bit_cast(bf16x8, pw);
+                softmax_step(sc[r], a.scale_log2, mrun[r], lrun[r], o[r]);
+                pf[r] = round_weights(sc[r][0], sc[r][1]);
+                pl[r] = weights_left(sc[r][0], sc[r][1], pf[r]);
             }
             if (next) dma::wait_vmcnt<8>();             // V has landed, the next K may not have
             else dma::wait_vmcnt<0>();
-            // a masked place may hold anything; 0 times an infinity or NaN would still
-            // reach the sums, so such values take another way
+            // a masked place may hold anything
             bool odd = false;
             if (masked) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const u32x4 v = *reinterpret_cast<const u32x4*>(vt + (i * 64 + lane) * 8);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        odd |= (v[e] & 0x7f80u) == 0x7f80u || (v[e] & 0x7f800000u) == 0x7f800000u;
-                }
+                for (int i = 0; i < 8; ++i)
+                    odd |= any_odd(*reinterpret_cast<const u32x4*>(vt + (i * 64 + lane) * 8));
                 odd = __builtin_amdgcn_ballot_w64(odd) != 0;
             }
 #pragma unroll
             for (int dt = 0; dt < 8; ++dt) {
-                const uint16_t* p0 = vt + vread[dt];
-                i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p0);
-                i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p0 + 16 * D));
-                if (odd) {
+                const bf16x8 vf = v_fragment(vt + vread[dt], odd);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if ((lo[e] & 0x7f80) == 0x7f80) lo[e] = 0;
-                        if ((hi[e] & 0x7f80) == 0x7f80) hi[e] = 0;
-                    }
-                }
-                const i16x8 vv = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-                const bf16x8 vf = __builtin_bit_cast(bf16x8, vv);
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
+                for (int r = 0; r < RT; ++r) {
                     o[r][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r], o[r][dt], 0, 0, 0);
+                    o[r][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl[r], o[r][dt], 0, 0, 0);
+                }
             }
             if (odd) {
-                // the infinities and NaN that a row does see: o(row l16, value 16 dt +
-                // 4 g + e) += p(row, key) v(key, value), key by key
-                for (int key = 0; key < KT; ++key) {
-                    const int from = 16 * ((key & 15) >> 2) + l16;    // the lane with p(row, key)
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) {
-                        const u32x4 pw = __builtin_bit_cast(u32x4, pf[r]);
-                        const int i = 4 * (key >> 4) + (key & 3);      // of the lane's eight
-                        uint32_t word = i < 4 ? (i < 2 ? pw[0] : pw[1]) : (i < 6 ? pw[2] : pw[3]);
-                        word = __shfl(word, from);
-                        const float p = __uint_as_float(i & 1 ? word & 0xffff0000u : word << 16);
-                        if (!(sees[r] >> key & 1)) continue;
-#pragma unroll
-                        for (int dt = 0; dt < 8; ++dt)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const int col = 16 * dt + 4 * g + e;
-                                const uint32_t b =
-                                    vt[key * D + vpos(key, col >> 3) * 8 + (col & 7)];
-                                if ((b & 0x7f80u) == 0x7f80u)
-                                    o[r][dt][e] += p * __uint_as_float(b << 16);
-                            }
-                    }
-                }
+                for (int r = 0; r < RT; ++r) add_odd(vt, pf[r], sees[r], o[r]);
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // V's tile has been read
             if (next) copy(nxt, base_of(t + 1), half, vt, false);
@@ -503,6 +579,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
             }
         }
         const bool whole = t0 == 0 && u.u1 <= end;
+        if (t0 == 0 && !whole) record = record_of(a, u, per);
         float* slot = slot_of<BM>(a.ws, share, t0 > 0 ? 0 : 1);
         float* red = reinterpret_cast<float*>(&tiles[wave][0][0]);     // 16 rows of kRed
         const int orow = threadIdx.x >> 4, ocol = (threadIdx.x & 15) * 8;
@@ -536,15 +613,14 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
                 const int hq = u.head * a.group + row - j * a.group;
                 const int64_t token = u.q.first + tk;
                 if (whole) {
-                    const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);   // NaN stays
+                    const float inv = inverse_sum(l);
                     const u32x4 w = {pack_bf16x2(v[0] * inv, v[1] * inv),
                                      pack_bf16x2(v[2] * inv, v[3] * inv),
                                      pack_bf16x2(v[4] * inv, v[5] * inv),
                                      pack_bf16x2(v[6] * inv, v[7] * inv)};
                     *reinterpret_cast<u32x4*>(a.out + token * a.ldo + (int64_t)hq * D + ocol) = w;
                     if (a.lse && ocol == 0)
-                        a.lse[(int64_t)hq * a.tokens + token] =
-                            l == 0.f ? -INFINITY : kLn2 * m + logf(l);
+                        a.lse[(int64_t)hq * a.tokens + token] = log_sum(m, l);
                 } else {
                     float* p = slot + row * D + ocol;
                     *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
@@ -559,88 +635,350 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
         }
         at = u.u0 + t1;
         // the next unit of the line: another block or head, or a later sequence
-        const int64_t all = uniform(seq_steps(a, u.q));
-        if (at >= start + all) {
-            start += all;
+        const int64_t steps = uniform(seq_steps(a, u.q));
+        if (at >= start + steps) {
+            start += steps;
             ++s;
+        }
+    }
+    leave_record(a, share, record);
+}
+
+// Many rows: BM = 128, four waves of two 16-row blocks, keys in tiles of 64 that the
+// waves copy together, two buffers, one barrier per tile.  The copies of the next
+// tile are issued between the score products, a quarter (16 keys: one page) at a
+// time.
+constexpr int kWideRows = 128;
+constexpr int WT = 64;                 // keys of a tile
+__global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
+    constexpr int RB = 2;
+    __shared__ __attribute__((aligned(16))) uint16_t tiles[2][2][WT * D];
+    __shared__ int64_t sums[NWAVE], found[2];
+    const int lane = threadIdx.x & 63, g = lane >> 4, l16 = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool causal = a.mask == nullptr;
+
+    const Line ln = lay_out(a, sums);
+    const int64_t per = uniform(plan::share(ln.total, kGroups, kLeastSteps));
+    const int64_t used = uniform(quotient(ln.total + per - 1, per));
+    if (blockIdx.x >= used) {
+        leave_record(a, blockIdx.x, Record{-1, 0, 0, 0});
+        return;
+    }
+    const int64_t share = share_index(blockIdx.x, used);
+    const int64_t begin = share * per, end = min(begin + per, ln.total);
+    int s;
+    int64_t start;
+    find_seq(a, ln, begin, found, &s, &start);
+    Record record = {-1, 0, 0, 0};
+
+    // copy round r fills tile rows 16 r + 4 wave + lane / 16, place lane % 16
+    const int crow = 4 * wave + g;
+    const uint32_t koff = (uint32_t)(crow * D * 2 + kpos(crow, l16) * 16);
+    const uint32_t voff = (uint32_t)(crow * D * 2 + vpos(crow, l16) * 16);
+    int kread[4], vread[8];
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) kread[ks] = l16 * D + kpos(l16, 4 * ks + g) * 8;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) {
+        const int r = 4 * g + (l16 >> 2), col = 16 * dt + 4 * (l16 & 3);
+        vread[dt] = r * D + vpos(r, col >> 3) * 8 + (col & 7);
+    }
+    const int shift = a.cache.page_shift;
+    const int64_t half = ((int64_t)a.cache.kv_heads << shift) * D;   // K to V of a page
+
+    for (int64_t at = begin; at < end;) {
+        if (seq_of(a, s).blocks == 0) {        // no new tokens: no steps either
+            ++s;
+            continue;
+        }
+        const Unit u = unit_at(a, s, start, at);
+        const int t0 = (int)(at - u.u0), t1 = (int)(min(end, u.u1) - u.u0);
+        const int lim = plan::block_keys(u.q, u.block, a.rows, causal);
+        const int all = seen_by_all(a, u);
+        const const_ints table =
+            (const_ints)(uintptr_t)(a.batch.table + (int64_t)u.s * a.batch.ld_table);
+        const int64_t head0 = ((int64_t)u.head << shift) * D;
+        auto page_at = [&](int key) {          // uniform; -1: nothing to read
+            const int col = key >> shift;
+            const int e = key < lim && col < a.batch.max_pages ? table[col] : -1;
+            return e >= 0 && e < a.cache.n_pages ? e : -1;
+        };
+        // keys [key, key + 16) of K and V into rows 16 r .. of a buffer
+        auto copy = [&](int page, int key, int buf, int r) {
+            const int left = __builtin_amdgcn_readfirstlane(
+                page < 0 ? 0 : min(max(lim - key, 0), 16));
+            const uint16_t* src = a.cache.pages + (int64_t)max(page, 0) * 2 * half + head0 +
+                                  (int64_t)(key & ((1 << shift) - 1)) * D;
+            uint16_t* dst = tiles[buf][0] + (16 * r + 4 * wave) * D;
+            dma::lds_dma16(dma::rsrc_words(src, (int64_t)left * D * 2), dst, koff, 0u);
+            dma::lds_dma16(dma::rsrc_words(src + half, (int64_t)left * D * 2), dst + WT * D, voff,
+                           0u);
+        };
+
+        int tok[RB], hq[RB];
+        bf16x8 qf[RB][4];
+        f32x4 o[RB][8];
+        float mrun[RB], lrun[RB];
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            const int row = 32 * wave + 16 * r + l16;
+            const int j = row / a.group;
+            hq[r] = u.head * a.group + row - j * a.group;
+            tok[r] = u.block * a.rows + j;
+            const bool on = j < a.rows && tok[r] < u.q.fresh;
+            if (!on) tok[r] = -1;
+            const uint16_t* q = a.q + (int64_t)(u.q.first + tok[r]) * a.ldq + (int64_t)hq[r] * D;
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+                qf[r][ks] = on ? *reinterpret_cast<const bf16x8*>(q + 32 * ks + 8 * g)
+                               : __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+            mrun[r] = -INFINITY;
+            lrun[r] = 0.f;
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) o[r][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+
+        const int first = t0 * plan::kStep;
+        const int last = min(t1 * plan::kStep, lim);      // keys [first, last) of the piece
+        int page[4], there = 0;
+        if (first < last) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                page[r] = page_at(first + 16 * r);
+                copy(page[r], first + 16 * r, 0, r);
+            }
+        }
+        dma::wait_vmcnt<0>();
+        __syncthreads();
+        int buf = 0;
+        for (int base = first; base < last; base += WT, buf ^= 1) {
+            const uint16_t* kt = tiles[buf][0];
+            const uint16_t* vt = tiles[buf][1];
+            there = 0;                                     // 16-key groups with a page
+#pragma unroll
+            for (int r = 0; r < 4; ++r) there |= (page[r] >= 0 ? 1 : 0) << r;
+            const bool next = base + WT < last;
+            if (next) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) page[r] = page_at(base + WT + 16 * r);
+            }
+            f32x4 sc[RB][4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int r = 0; r < RB; ++r) sc[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bf16x8 kf =
+                        *reinterpret_cast<const bf16x8*>(kt + 16 * j * D + kread[ks]);
+#pragma unroll
+                    for (int r = 0; r < RB; ++r)
+                        sc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][ks], sc[r][j],
+                                                                           0, 0, 0);
+                }
+                // the other buffer was last read before the last barrier
+                if (next) copy(page[ks], base + WT + 16 * ks, buf ^ 1, ks);
+            }
+            const bool masked = base + WT > all || base + WT > lim || there != 15;
+            uint64_t sees[RB];
+            bool odd = false;
+            if (masked) {
+                uint64_t on = 0;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (there >> r & 1) on |= 0xffffull << (16 * r);
+                if (lim - base < WT) on &= (1ull << (lim - base)) - 1;
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    sees[r] = sees_keys(a, u, tok[r], base) & on;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!(sees[r] >> (16 * j + 4 * g + e) & 1)) sc[r][j][e] = -INFINITY;
+                }
+                // a masked place may hold anything
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    odd |= any_odd(*reinterpret_cast<const u32x4*>(vt + (i * 64 + lane) * 8));
+                odd = __builtin_amdgcn_ballot_w64(odd) != 0;
+            }
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+                softmax_step(sc[r], a.scale_log2, mrun[r], lrun[r], o[r]);
+#pragma unroll
+            for (int sl = 0; sl < 2; ++sl) {
+                bf16x8 pf[RB];
+#pragma unroll
+                for (int r = 0; r < RB; ++r) pf[r] = round_weights(sc[r][2 * sl], sc[r][2 * sl + 1]);
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) {
+                    const bf16x8 vf = v_fragment(vt + 32 * sl * D + vread[dt], odd);
+#pragma unroll
+                    for (int r = 0; r < RB; ++r)
+                        o[r][dt] =
+                            __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r], o[r][dt], 0, 0, 0);
+                }
+                if (odd) {
+#pragma unroll
+                    for (int r = 0; r < RB; ++r)
+                        add_odd(vt + 32 * sl * D, pf[r], (uint32_t)(sees[r] >> (32 * sl)), o[r]);
+                }
+            }
+            dma::wait_vmcnt<0>();
+            __syncthreads();
+        }
+
+        const bool whole = t0 == 0 && u.u1 <= end;
+        if (t0 == 0 && !whole) record = record_of(a, u, per);
+        float* slot = slot_of<kWideRows>(a.ws, share, t0 > 0 ? 0 : 1);
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            const float l = row_sum4(lrun[r]);
+            if (tok[r] < 0) continue;
+            const int64_t token = u.q.first + tok[r];
+            if (whole) {
+                const float inv = inverse_sum(l);
+                uint16_t* p = a.out + token * a.ldo + (int64_t)hq[r] * D + 4 * g;
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt)
+                    *reinterpret_cast<u32x2*>(p + 16 * dt) =
+                        u32x2{pack_bf16x2(o[r][dt][0] * inv, o[r][dt][1] * inv),
+                              pack_bf16x2(o[r][dt][2] * inv, o[r][dt][3] * inv)};
+                if (a.lse && g == 0) a.lse[(int64_t)hq[r] * a.tokens + token] = log_sum(mrun[r], l);
+            } else {
+                const int row = 32 * wave + 16 * r + l16;
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt)
+                    *reinterpret_cast<f32x4*>(slot + row * D + 16 * dt + 4 * g) = o[r][dt];
+                if (g == 0) {
+                    slot[kWideRows * D + row] = mrun[r];
+                    slot[kWideRows * D + kWideRows + row] = l;
+                }
+            }
+        }
+        at = u.u0 + t1;
+        // the next unit of the line: another block or head, or a later sequence
+        const int64_t steps = uniform(seq_steps(a, u.q));
+        if (at >= start + steps) {
+            start += steps;
+            ++s;
+        }
+    }
+    leave_record(a, share, record);
+}
+
+// The unit that begins in share blockIdx.x and goes on behind it: its pieces are
+// slot 1 of that share and slot 0 of the following ones, added in order.  Few pieces:
+// a wave per row.  Many (a long context): the workgroup takes its R rows one by one,
+// eight half waves every eighth piece each, four values per lane.
+constexpr int kManyPieces = 16;
+template <int BM, int R>
+__global__ __launch_bounds__(NTHR) void join_kernel(Args a) {
+    constexpr int H = NTHR / 32;
+    __shared__ float tops[H], parts[H][D + 4];
+    const int64_t share = blockIdx.x;
+    const Record rec = reinterpret_cast<const Record*>(a.ws)[share];
+    if (rec.last < 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hw = tid / 32, l32 = tid & 31;
+    const int n = min(rec.tokens * a.group, BM);      // rows of the unit
+    auto piece = [&](int i) { return slot_of<BM>(a.ws, share + i, i == 0); };
+    auto finish = [&](int row, int value, float x, float y, float top, float l) {
+        const int j = row / a.group, hq = rec.head * a.group + row - j * a.group;
+        const int64_t token = rec.token + j;
+        const float inv = inverse_sum(l);
+        *reinterpret_cast<uint32_t*>(a.out + token * a.ldo + (int64_t)hq * D + value) =
+            pack_bf16x2(x * inv, y * inv);
+        if (a.lse && value == 0) a.lse[(int64_t)hq * a.tokens + token] = log_sum(top, l);
+    };
+    const int pieces = rec.last - (int)share + 1;
+    for (int row0 = blockIdx.y * R; row0 < n; row0 += gridDim.y * R) {
+        if (pieces <= kManyPieces) {
+            for (int row = row0 + wave; row < min(row0 + R, n); row += NWAVE) {
+                float top = lane < pieces ? piece(lane)[BM * D + row] : -INFINITY;
+#pragma unroll
+                for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+                float x = 0.f, y = 0.f, l = 0.f;
+#pragma unroll 4
+                for (int i = 0; i < pieces; ++i) {
+                    const float* p = piece(i);
+                    const float f = weight_of(p[BM * D + row], top);
+                    const f32x2 v = *reinterpret_cast<const f32x2*>(p + row * D + 2 * lane);
+                    l += f * p[BM * D + BM + row];
+                    x += f * v[0];
+                    y += f * v[1];
+                }
+                finish(row, 2 * lane, x, y, top, l);
+            }
+            continue;
+        }
+        for (int row = row0; row < min(row0 + R, n); ++row) {
+            float top = -INFINITY;
+            for (int i = tid; i < pieces; i += NTHR) top = fmaxf(top, piece(i)[BM * D + row]);
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+            if (l32 == 0) tops[hw] = top;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < H; ++i) top = fmaxf(top, tops[i]);
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+            float l = 0.f;
+#pragma unroll 8
+            for (int i = hw; i < pieces; i += H) {
+                const float* p = piece(i);
+                const float f = weight_of(p[BM * D + row], top);
+                l += f * p[BM * D + BM + row];
+                sum += f * *reinterpret_cast<const f32x4*>(p + row * D + 4 * l32);
+            }
+            *reinterpret_cast<f32x4*>(&parts[hw][4 * l32]) = sum;
+            if (l32 == 0) parts[hw][D] = l;
+            __syncthreads();
+            if (tid < D / 2) {
+                float x = 0.f, y = 0.f;
+                l = 0.f;
+#pragma unroll
+                for (int i = 0; i < H; ++i) {
+                    x += parts[i][2 * tid];
+                    y += parts[i][2 * tid + 1];
+                    l += parts[i][D];
+                }
+                finish(row, 2 * tid, x, y, top, l);
+            }
+            __syncthreads();
         }
     }
 }
 
-// The unit that is cut at the end of share blockIdx.x, if it began there: its
-// pieces are slot 1 of that share and slot 0 of the following ones.  A wave joins
-// one row.
-template <int RT>
-__global__ __launch_bounds__(NTHR) void join_kernel(Args a) {
-    constexpr int BM = 16 * RT;
-    __shared__ int64_t sums[NWAVE], found[2];
-    const int lane = threadIdx.x & 63;
-    const Line ln = lay_out(a, sums);
-    if (ln.total == 0) return;
-    const int64_t per = plan::share(ln.total, kGroups, kLeastSteps);
-    const int64_t share = blockIdx.x;
-    const int64_t begin = share * per, end = begin + per;
-    if (end >= ln.total) return;                    // nothing follows
-    int s;
-    int64_t start;
-    find_seq(a, ln, end - 1, found, &s, &start);
-    const Unit u = unit_at(a, s, start, end - 1);
-    if (u.u1 <= end || u.u0 < begin) return;
-    const int64_t last = (u.u1 - 1) / per;          // share of its last step
-    const int row = blockIdx.y * NWAVE + (threadIdx.x >> 6);
-    const int j = row / a.group, tk = u.block * a.rows + j;
-    if (j >= a.rows || tk >= u.q.fresh) return;
-
-    float top = -INFINITY;
-    for (int64_t w = share + lane; w <= last; w += 64)
-        top = fmaxf(top, slot_of<BM>(a.ws, w, w == share)[BM * D + row]);
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    f32x2 sum = {0.f, 0.f};
-    float l = 0.f;
-#pragma unroll 4
-    for (int64_t w = share; w <= last; ++w) {
-        const float* p = slot_of<BM>(a.ws, w, w == share);
-        const float f = weight_of(p[BM * D + row], top);
-        l += f * p[BM * D + BM + row];
-        const f32x2 v = *reinterpret_cast<const f32x2*>(p + row * D + 2 * lane);
-        sum[0] += f * v[0];
-        sum[1] += f * v[1];
-    }
-    const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-    const int hq = u.head * a.group + row - j * a.group;
-    const int64_t token = u.q.first + tk;
-    *reinterpret_cast<uint32_t*>(a.out + token * a.ldo + (int64_t)hq * D + 2 * lane) =
-        pack_bf16x2(sum[0] * inv, sum[1] * inv);
-    if (a.lse && lane == 0)
-        a.lse[(int64_t)hq * a.tokens + token] = l == 0.f ? -INFINITY : kLn2 * top + logf(l);
-}
-
-// 16-row tiles of a unit: as few as hold a sequence's rows, at most four.
-int row_tiles(int group, int max_new) {
+// Rows of a unit: 16 or 32 while they hold a sequence's rows (the bytes count), else
+// 128 (the products do).  A token's heads stay together.
+int unit_rows(int group, int max_new) {
     const int64_t rows = (int64_t)group * max_new;
-    const int need = rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
-    const int least = group <= 16 ? 1 : (group <= 32 ? 2 : 4);   // a token's heads stay together
-    return std::max(need, least);
+    return rows <= 16 ? 16 : (rows <= 32 ? 32 : kWideRows);
 }
 
-template <int RT>
-hipError_t launch(const Args& a, unsigned grid, hipStream_t s) {
-    attention_cache_kernel<RT><<<grid, NTHR, 0, s>>>(a);
+// rows: what a unit is expected to hold; the joining workgroups walk all it has
+template <int BM, int R>
+hipError_t launch(void (*kernel)(Args), const Args& a, unsigned grid, int64_t rows,
+                  hipStream_t s) {
+    kernel<<<grid, NTHR, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || grid <= 1) return e;
-    join_kernel<RT><<<dim3(grid, 16 * RT / NWAVE), NTHR, 0, s>>>(a);
+    const unsigned per = (unsigned)((std::min<int64_t>(rows, BM) + R - 1) / R);
+    join_kernel<BM, R><<<dim3(grid, per), NTHR, 0, s>>>(a);
     return hipGetLastError();
 }
 
 }  // namespace
 
 int64_t cache_attention_ws_floats(int group, int max_new) {
-    return (int64_t)kGroups * 2 * 16 * row_tiles(group, max_new) * (D + 2);
+    return kRecordFloats + (int64_t)kGroups * 2 * unit_rows(group, max_new) * (D + 2);
 }
 
 hipError_t launch_cache_attention(const CacheAttentionProblem& p, hipStream_t s) {
-    const int rt = row_tiles(p.group, p.max_new);
+    const int bm = unit_rows(p.group, p.max_new);
     Args a = {};
     a.cache = p.cache;
     a.batch = p.batch;
@@ -651,19 +989,18 @@ hipError_t launch_cache_attention(const CacheAttentionProblem& p, hipStream_t s)
     a.ws = p.ws;
     a.tokens = (int)p.tokens;
     a.group = p.group;
-    a.rows = 16 * rt / p.group;
+    a.rows = bm / p.group;
     a.cap = (int64_t)p.batch.max_pages << p.cache.page_shift;
     a.scale_log2 = 1.4426950408889634f / sqrtf((float)D);
     // no batch of these sizes has more steps than this
     const int64_t units = std::min<int64_t>(p.batch.n_seqs, p.tokens) + p.tokens / a.rows;
-    const int64_t steps = 2 * ((a.cap + plan::kStep - 1) / plan::kStep) + 3;
+    const int64_t steps = 2 * ((a.cap + p.tokens) / plan::kStep) + 5;
     const int64_t most = std::min<int64_t>(units * p.cache.kv_heads, 1 << 20) * steps;
     const unsigned grid = (unsigned)std::min<int64_t>(kGroups, most);
-    switch (rt) {
-        case 1: return launch<1>(a, grid, s);
-        case 2: return launch<2>(a, grid, s);
-        default: return launch<4>(a, grid, s);
-    }
+    const int64_t rows = (int64_t)p.group * p.max_new;
+    if (bm == 16) return launch<16, 1>(attention_cache_kernel<1>, a, grid, rows, s);
+    if (bm == 32) return launch<32, 1>(attention_cache_kernel<2>, a, grid, rows, s);
+    return launch<kWideRows, 4>(attention_cache_wide_kernel, a, grid, rows, s);
 }
 
 }  // namespace atp
