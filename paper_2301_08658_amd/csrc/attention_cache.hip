@@ -232,6 +232,46 @@ __device__ __forceinline__ Record record_of(const Args& a, const Unit& u, int64_
     return Record{(int)quotient(u.u1 - 1, per), u.q.first + tok, min(a.rows, u.q.fresh - tok), u.head};
 }
 
+// Where a unit's keys are: the table row, and a head's place in a page.
+struct Keys {
+    const_ints table;
+    int64_t head0, half;       // elements: the head in a page, and from keys to values
+    int lim, shift, max_pages, n_pages;
+    const uint16_t* pages;
+    // the page of a key that some row may see, -1 for none
+    __device__ __forceinline__ int page_at(int key) const {
+        const int col = key >> shift;
+        const int e = key < lim && col < max_pages ? table[col] : -1;
+        return e >= 0 && e < n_pages ? e : -1;
+    }
+    // N keys of one page from `key` on, as buffer resources of keys and values: rows at
+    // and behind lim, and all of a missing page, are past the range and read zeros
+    template <int N>
+    __device__ __forceinline__ void source(int page, int key, dma::u32x4& k, dma::u32x4& v) const {
+        const int left =
+            __builtin_amdgcn_readfirstlane(page < 0 ? 0 : min(max(lim - key, 0), N)) * D * 2;
+        const int64_t at = (int64_t)max(page, 0) * 2 * half + head0 +
+                           (int64_t)(key & ((1 << shift) - 1)) * D;
+        const uint64_t a = reinterpret_cast<uint64_t>(pages + at), b = a + (uint64_t)half * 2;
+        k = dma::u32x4{(uint32_t)a, (uint32_t)(a >> 32) & 0xffffu, (uint32_t)left,
+                       dma::kRsrcWord3};
+        v = dma::u32x4{(uint32_t)b, (uint32_t)(b >> 32) & 0xffffu, (uint32_t)left,
+                       dma::kRsrcWord3};
+    }
+};
+__device__ __forceinline__ Keys keys_of(const Args& a, const Unit& u, int lim) {
+    Keys k;
+    k.shift = a.cache.page_shift;
+    k.table = (const_ints)(uintptr_t)(a.batch.table + (int64_t)u.s * a.batch.ld_table);
+    k.head0 = ((int64_t)u.head << k.shift) * D;
+    k.half = ((int64_t)a.cache.kv_heads << k.shift) * D;
+    k.lim = lim;
+    k.max_pages = a.batch.max_pages;
+    k.n_pages = a.cache.n_pages;
+    k.pages = a.cache.pages;
+    return k;
+}
+
 // Keys below this one are seen by every row of a unit.
 __device__ __forceinline__ int seen_by_all(const Args& a, const Unit& u) {
     return u.q.ctx + (a.mask == nullptr ? min(u.block * a.rows + 1, u.q.fresh) : 0);
@@ -262,45 +302,54 @@ __device__ __forceinline__ bool any_odd(const u32x4& v) {
         odd |= (v[e] & 0x7f80u) == 0x7f80u || (v[e] & 0x7f800000u) == 0x7f800000u;
     return odd;
 }
-__device__ __forceinline__ bool is_odd(uint32_t b) { return (b & 0x7f80u) == 0x7f80u; }
-
-// V^T's fragment of a 32-key slice: two transposing reads 16 rows apart; with
-// `odd`, values that are not finite are left out (0 times them would reach the
-// sums of rows that do not see them).
-__device__ __forceinline__ bf16x8 v_fragment(const uint16_t* p, bool odd) {
-    i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p);
-    i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 16 * D));
-    if (odd) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (is_odd((uint16_t)lo[e])) lo[e] = 0;
-            if (is_odd((uint16_t)hi[e])) hi[e] = 0;
-        }
-    }
+// V^T's fragment of a 32-key slice: two transposing reads 16 rows apart.
+__device__ __forceinline__ bf16x8 v_fragment(const uint16_t* p) {
+    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p);
+    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 16 * D));
     const i16x8 vv = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     return __builtin_bit_cast(bf16x8, vv);
 }
-// The infinities and NaN that the rows do see: o(row lane % 16, value 16 dt + 4 g +
-// e) += p(row, key) v(key, value) for the 32 keys of a slice, key by key.  pf: the
+// Infinities and NaN of a 32-key slice of V where not every row sees them: 0 times them
+// would reach the other rows' sums in a matrix product, so what the rows do see is
+// added here, key by key, o(row lane % 16, value 16 dt + 4 g + e) += p(row, key) v(key,
+// value), and the slice is cleared of them (clear_odd) before the product.  pf: the
 // lane's weights, sees: bits of its row.
+__device__ __forceinline__ float odd_value(uint32_t b) {   // of the low half; else 0
+    return (b & 0x7f80u) == 0x7f80u ? __uint_as_float(b << 16) : 0.f;
+}
 __device__ __forceinline__ void add_odd(const uint16_t* vt, const bf16x8& pf, uint32_t sees,
                                         f32x4 (&o)[8]) {
     const int lane = threadIdx.x & 63, g = lane >> 4, l16 = lane & 15;
     const u32x4 pw = __builtin_bit_cast(u32x4, pf);
+#pragma unroll 1
     for (int key = 0; key < 32; ++key) {
         const int i = 4 * (key >> 4) + (key & 3);          // of the holding lane's eight
         uint32_t word = i < 4 ? (i < 2 ? pw[0] : pw[1]) : (i < 6 ? pw[2] : pw[3]);
         word = __shfl(word, 16 * ((key & 15) >> 2) + l16);
         const float p = __uint_as_float(i & 1 ? word & 0xffff0000u : word << 16);
+        if (!(sees >> key & 1)) continue;
+        int g_ = g;
+        asm volatile("" : "+v"(g_));      // addresses are formed here, not kept in registers
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt)
+        for (int dt = 0; dt < 8; ++dt) {
+            const u32x2 b = *reinterpret_cast<const u32x2*>(
+                vt + key * D + vpos(key, 2 * dt + (g_ >> 1)) * 8 + 4 * (g_ & 1));
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int col = 16 * dt + 4 * g + e;
-                const uint32_t b = vt[key * D + vpos(key, col >> 3) * 8 + (col & 7)];
-                if (is_odd(b) && (sees >> key & 1)) o[dt][e] += p * __uint_as_float(b << 16);
+                const uint32_t v = e & 1 ? b[e >> 1] >> 16 : b[e >> 1];
+                if (odd_value(v) != 0.f) o[dt][e] += p * odd_value(v);   // NaN != 0 too
             }
+        }
     }
+}
+__device__ __forceinline__ void clear_odd(u32x4* chunk) {
+    u32x4 v = *chunk;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if ((v[e] & 0x7f80u) == 0x7f80u) v[e] &= 0xffff0000u;
+        if ((v[e] & 0x7f800000u) == 0x7f800000u) v[e] &= 0xffffu;
+    }
+    *chunk = v;
 }
 
 // Softmax of a row's new scores (N 16-key tiles, scaled to base 2): weights in sc,
@@ -361,7 +410,8 @@ __device__ __forceinline__ float log_sum(float m, float l) {
     return l == 0.f ? -INFINITY : kLn2 * m + logf(l);
 }
 
-template <int RT>
+// SMALL: pages of 16 tokens, so that a wave's tile of 32 keys spans two.
+template <int RT, bool SMALL>
 __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
     constexpr int BM = 16 * RT;
     constexpr int kRed = D + 4;      // padded row of the merge
@@ -404,9 +454,6 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
         const int r = 4 * g + (l16 >> 2), col = 16 * dt + 4 * (l16 & 3);
         vread[dt] = r * D + vpos(r, col >> 3) * 8 + (col & 7);
     }
-    const int shift = a.cache.page_shift;
-    const int64_t half = ((int64_t)a.cache.kv_heads << shift) * D;   // K to V of a page
-
     for (int64_t at = begin; at < end;) {
         if (seq_of(a, s).blocks == 0) {        // no new tokens: no steps either
             ++s;
@@ -416,14 +463,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
         const int t0 = (int)(at - u.u0), t1 = (int)(min(end, u.u1) - u.u0);
         const int lim = plan::block_keys(u.q, u.block, a.rows, causal);
         const int all = seen_by_all(a, u);
-        const const_ints table =
-            (const_ints)(uintptr_t)(a.batch.table + (int64_t)u.s * a.batch.ld_table);
-        const int64_t head0 = ((int64_t)u.head << shift) * D;
-        auto page_at = [&](int key) {          // uniform
-            const int col = key >> shift;
-            const int e = col < a.batch.max_pages ? table[col] : -1;
-            return e >= 0 && e < a.cache.n_pages ? e : -1;
-        };
+        const Keys src = keys_of(a, u, lim);
 
         // rows: token block * rows + r / group of the sequence, query head r % group
         int tok[RT];
@@ -454,47 +494,54 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
 
         // the wave's tiles: keys [base, base + 32) of every step
         auto base_of = [&](int t) { return t * plan::kStep + KT * wave; };
+        constexpr int P = SMALL ? 2 : 1, PK = KT / P;     // pages of a tile, keys of each
         struct Tile {
-            int page[2];
+            int page[P];
+            dma::u32x4 k[P], v[P];
         };
-        auto pages_of = [&](int base) {
-            Tile p;
-            p.page[0] = base < lim ? page_at(base) : -1;
-            p.page[1] = base + 16 < lim ? page_at(base + 16) : -1;
-            return p;
+        auto look_up = [&](int base, int (&page)[P]) {
+#pragma unroll
+            for (int h = 0; h < P; ++h) page[h] = src.page_at(base + PK * h);
         };
-        // half h of a tile: 16 rows of one page; rows at and behind lim, and those of an
-        // empty place, are past the range and read zeros
-        auto copy = [&](const Tile& p, int base, int64_t kv, uint16_t* dst, bool keys) {
+        auto aim = [&](int base, const int (&page)[P]) {
+            Tile tl;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int key = base + 16 * h;
-                const int page = max(p.page[h], 0);
-                const int left = __builtin_amdgcn_readfirstlane(
-                    p.page[h] < 0 ? 0 : min(max(lim - key, 0), 16));
-                const uint16_t* src = a.cache.pages + (int64_t)page * 2 * half + kv + head0 +
-                                      (int64_t)(key & ((1 << shift) - 1)) * D;
-                const dma::u32x4 rs = dma::rsrc_words(src, (int64_t)left * D * 2);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    dma::lds_dma16(rs, dst + (16 * h + 4 * i) * D,
-                                   keys ? koffs[i] : voffs[i & 1] + (uint32_t)((i >> 1) * 8 * D * 2),
-                                   0u);
+            for (int h = 0; h < P; ++h) {
+                tl.page[h] = page[h];
+                src.source<PK>(page[h], base + PK * h, tl.k[h], tl.v[h]);
             }
+            return tl;
+        };
+        auto copy_keys = [&](const Tile& tl) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                dma::lds_dma16(tl.k[i * P / 8], kt + 4 * i * D,
+                               koffs[i & 3] + (SMALL ? 0u : (uint32_t)((i >> 2) * 16 * D * 2)), 0u);
+        };
+        auto copy_values = [&](const Tile& tl) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                dma::lds_dma16(tl.v[i * P / 8], vt + 4 * i * D,
+                               voffs[i & 1] +
+                                   (uint32_t)(((SMALL ? i & 3 : i) >> 1) * 8 * D * 2), 0u);
         };
         int t = t0;
         bool more = t < t1 && base_of(t) < lim;
-        Tile cur = {{-1, -1}};
+        Tile cur;
+        int ahead[P];                              // pages of the tile after the next copy
+        look_up(base_of(t), ahead);
         if (more) {
-            cur = pages_of(base_of(t));
-            copy(cur, base_of(t), 0, kt, true);
-            copy(cur, base_of(t), half, vt, false);
+            cur = aim(base_of(t), ahead);
+            copy_keys(cur);
+            copy_values(cur);
         }
+        look_up(base_of(t + 1), ahead);
         while (more) {
             const int base = base_of(t);
             const bool next = t + 1 < t1 && base_of(t + 1) < lim;
-            Tile nxt = {{-1, -1}};
-            if (next) nxt = pages_of(base_of(t + 1));
+            Tile nxt = cur;
+            if (next) nxt = aim(base_of(t + 1), ahead);
+            look_up(base_of(t + 2), ahead);
             dma::wait_vmcnt<8>();                       // K has landed, V may be under way
             f32x4 sc[RT][2];
 #pragma unroll
@@ -511,15 +558,15 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
                                                                            0, 0, 0);
                 }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // K's tile has been read
-            if (next) copy(nxt, base_of(t + 1), 0, kt, true);
+            if (next) copy_keys(nxt);
 
             // what the rows see of these 32 keys, where that is not everything
             const bool masked =
-                base + KT > all || base + KT > lim || cur.page[0] < 0 || cur.page[1] < 0;
+                base + KT > all || base + KT > lim || cur.page[0] < 0 || cur.page[P - 1] < 0;
             uint32_t sees[RT];
             if (masked) {
                 uint32_t there = (cur.page[0] < 0 ? 0u : 0xffffu) |
-                                 (cur.page[1] < 0 ? 0u : 0xffff0000u);
+                                 (cur.page[P - 1] < 0 ? 0u : 0xffff0000u);
                 if (lim - base < KT) there &= (1u << (lim - base)) - 1;
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
@@ -549,21 +596,24 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
                     odd |= any_odd(*reinterpret_cast<const u32x4*>(vt + (i * 64 + lane) * 8));
                 odd = __builtin_amdgcn_ballot_w64(odd) != 0;
             }
+            if (odd) {
+#pragma unroll
+                for (int r = 0; r < RT; ++r) add_odd(vt, pf[r], sees[r], o[r]);
+                for (int i = 0; i < 8; ++i)
+                    clear_odd(reinterpret_cast<u32x4*>(vt + (i * 64 + lane) * 8));
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
 #pragma unroll
             for (int dt = 0; dt < 8; ++dt) {
-                const bf16x8 vf = v_fragment(vt + vread[dt], odd);
+                const bf16x8 vf = v_fragment(vt + vread[dt]);
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
                     o[r][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r], o[r][dt], 0, 0, 0);
                     o[r][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl[r], o[r][dt], 0, 0, 0);
                 }
             }
-            if (odd) {
-#pragma unroll
-                for (int r = 0; r < RT; ++r) add_odd(vt, pf[r], sees[r], o[r]);
-            }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // V's tile has been read
-            if (next) copy(nxt, base_of(t + 1), half, vt, false);
+            if (next) copy_values(nxt);
             cur = nxt;
             more = next;
             ++t;
@@ -650,6 +700,8 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
 // time.
 constexpr int kWideRows = 128;
 constexpr int WT = 64;                 // keys of a tile
+// SMALL: pages of fewer than 64 tokens; a tile's quarters are looked up one by one.
+template <bool SMALL>
 __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
     constexpr int RB = 2;
     __shared__ __attribute__((aligned(16))) uint16_t tiles[2][2][WT * D];
@@ -684,9 +736,6 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
         const int r = 4 * g + (l16 >> 2), col = 16 * dt + 4 * (l16 & 3);
         vread[dt] = r * D + vpos(r, col >> 3) * 8 + (col & 7);
     }
-    const int shift = a.cache.page_shift;
-    const int64_t half = ((int64_t)a.cache.kv_heads << shift) * D;   // K to V of a page
-
     for (int64_t at = begin; at < end;) {
         if (seq_of(a, s).blocks == 0) {        // no new tokens: no steps either
             ++s;
@@ -696,24 +745,20 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
         const int t0 = (int)(at - u.u0), t1 = (int)(min(end, u.u1) - u.u0);
         const int lim = plan::block_keys(u.q, u.block, a.rows, causal);
         const int all = seen_by_all(a, u);
-        const const_ints table =
-            (const_ints)(uintptr_t)(a.batch.table + (int64_t)u.s * a.batch.ld_table);
-        const int64_t head0 = ((int64_t)u.head << shift) * D;
-        auto page_at = [&](int key) {          // uniform; -1: nothing to read
-            const int col = key >> shift;
-            const int e = key < lim && col < a.batch.max_pages ? table[col] : -1;
-            return e >= 0 && e < a.cache.n_pages ? e : -1;
+        const Keys src = keys_of(a, u, lim);
+        constexpr int P = SMALL ? 4 : 1, PK = WT / P;     // pages of a tile, keys of each
+        auto look_up = [&](int base, int (&page)[P]) {
+#pragma unroll
+            for (int h = 0; h < P; ++h) page[h] = src.page_at(base + PK * h);
         };
-        // keys [key, key + 16) of K and V into rows 16 r .. of a buffer
-        auto copy = [&](int page, int key, int buf, int r) {
-            const int left = __builtin_amdgcn_readfirstlane(
-                page < 0 ? 0 : min(max(lim - key, 0), 16));
-            const uint16_t* src = a.cache.pages + (int64_t)max(page, 0) * 2 * half + head0 +
-                                  (int64_t)(key & ((1 << shift) - 1)) * D;
+        // quarter r (16 keys) of the tile at `base` into a buffer
+        dma::u32x4 rk, rv;
+        auto copy = [&](int base, const int (&page)[P], int buf, int r) {
+            if (SMALL || r == 0) src.source<PK>(page[r * P / 4], base + PK * (r * P / 4), rk, rv);
             uint16_t* dst = tiles[buf][0] + (16 * r + 4 * wave) * D;
-            dma::lds_dma16(dma::rsrc_words(src, (int64_t)left * D * 2), dst, koff, 0u);
-            dma::lds_dma16(dma::rsrc_words(src + half, (int64_t)left * D * 2), dst + WT * D, voff,
-                           0u);
+            const uint32_t down = SMALL ? 0u : (uint32_t)(r * 16 * D * 2);
+            dma::lds_dma16(rk, dst, koff + down, 0u);
+            dma::lds_dma16(rv, dst + WT * D, voff + down, 0u);
         };
 
         int tok[RB], hq[RB];
@@ -741,28 +786,20 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
 
         const int first = t0 * plan::kStep;
         const int last = min(t1 * plan::kStep, lim);      // keys [first, last) of the piece
-        int page[4], there = 0;
+        int page[P], ahead[P];            // of the tile at hand, of the one to be copied
+        look_up(first, page);
         if (first < last) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                page[r] = page_at(first + 16 * r);
-                copy(page[r], first + 16 * r, 0, r);
-            }
+            for (int r = 0; r < 4; ++r) copy(first, page, 0, r);
         }
+        look_up(first + WT, ahead);
         dma::wait_vmcnt<0>();
         __syncthreads();
         int buf = 0;
         for (int base = first; base < last; base += WT, buf ^= 1) {
             const uint16_t* kt = tiles[buf][0];
             const uint16_t* vt = tiles[buf][1];
-            there = 0;                                     // 16-key groups with a page
-#pragma unroll
-            for (int r = 0; r < 4; ++r) there |= (page[r] >= 0 ? 1 : 0) << r;
             const bool next = base + WT < last;
-            if (next) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) page[r] = page_at(base + WT + 16 * r);
-            }
             f32x4 sc[RB][4];
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -780,16 +817,18 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
                                                                            0, 0, 0);
                 }
                 // the other buffer was last read before the last barrier
-                if (next) copy(page[ks], base + WT + 16 * ks, buf ^ 1, ks);
+                if (next) copy(base + WT, ahead, buf ^ 1, ks);
             }
-            const bool masked = base + WT > all || base + WT > lim || there != 15;
+            bool masked = base + WT > all || base + WT > lim;
+#pragma unroll
+            for (int h = 0; h < P; ++h) masked |= page[h] < 0;
             uint64_t sees[RB];
             bool odd = false;
             if (masked) {
                 uint64_t on = 0;
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    if (there >> r & 1) on |= 0xffffull << (16 * r);
+                    if (page[r * P / 4] >= 0) on |= 0xffffull << (16 * r);
                 if (lim - base < WT) on &= (1ull << (lim - base)) - 1;
 #pragma unroll
                 for (int r = 0; r < RB; ++r) {
@@ -809,6 +848,20 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
 #pragma unroll
             for (int r = 0; r < RB; ++r)
                 softmax_step(sc[r], a.scale_log2, mrun[r], lrun[r], o[r]);
+            if (odd) {                    // the same in all four waves: one tile
+                for (int sl = 0; sl < 2; ++sl)
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) {
+                        const bf16x8 pf = sl ? round_weights(sc[r][2], sc[r][3])
+                                             : round_weights(sc[r][0], sc[r][1]);
+                        add_odd(vt + 32 * sl * D, pf, (uint32_t)(sees[r] >> (32 * sl)), o[r]);
+                    }
+                __syncthreads();
+                for (int i = 0; i < 4; ++i)
+                    clear_odd(reinterpret_cast<u32x4*>(tiles[buf][1] +
+                                                       (i * NTHR + (int)threadIdx.x) * 8));
+                __syncthreads();
+            }
 #pragma unroll
             for (int sl = 0; sl < 2; ++sl) {
                 bf16x8 pf[RB];
@@ -816,18 +869,16 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
                 for (int r = 0; r < RB; ++r) pf[r] = round_weights(sc[r][2 * sl], sc[r][2 * sl + 1]);
 #pragma unroll
                 for (int dt = 0; dt < 8; ++dt) {
-                    const bf16x8 vf = v_fragment(vt + 32 * sl * D + vread[dt], odd);
+                    const bf16x8 vf = v_fragment(vt + 32 * sl * D + vread[dt]);
 #pragma unroll
                     for (int r = 0; r < RB; ++r)
                         o[r][dt] =
                             __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r], o[r][dt], 0, 0, 0);
                 }
-                if (odd) {
-#pragma unroll
-                    for (int r = 0; r < RB; ++r)
-                        add_odd(vt + 32 * sl * D, pf[r], (uint32_t)(sees[r] >> (32 * sl)), o[r]);
-                }
             }
+#pragma unroll
+            for (int h = 0; h < P; ++h) page[h] = ahead[h];
+            look_up(base + 2 * WT, ahead);
             dma::wait_vmcnt<0>();
             __syncthreads();
         }
@@ -872,80 +923,79 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
 }
 
 // The unit that begins in share blockIdx.x and goes on behind it: its pieces are
-// slot 1 of that share and slot 0 of the following ones, added in order.  Few pieces:
-// a wave per row.  Many (a long context): the workgroup takes its R rows one by one,
-// eight half waves every eighth piece each, four values per lane.
+// slot 1 of that share and slot 0 of the following ones, added in order with a
+// running maximum.  A half wave holds a row, four values per lane.  Few pieces: it
+// takes a row's pieces by itself (a unit of 128 rows is cut in two as a rule, and the
+// rows under way count).  Many (a long context, few rows): the workgroup takes its R
+// rows one by one, its half waves every H-th piece each.
 constexpr int kManyPieces = 16;
-template <int BM, int R>
-__global__ __launch_bounds__(NTHR) void join_kernel(Args a) {
-    constexpr int H = NTHR / 32;
-    __shared__ float tops[H], parts[H][D + 4];
+struct Joined {
+    float m, l;
+    f32x4 v;
+    __device__ __forceinline__ void clear() {
+        m = -INFINITY;
+        l = 0.f;
+        v = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    __device__ __forceinline__ void add(float m2, float l2, const f32x4& v2) {
+        const float top = fmaxf(m, m2), f = weight_of(m, top), f2 = weight_of(m2, top);
+        m = top;
+        l = l * f + l2 * f2;
+        v = v * f + v2 * f2;
+    }
+};
+template <int BM, int R, int NT>
+__global__ __launch_bounds__(NT) void join_kernel(Args a) {
+    constexpr int H = NT / 32;
+    __shared__ float parts[H][D + 4];
     const int64_t share = blockIdx.x;
     const Record rec = reinterpret_cast<const Record*>(a.ws)[share];
     if (rec.last < 0) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hw = tid / 32, l32 = tid & 31;
+    const int hw = threadIdx.x / 32, l32 = threadIdx.x & 31;
     const int n = min(rec.tokens * a.group, BM);      // rows of the unit
-    auto piece = [&](int i) { return slot_of<BM>(a.ws, share + i, i == 0); };
-    auto finish = [&](int row, int value, float x, float y, float top, float l) {
+    const int pieces = rec.last - (int)share + 1;
+    auto add_piece = [&](Joined& j, int i, int row) {
+        const float* p = slot_of<BM>(a.ws, share + i, i == 0);
+        j.add(p[BM * D + row], p[BM * D + BM + row],
+              *reinterpret_cast<const f32x4*>(p + row * D + 4 * l32));
+    };
+    auto finish = [&](const Joined& r, int row) {
         const int j = row / a.group, hq = rec.head * a.group + row - j * a.group;
         const int64_t token = rec.token + j;
-        const float inv = inverse_sum(l);
-        *reinterpret_cast<uint32_t*>(a.out + token * a.ldo + (int64_t)hq * D + value) =
-            pack_bf16x2(x * inv, y * inv);
-        if (a.lse && value == 0) a.lse[(int64_t)hq * a.tokens + token] = log_sum(top, l);
+        const float inv = inverse_sum(r.l);
+        *reinterpret_cast<u32x2*>(a.out + token * a.ldo + (int64_t)hq * D + 4 * l32) =
+            u32x2{pack_bf16x2(r.v[0] * inv, r.v[1] * inv), pack_bf16x2(r.v[2] * inv, r.v[3] * inv)};
+        if (a.lse && l32 == 0) a.lse[(int64_t)hq * a.tokens + token] = log_sum(r.m, r.l);
     };
-    const int pieces = rec.last - (int)share + 1;
     for (int row0 = blockIdx.y * R; row0 < n; row0 += gridDim.y * R) {
+        const int row1 = min(row0 + R, n);
+        Joined j;
         if (pieces <= kManyPieces) {
-            for (int row = row0 + wave; row < min(row0 + R, n); row += NWAVE) {
-                float top = lane < pieces ? piece(lane)[BM * D + row] : -INFINITY;
-#pragma unroll
-                for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-                float x = 0.f, y = 0.f, l = 0.f;
-#pragma unroll 4
-                for (int i = 0; i < pieces; ++i) {
-                    const float* p = piece(i);
-                    const float f = weight_of(p[BM * D + row], top);
-                    const f32x2 v = *reinterpret_cast<const f32x2*>(p + row * D + 2 * lane);
-                    l += f * p[BM * D + BM + row];
-                    x += f * v[0];
-                    y += f * v[1];
-                }
-                finish(row, 2 * lane, x, y, top, l);
+            for (int row = row0 + hw; row < row1; row += H) {
+                j.clear();
+#pragma unroll 2
+                for (int i = 0; i < pieces; ++i) add_piece(j, i, row);
+                finish(j, row);
             }
             continue;
         }
-        for (int row = row0; row < min(row0 + R, n); ++row) {
-            float top = -INFINITY;
-            for (int i = tid; i < pieces; i += NTHR) top = fmaxf(top, piece(i)[BM * D + row]);
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-            if (l32 == 0) tops[hw] = top;
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < H; ++i) top = fmaxf(top, tops[i]);
-            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-            float l = 0.f;
-#pragma unroll 8
-            for (int i = hw; i < pieces; i += H) {
-                const float* p = piece(i);
-                const float f = weight_of(p[BM * D + row], top);
-                l += f * p[BM * D + BM + row];
-                sum += f * *reinterpret_cast<const f32x4*>(p + row * D + 4 * l32);
+        for (int row = row0; row < row1; ++row) {
+            j.clear();
+#pragma unroll 4
+            for (int i = hw; i < pieces; i += H) add_piece(j, i, row);
+            *reinterpret_cast<f32x4*>(&parts[hw][4 * l32]) = j.v;
+            if (l32 == 0) {
+                parts[hw][D] = j.m;
+                parts[hw][D + 1] = j.l;
             }
-            *reinterpret_cast<f32x4*>(&parts[hw][4 * l32]) = sum;
-            if (l32 == 0) parts[hw][D] = l;
             __syncthreads();
-            if (tid < D / 2) {
-                float x = 0.f, y = 0.f;
-                l = 0.f;
+            if (hw == 0) {
+                j.clear();
 #pragma unroll
-                for (int i = 0; i < H; ++i) {
-                    x += parts[i][2 * tid];
-                    y += parts[i][2 * tid + 1];
-                    l += parts[i][D];
-                }
-                finish(row, 2 * tid, x, y, top, l);
+                for (int i = 0; i < H; ++i)
+                    j.add(parts[i][D], parts[i][D + 1],
+                          *reinterpret_cast<const f32x4*>(&parts[i][4 * l32]));
+                finish(j, row);
             }
             __syncthreads();
         }
@@ -960,14 +1010,14 @@ int unit_rows(int group, int max_new) {
 }
 
 // rows: what a unit is expected to hold; the joining workgroups walk all it has
-template <int BM, int R>
+template <int BM, int R, int NT>
 hipError_t launch(void (*kernel)(Args), const Args& a, unsigned grid, int64_t rows,
                   hipStream_t s) {
     kernel<<<grid, NTHR, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || grid <= 1) return e;
     const unsigned per = (unsigned)((std::min<int64_t>(rows, BM) + R - 1) / R);
-    join_kernel<BM, R><<<dim3(grid, per), NTHR, 0, s>>>(a);
+    join_kernel<BM, R, NT><<<dim3(grid, per), NT, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -998,9 +1048,16 @@ hipError_t launch_cache_attention(const CacheAttentionProblem& p, hipStream_t s)
     const int64_t most = std::min<int64_t>(units * p.cache.kv_heads, 1 << 20) * steps;
     const unsigned grid = (unsigned)std::min<int64_t>(kGroups, most);
     const int64_t rows = (int64_t)p.group * p.max_new;
-    if (bm == 16) return launch<16, 1>(attention_cache_kernel<1>, a, grid, rows, s);
-    if (bm == 32) return launch<32, 1>(attention_cache_kernel<2>, a, grid, rows, s);
-    return launch<kWideRows, 4>(attention_cache_wide_kernel, a, grid, rows, s);
+    const int shift = p.cache.page_shift;
+    if (bm == 16)
+        return launch<16, 1, 512>(shift < 5 ? attention_cache_kernel<1, true>
+                                            : attention_cache_kernel<1, false>, a, grid, rows, s);
+    if (bm == 32)
+        return launch<32, 1, 512>(shift < 5 ? attention_cache_kernel<2, true>
+                                            : attention_cache_kernel<2, false>, a, grid, rows, s);
+    return launch<kWideRows, 16, 256>(shift < 6 ? attention_cache_wide_kernel<true>
+                                                : attention_cache_wide_kernel<false>, a, grid, rows,
+                                      s);
 }
 
 }  // namespace atp

@@ -338,26 +338,29 @@ __global__ __launch_bounds__(kThreads) void norm_rope_bwd_kernel(Args A) {
     A.part[(int64_t)blockIdx.x * 2 * kHead + threadIdx.x] = sum;
 }
 
-// Column sums of n rows of 256 partials: 16 columns per workgroup, 16 lanes'
-// worth of rows each, joined in order.
-__global__ __launch_bounds__(kThreads) void weight_sum_kernel(const float* part, int n, float* dqw,
-                                                              float* dkw) {
-    __shared__ float red[16][17];
+// Column sums of n rows of 256 partials: 16 columns per workgroup, 64 runs of rows
+// (every 64th), joined in order.  16 runs and one load under way took 20 us for
+// 1024 rows.
+constexpr int kSumThreads = 1024;
+__global__ __launch_bounds__(kSumThreads) void weight_sum_kernel(const float* part, int n,
+                                                                 float* dqw, float* dkw) {
+    constexpr int G = kSumThreads / 16;
+    __shared__ float red[G][17];
     const int c = threadIdx.x & 15, g = threadIdx.x / 16;
     const int col = blockIdx.x * 16 + c;
     float sum = 0.f;
-    for (int i = g; i < n; i += 16) sum += part[(int64_t)i * 2 * kHead + col];
+#pragma unroll 8
+    for (int i = g; i < n; i += G) sum += part[(int64_t)i * 2 * kHead + col];
     red[g][c] = sum;
     __syncthreads();
-    if (g == 0) {
-        sum = 0.f;
+    if (g != 0) return;
+    sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum += red[i][c];
-        if (col < kHead) {
-            if (dqw) dqw[col] = sum;
-        } else if (dkw) {
-            dkw[col - kHead] = sum;
-        }
+    for (int i = 0; i < G; ++i) sum += red[i][c];
+    if (col < kHead) {
+        if (dqw) dqw[col] = sum;
+    } else if (dkw) {
+        dkw[col - kHead] = sum;
     }
 }
 
@@ -419,7 +422,7 @@ hipError_t launch_norm_rope(const NormRopeProblem& p, hipStream_t s) {
 
 hipError_t launch_norm_rope_bwd(const NormRopeBwdProblem& p, hipStream_t s) {
     if (p.tokens == 0) {      // sums of nothing
-        weight_sum_kernel<<<16, kThreads, 0, s>>>(nullptr, 0, p.dqw, p.dkw);
+        weight_sum_kernel<<<16, kSumThreads, 0, s>>>(nullptr, 0, p.dqw, p.dkw);
         return hipGetLastError();
     }
     const int heads = p.kv_heads * (p.group + 2);
@@ -435,7 +438,7 @@ hipError_t launch_norm_rope_bwd(const NormRopeBwdProblem& p, hipStream_t s) {
     k<<<dim3((unsigned)grid), kThreads, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.part) return e;
-    weight_sum_kernel<<<16, kThreads, 0, s>>>(p.ws, (int)grid, p.dqw, p.dkw);
+    weight_sum_kernel<<<16, kSumThreads, 0, s>>>(p.ws, (int)grid, p.dqw, p.dkw);
     return hipGetLastError();
 }
 
