@@ -353,8 +353,14 @@ def _vec(t: Optional[torch.Tensor], n: int, dtype, name: str):
     return t.data_ptr()
 
 
-def _stream(s) -> Optional[int]:
+# the raw handle of a device's current stream, without a Stream object around it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream(s, dev: Optional[int] = None) -> Optional[int]:
     if s is None:
+        if dev is not None and _raw_stream is not None:
+            return _raw_stream(dev)
         return torch.cuda.current_stream().cuda_stream
     if isinstance(s, int):
         return s
@@ -757,37 +763,67 @@ def atp_attention_bwd_noalloc(m: atp_mesh, block_mode: int, batch: int, seq: int
         ldo, _ptr(lse, "lse"), dop, lddo, dqp, lddq, _stream(stream)))
 
 
-def _ints(t: Optional[torch.Tensor], n: int, name: str):
-    """Pointer of a device list of at least n int32 values (None stays NULL)."""
-    return _vec(t, n, torch.int32, name)
+# The calls below are made token by token, so their arguments are looked at once and
+# quickly; what does not fit goes to _mat / _vec, which say what is wrong.
+def _rows(t, rows: int, cols: int, name: str, dev: int):
+    """(pointer, ld) of a bf16 matrix on device dev."""
+    if t is not None and t.dtype is torch.bfloat16 and t.get_device() == dev and t.dim() == 2:
+        r, c = t.shape
+        s0, s1 = t.stride()
+        if r >= rows and c >= cols and (s1 == 1 or c <= 1):
+            return t.data_ptr(), (s0 if r > 1 else max(c, cols))
+    return _mat(t, rows, cols, torch.bfloat16, name)
 
 
-class qk_norm_rope:
+def _list(t, n: int, name: str, dev: int, dtype=torch.int32):
+    """Pointer of a contiguous vector of at least n values (None stays NULL)."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.get_device() == dev and t.numel() >= n and t.is_contiguous():
+        return t.data_ptr()
+    return _vec(t, n, dtype, name)
+
+
+def _bytes(workspace, dev: int):
+    if workspace is not None and workspace.get_device() == dev:
+        return workspace.data_ptr(), workspace.nbytes
+    return _workspace(workspace)
+
+
+class _Held:
+    """A C struct and the tensors it points into."""
+
+    def _hold(self, struct, **tensors):
+        self.c = struct
+        self._tensors = [(t, name) for name, t in tensors.items() if t is not None]
+        self._ref = ctypes.byref(struct)
+
+    def ref(self, dev: int):
+        for t, name in self._tensors:
+            if t.get_device() != dev:
+                _on_device(t, name)
+        return self._ref
+
+
+class qk_norm_rope(_Held):
     """Parameters of the query/key norms with the position rotation
     (atp_qk_norm_rope in include/atp.h); keeps its tensors alive.  q_weight,
     k_weight: bf16 [128]; inv_freq: float32 [rotary_dims / 2]."""
 
     def __init__(self, q_weight=None, k_weight=None, eps: float = 1e-6, inv_freq=None,
                  rotary_dims: int = 0, interleaved: bool = False, norm: bool = True):
-        self.q_weight, self.k_weight, self.inv_freq = q_weight, k_weight, inv_freq
         rotary_dims = int(rotary_dims)
         if rotary_dims > 0 and inv_freq is None:
             raise ValueError("inv_freq: a rotation needs its frequencies")
-        self.c = atp_qk_norm_rope(
+        self._hold(atp_qk_norm_rope(
             _vec(q_weight, HEAD_DIM, torch.bfloat16, "q_weight"),
             _vec(k_weight, HEAD_DIM, torch.bfloat16, "k_weight"),
             _vec(inv_freq, max(0, rotary_dims) // 2, torch.float32, "inv_freq"), float(eps),
-            int(norm), rotary_dims, int(interleaved))
-
-    def ref(self):
-        for t, name in ((self.q_weight, "q_weight"), (self.k_weight, "k_weight"),
-                        (self.inv_freq, "inv_freq")):
-            if t is not None:
-                _on_device(t, name)
-        return ctypes.byref(self.c)
+            int(norm), rotary_dims, int(interleaved)),
+            q_weight=q_weight, k_weight=k_weight, inv_freq=inv_freq)
 
 
-class kv_cache:
+class kv_cache(_Held):
     """One layer's cache: pages, a contiguous bf16 tensor [n_pages, 2, kv_heads,
     page_size, 128] (keys, then values)."""
 
@@ -798,16 +834,12 @@ class kv_cache:
                 not pages.is_contiguous()):
             raise ValueError("pages: needs a contiguous [n_pages, 2, kv_heads, page_size, "
                              f"{HEAD_DIM}] tensor, got {tuple(pages.shape)}")
-        self.pages = pages
         self.n_pages, _, self.kv_heads, self.page_size, _ = pages.shape
-        self.c = atp_kv_cache(_ptr(pages, "pages"), self.n_pages, self.kv_heads, self.page_size)
-
-    def ref(self):
-        _on_device(self.pages, "pages")
-        return ctypes.byref(self.c)
+        self._hold(atp_kv_cache(_ptr(pages, "pages"), self.n_pages, self.kv_heads,
+                                self.page_size), pages=pages)
 
 
-class kv_batch:
+class kv_batch(_Held):
     """A batch of sequences over a cache: table int32 [n_seqs, max_pages], ctx
     int32 [n_seqs], cu_new int32 [n_seqs + 1] (either may be None for the calls
     that do not read it).  The tensors are read when a call's kernels run."""
@@ -817,30 +849,25 @@ class kv_batch:
             raise TypeError(f"table: expected torch.int32, got {table.dtype}")
         if table.dim() != 2 or (table.size(1) > 1 and table.stride(1) != 1):
             raise ValueError("table: needs a 2-D row-major tensor")
-        self.table, self.ctx, self.cu_new = table, ctx, cu_new
         self.n_seqs, self.max_pages = table.shape
         ld = table.stride(0) if self.n_seqs > 1 else self.max_pages
-        self.c = atp_kv_batch(_ptr(table, "table"), ld, self.max_pages, self.n_seqs,
-                              _ints(ctx, self.n_seqs, "ctx"),
-                              _ints(cu_new, self.n_seqs + 1, "cu_new"))
-
-    def ref(self):
-        for t, name in ((self.table, "table"), (self.ctx, "ctx"), (self.cu_new, "cu_new")):
-            if t is not None:
-                _on_device(t, name)
-        return ctypes.byref(self.c)
+        self._hold(atp_kv_batch(_ptr(table, "table"), ld, self.max_pages, self.n_seqs,
+                                _vec(ctx, self.n_seqs, torch.int32, "ctx"),
+                                _vec(cu_new, self.n_seqs + 1, torch.int32, "cu_new")),
+                   table=table, ctx=ctx, cu_new=cu_new)
 
 
 def atp_qk_norm_rope_fwd(batch: int, seq: int, kv_heads: int, group: int, params: qk_norm_rope,
                          qkv, out, positions=None, stream=None):
     """qkv, out: bf16 [batch*seq, kv_heads*(group+2)*128] (out may be qkv);
     positions: int32 [batch*seq], or None for t % seq."""
+    dev = torch.cuda.current_device()
     T, cols = batch * seq, kv_heads * (group + 2) * HEAD_DIM
-    xp, ldx = _mat(qkv, T, cols, torch.bfloat16, "qkv")
-    op, ldo = _mat(out, T, cols, torch.bfloat16, "out")
+    xp, ldx = _rows(qkv, T, cols, "qkv", dev)
+    op, ldo = _rows(out, T, cols, "out", dev)
     _check(load_library().atp_qk_norm_rope_fwd(
-        int(batch), int(seq), int(kv_heads), int(group), params.ref(),
-        _ints(positions, T, "positions"), xp, ldx, op, ldo, _stream(stream)))
+        int(batch), int(seq), int(kv_heads), int(group), params.ref(dev),
+        _list(positions, T, "positions", dev), xp, ldx, op, ldo, _stream(stream, dev)))
 
 
 def atp_qk_norm_rope_workspace_bytes(tokens: int) -> int:
@@ -853,83 +880,95 @@ def atp_qk_norm_rope_bwd(batch: int, seq: int, kv_heads: int, group: int, params
     """Gradient of atp_qk_norm_rope_fwd: d_qkv (may be d_out) and, where
     given, the weights' gradients (float32 [128]; they need a workspace of
     atp_qk_norm_rope_workspace_bytes(batch*seq) bytes)."""
+    dev = torch.cuda.current_device()
     T, cols = batch * seq, kv_heads * (group + 2) * HEAD_DIM
-    xp, ldx = _mat(qkv, T, cols, torch.bfloat16, "qkv")
-    gp, ldg = _mat(d_out, T, cols, torch.bfloat16, "d_out")
-    dp_, ldd = _mat(d_qkv, T, cols, torch.bfloat16, "d_qkv")
-    wsp, wsb = _workspace(workspace)
+    xp, ldx = _rows(qkv, T, cols, "qkv", dev)
+    gp, ldg = _rows(d_out, T, cols, "d_out", dev)
+    dp_, ldd = _rows(d_qkv, T, cols, "d_qkv", dev)
+    wsp, wsb = _bytes(workspace, dev)
     _check(load_library().atp_qk_norm_rope_bwd(
-        int(batch), int(seq), int(kv_heads), int(group), params.ref(),
-        _ints(positions, T, "positions"), xp, ldx, gp, ldg, dp_, ldd,
-        _vec(dq_weight, HEAD_DIM, torch.float32, "dq_weight"),
-        _vec(dk_weight, HEAD_DIM, torch.float32, "dk_weight"), wsp, wsb, _stream(stream)))
+        int(batch), int(seq), int(kv_heads), int(group), params.ref(dev),
+        _list(positions, T, "positions", dev), xp, ldx, gp, ldg, dp_, ldd,
+        _list(dq_weight, HEAD_DIM, "dq_weight", dev, torch.float32),
+        _list(dk_weight, HEAD_DIM, "dk_weight", dev, torch.float32), wsp, wsb,
+        _stream(stream, dev)))
 
 
 def atp_qk_norm_rope_cache(cache: kv_cache, batch: kv_batch, tokens: int, group: int,
                            params: qk_norm_rope, qkv, q, positions=None, stream=None):
     """The step's rows qkv [tokens, kv_heads*(group+2)*128]: queries into q
     [tokens, kv_heads*group*128], keys and values into the cache."""
-    xp, ldx = _mat(qkv, tokens, cache.kv_heads * (group + 2) * HEAD_DIM, torch.bfloat16, "qkv")
-    qp, ldq = _mat(q, tokens, cache.kv_heads * group * HEAD_DIM, torch.bfloat16, "q")
+    dev = torch.cuda.current_device()
+    xp, ldx = _rows(qkv, tokens, cache.kv_heads * (group + 2) * HEAD_DIM, "qkv", dev)
+    qp, ldq = _rows(q, tokens, cache.kv_heads * group * HEAD_DIM, "q", dev)
     _check(load_library().atp_qk_norm_rope_cache(
-        cache.ref(), batch.ref(), int(tokens), int(group), params.ref(),
-        _ints(positions, tokens, "positions"), xp, ldx, qp, ldq, _stream(stream)))
+        cache.ref(dev), batch.ref(dev), int(tokens), int(group), params.ref(dev),
+        _list(positions, tokens, "positions", dev), xp, ldx, qp, ldq, _stream(stream, dev)))
 
 
 def atp_cache_workspace_bytes(n_pages: int, n_seqs: int) -> int:
     return load_library().atp_cache_workspace_bytes(int(n_pages), int(n_seqs))
 
 
-def _refs(refs):
+def _refs(refs, dev: int):
     if refs is None:
         raise ValueError("refs: needs the pages' reference counts")
-    return refs.numel(), _ints(refs, refs.numel(), "refs")
+    return refs.numel(), _list(refs, refs.numel(), "refs", dev)
 
 
 def atp_cache_reserve(page_size: int, refs, batch: kv_batch, missing, copy_src, copy_dst,
                       copy_rows, workspace, stream=None):
     """Pages for every sequence's new tokens; refs: int32 [n_pages]; missing,
     copy_src, copy_dst, copy_rows: int32 [n_seqs], written."""
-    n, rp = _refs(refs)
-    wsp, wsb = _workspace(workspace)
+    dev = torch.cuda.current_device()
+    n, rp = _refs(refs, dev)
+    wsp, wsb = _bytes(workspace, dev)
     _check(load_library().atp_cache_reserve(
-        n, int(page_size), rp, batch.ref(), _ints(missing, batch.n_seqs, "missing"),
-        _ints(copy_src, batch.n_seqs, "copy_src"), _ints(copy_dst, batch.n_seqs, "copy_dst"),
-        _ints(copy_rows, batch.n_seqs, "copy_rows"), wsp, wsb, _stream(stream)))
+        n, int(page_size), rp, batch.ref(dev), _list(missing, batch.n_seqs, "missing", dev),
+        _list(copy_src, batch.n_seqs, "copy_src", dev),
+        _list(copy_dst, batch.n_seqs, "copy_dst", dev),
+        _list(copy_rows, batch.n_seqs, "copy_rows", dev), wsp, wsb, _stream(stream, dev)))
 
 
 def atp_cache_fork(page_size: int, refs, batch: kv_batch, parents, children, done, stream=None):
     """children[f] takes over parents[f]'s pages (int32 lists of one length);
     done: int32, 0 or 1 (refused) per fork."""
-    n, rp = _refs(refs)
+    dev = torch.cuda.current_device()
+    n, rp = _refs(refs, dev)
     forks = parents.numel()
     _check(load_library().atp_cache_fork(
-        n, int(page_size), rp, batch.ref(), forks, _ints(parents, forks, "parents"),
-        _ints(children, forks, "children"), _ints(done, forks, "done"), _stream(stream)))
+        n, int(page_size), rp, batch.ref(dev), forks, _list(parents, forks, "parents", dev),
+        _list(children, forks, "children", dev), _list(done, forks, "done", dev),
+        _stream(stream, dev)))
 
 
 def atp_cache_release(page_size: int, refs, batch: kv_batch, keep, stream=None):
     """Gives back the pages behind the first keep[s] >= 0 tokens of sequence s."""
-    n, rp = _refs(refs)
-    _check(load_library().atp_cache_release(n, int(page_size), rp, batch.ref(),
-                                            _ints(keep, batch.n_seqs, "keep"), _stream(stream)))
+    dev = torch.cuda.current_device()
+    n, rp = _refs(refs, dev)
+    _check(load_library().atp_cache_release(
+        n, int(page_size), rp, batch.ref(dev), _list(keep, batch.n_seqs, "keep", dev),
+        _stream(stream, dev)))
 
 
 def atp_cache_copy_pages(cache: kv_cache, src, dst, rows=None, stream=None):
     """The first rows[i] tokens (all for None) of page src[i] to page dst[i]."""
+    dev = torch.cuda.current_device()
     n = src.numel()
     _check(load_library().atp_cache_copy_pages(
-        cache.ref(), n, _ints(src, n, "src"), _ints(dst, n, "dst"), _ints(rows, n, "rows"),
-        _stream(stream)))
+        cache.ref(dev), n, _list(src, n, "src", dev), _list(dst, n, "dst", dev),
+        _list(rows, n, "rows", dev), _stream(stream, dev)))
 
 
 def atp_cache_compact(cache: kv_cache, batch: kv_batch, cu_keep, keep, moved=None, stream=None):
     """Moves tokens ctx[s] + keep[cu_keep[s] + i] to places ctx[s] + i; moved:
     int32 [n_seqs], rows moved or -1 (refused)."""
+    dev = torch.cuda.current_device()
     n = keep.numel()
     _check(load_library().atp_cache_compact(
-        cache.ref(), batch.ref(), _ints(cu_keep, batch.n_seqs + 1, "cu_keep"),
-        _ints(keep, n, "keep"), n, _ints(moved, batch.n_seqs, "moved"), _stream(stream)))
+        cache.ref(dev), batch.ref(dev), _list(cu_keep, batch.n_seqs + 1, "cu_keep", dev),
+        _list(keep, n, "keep", dev), n, _list(moved, batch.n_seqs, "moved", dev),
+        _stream(stream, dev)))
 
 
 def atp_attention_cache_workspace_bytes(kv_heads: int, group: int, max_new: int) -> int:
@@ -944,9 +983,10 @@ def atp_attention_cache_fwd(cache: kv_cache, batch: kv_batch, tokens: int, group
     [tokens, kv_heads*group*128]); lse: float32 [kv_heads*group, tokens];
     tree_mask: int64 or uint64 [tokens, words], contiguous; workspace:
     atp_attention_cache_workspace_bytes(kv_heads, group, max_new) bytes."""
+    dev = torch.cuda.current_device()
     cols = cache.kv_heads * group * HEAD_DIM
-    qp, ldq = _mat(q, tokens, cols, torch.bfloat16, "q")
-    op, ldo = _mat(out, tokens, cols, torch.bfloat16, "out")
+    qp, ldq = _rows(q, tokens, cols, "q", dev)
+    op, ldo = _rows(out, tokens, cols, "out", dev)
     words, mp = 0, None
     if tree_mask is not None:
         if tree_mask.dtype not in (torch.int64, torch.uint64):
@@ -954,11 +994,11 @@ def atp_attention_cache_fwd(cache: kv_cache, batch: kv_batch, tokens: int, group
         if tree_mask.dim() != 2 or tree_mask.size(0) < tokens or not tree_mask.is_contiguous():
             raise ValueError(f"tree_mask: needs a contiguous [{tokens}, words] tensor")
         words, mp = tree_mask.size(1), _ptr(tree_mask, "tree_mask")
-    wsp, wsb = _workspace(workspace)
+    wsp, wsb = _bytes(workspace, dev)
     _check(load_library().atp_attention_cache_fwd(
-        cache.ref(), batch.ref(), int(tokens), int(group), int(max_new), qp, ldq, mp, words, op,
-        ldo, _vec(lse, cache.kv_heads * group * tokens, torch.float32, "lse"), wsp, wsb,
-        _stream(stream)))
+        cache.ref(dev), batch.ref(dev), int(tokens), int(group), int(max_new), qp, ldq, mp, words,
+        op, ldo, _list(lse, cache.kv_heads * group * tokens, "lse", dev, torch.float32), wsp, wsb,
+        _stream(stream, dev)))
 
 
 def _attn_weights(G, w, b, layout: int):
