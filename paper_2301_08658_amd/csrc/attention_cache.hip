@@ -28,6 +28,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "cache_kernels.h"
 #include "cache_plan.h"
@@ -125,62 +126,110 @@ __device__ __forceinline__ int64_t seq_steps(const Args& a, const plan::Seq& q) 
     return plan::steps_before(q, q.blocks, a.rows, a.mask == nullptr) * a.cache.kv_heads;
 }
 
-// Steps of the whole batch and, for thread t, of the sequences before its run of
-// them (runs of `run` consecutive sequences).
-struct Line {
-    int64_t total, before, mine;
-    int run;
+// A workgroup's share of the line: steps [begin, end), the sequence of step `begin`
+// and the step that sequence starts at.  None: begin == end.
+struct Share {
+    int64_t index, per, begin, end, start;
+    int s;
+    plan::Seq q;
 };
-__device__ __forceinline__ Line lay_out(const Args& a, int64_t* sums) {
-    Line ln;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = a.batch.n_seqs;
-    ln.run = (n + NTHR - 1) / NTHR;
-    ln.mine = 0;
-    for (int i = 0; i < ln.run; ++i) {
-        const int s = tid * ln.run + i;
-        if (s < n)
-            ln.mine += seq_steps(a, plan::make_seq(a.batch.ctx[s], a.batch.cu[s], a.batch.cu[s + 1],
-                                                   a.tokens, a.cap, a.rows));
+// Shares are numbered so that consecutive ones run on one XCD (workgroups go
+// round the eight dies): the row blocks of a head share its keys in that L2.
+__device__ __forceinline__ bool take_share(int64_t total, Share& sh) {
+    sh.per = uniform(plan::share(total, kGroups, kLeastSteps));
+    const int64_t used = uniform(quotient(total + sh.per - 1, sh.per));
+    const int bid = blockIdx.x;
+    if (bid >= used) {
+        sh.index = bid;
+        sh.begin = sh.end = 0;
+        return false;
     }
-    int64_t inc = ln.mine;
+    const int64_t base = used / kXcds, rem = used % kXcds;
+    const int x = bid % kXcds;
+    sh.index = x * base + (x < rem ? x : rem) + bid / kXcds;
+    sh.begin = sh.index * sh.per;
+    sh.end = min(sh.begin + sh.per, total);
+    return true;
+}
+
+// Inclusive prefix sum over the wave (rows of 16 lanes, then across them).
+__device__ __forceinline__ uint32_t wave_prefix(uint32_t v) {
+    auto add = [&](auto ctrl, auto rows) {
+        v += __builtin_amdgcn_update_dpp(0u, v, decltype(ctrl)::value, decltype(rows)::value, 0xf,
+                                         false);
+    };
+    add(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});   // row_shr:1
+    add(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+    add(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+    add(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+    add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // row_bcast:15
+    add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // row_bcast:31
+    return v;
+}
+
+__device__ __forceinline__ plan::Seq load_seq(const Args& a, int s) {
+    return plan::make_seq(a.batch.ctx[s], a.batch.cu[s], a.batch.cu[s + 1], a.tokens, a.cap, a.rows);
+}
+
+// Every workgroup lays out the batch for itself: reading a few lengths costs less
+// than a launch that would do it once.  Up to 64 sequences: one per lane, each wave by
+// itself, nothing but registers (8.7 -> 7.0 us for one sequence's token).  More: runs of
+// consecutive sequences per thread, added up through LDS.
+__device__ __forceinline__ Share find_share(const Args& a, int64_t* lds) {
+    Share sh;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = a.batch.n_seqs;
+    if (n <= 64) {
+        plan::Seq q = {0, 0, 0, 0, 0};
+        if (lane < n) q = load_seq(a, lane);
+        const int64_t mine = lane < n ? seq_steps(a, q) : 0;
+        if (__builtin_amdgcn_ballot_w64(mine >> 25 != 0) == 0) {
+            const uint32_t upto = wave_prefix((uint32_t)mine);
+            const uint32_t total = __builtin_amdgcn_readlane(upto, 63);
+            if (!take_share(total, sh)) return sh;
+            // no lane behind the last sequence counts: its prefix is the total
+            sh.s = __popcll(__builtin_amdgcn_ballot_w64(upto <= (uint32_t)sh.begin));
+            sh.start = (uint32_t)__builtin_amdgcn_readlane(upto - (uint32_t)mine, sh.s);
+            sh.q.first = __builtin_amdgcn_readlane(q.first, sh.s);
+            sh.q.fresh = __builtin_amdgcn_readlane(q.fresh, sh.s);
+            sh.q.ctx = __builtin_amdgcn_readlane(q.ctx, sh.s);
+            sh.q.keys = __builtin_amdgcn_readlane(q.keys, sh.s);
+            sh.q.blocks = __builtin_amdgcn_readlane(q.blocks, sh.s);
+            return sh;
+        }
+    }
+    const int run = (n + NTHR - 1) / NTHR;
+    int64_t mine = 0;
+    for (int i = tid * run; i < min((tid + 1) * run, n); ++i) mine += seq_steps(a, load_seq(a, i));
+    int64_t inc = mine;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
         const int64_t up = __shfl_up(inc, d);
         if (lane >= d) inc += up;
     }
-    if (lane == 63) sums[wave] = inc;
+    if (lane == 63) lds[wave] = inc;
     __syncthreads();
-    ln.total = 0;
-    ln.before = inc - ln.mine;
+    int64_t total = 0, before = inc - mine;
 #pragma unroll
     for (int w = 0; w < NWAVE; ++w) {
-        if (w < wave) ln.before += sums[w];
-        ln.total += sums[w];
+        if (w < wave) before += lds[w];
+        total += lds[w];
     }
-    ln.total = uniform(ln.total);
-    return ln;
-}
-// The sequence of step `at` (0 <= at < total) and the step it starts at, for the
-// whole workgroup.
-__device__ __forceinline__ void find_seq(const Args& a, const Line& ln, int64_t at, int64_t* found,
-                                         int* s, int64_t* start) {
-    if (ln.mine > 0 && ln.before <= at && at < ln.before + ln.mine) {
-        int64_t p = ln.before;
-        int i = threadIdx.x * ln.run;
+    if (!take_share(uniform(total), sh)) return sh;
+    if (mine > 0 && before <= sh.begin && sh.begin < before + mine) {
+        int i = tid * run;
         for (;; ++i) {
-            const int64_t n = seq_steps(a, plan::make_seq(a.batch.ctx[i], a.batch.cu[i],
-                                                          a.batch.cu[i + 1], a.tokens, a.cap,
-                                                          a.rows));
-            if (at < p + n || i + 1 >= a.batch.n_seqs) break;
-            p += n;
+            const int64_t m = seq_steps(a, load_seq(a, i));
+            if (sh.begin < before + m || i + 1 >= n) break;
+            before += m;
         }
-        found[0] = i;
-        found[1] = p;
+        lds[NWAVE] = i;
+        lds[NWAVE + 1] = before;
     }
     __syncthreads();
-    *s = (int)uniform(found[0]);
-    *start = uniform(found[1]);
-    __syncthreads();
+    sh.s = (int)uniform(lds[NWAVE]);
+    sh.start = uniform(lds[NWAVE + 1]);
+    sh.q = seq_of(a, sh.s);
+    return sh;
 }
 
 // One row block of one head of one sequence, and its steps [u0, u1) of the line.
@@ -189,26 +238,30 @@ struct Unit {
     int s, head, block;
     int64_t u0, u1;
 };
-__device__ __forceinline__ Unit unit_at(const Args& a, int s, int64_t start, int64_t at) {
+__device__ __forceinline__ Unit unit_at(const Args& a, const plan::Seq& q, int s, int64_t start,
+                                        int64_t at) {
     Unit u;
     const bool causal = a.mask == nullptr;
     u.s = s;
-    u.q = seq_of(a, s);
-    const int64_t head = plan::steps_before(u.q, u.q.blocks, a.rows, causal);
+    u.q = q;
+    const int64_t head = plan::steps_before(q, q.blocks, a.rows, causal);
     u.head = __builtin_amdgcn_readfirstlane((int)quotient(at - start, head));
     const int64_t h0 = start + u.head * head;
-    u.block = __builtin_amdgcn_readfirstlane(plan::block_of(u.q, at - h0, a.rows, causal));
-    u.u0 = uniform(h0 + plan::steps_before(u.q, u.block, a.rows, causal));
-    u.u1 = uniform(h0 + plan::steps_before(u.q, u.block + 1, a.rows, causal));
+    u.block = __builtin_amdgcn_readfirstlane(plan::block_of(q, at - h0, a.rows, causal));
+    u.u0 = uniform(h0 + plan::steps_before(q, u.block, a.rows, causal));
+    u.u1 = uniform(h0 + plan::steps_before(q, u.block + 1, a.rows, causal));
     return u;
 }
 
-// Shares are numbered so that consecutive ones run on one XCD (workgroups go
-// round the eight dies): the row blocks of a head share its keys in that L2.
-__device__ __forceinline__ int64_t share_index(int bid, int64_t used) {
-    const int64_t base = used / kXcds, rem = used % kXcds;
-    const int x = bid % kXcds;
-    return x * base + (x < rem ? x : rem) + bid / kXcds;
+// Moves a share on to the sequence of step `at` (sequences without new tokens have no
+// steps).
+__device__ __forceinline__ void next_seq(const Args& a, Share& sh, int64_t at) {
+    const int64_t steps = uniform(seq_steps(a, sh.q));
+    if (at < sh.start + steps) return;
+    sh.start += steps;
+    if (at >= sh.end) return;
+    do sh.q = seq_of(a, ++sh.s);
+    while (sh.q.blocks == 0);
 }
 
 // The workspace: a record of every share, then two slots per share.  The record
@@ -417,23 +470,12 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
     constexpr int kRed = D + 4;      // padded row of the merge
     __shared__ __attribute__((aligned(16))) uint16_t tiles[NWAVE][2][KT * D];
     __shared__ float wm[NWAVE][BM], wl[NWAVE][BM];
-    __shared__ int64_t sums[NWAVE], found[2];
+    __shared__ int64_t lds[NWAVE + 2];
     const int lane = threadIdx.x & 63, g = lane >> 4, l16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool causal = a.mask == nullptr;
 
-    const Line ln = lay_out(a, sums);
-    const int64_t per = uniform(plan::share(ln.total, kGroups, kLeastSteps));
-    const int64_t used = uniform(quotient(ln.total + per - 1, per));
-    if (blockIdx.x >= used) {
-        leave_record(a, blockIdx.x, Record{-1, 0, 0, 0});
-        return;
-    }
-    const int64_t share = share_index(blockIdx.x, used);
-    const int64_t begin = share * per, end = min(begin + per, ln.total);
-    int s;
-    int64_t start;
-    find_seq(a, ln, begin, found, &s, &start);
+    Share sh = find_share(a, lds);
     Record record = {-1, 0, 0, 0};
 
     uint16_t* kt = tiles[wave][0];
@@ -454,13 +496,9 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
         const int r = 4 * g + (l16 >> 2), col = 16 * dt + 4 * (l16 & 3);
         vread[dt] = r * D + vpos(r, col >> 3) * 8 + (col & 7);
     }
-    for (int64_t at = begin; at < end;) {
-        if (seq_of(a, s).blocks == 0) {        // no new tokens: no steps either
-            ++s;
-            continue;
-        }
-        const Unit u = unit_at(a, s, start, at);
-        const int t0 = (int)(at - u.u0), t1 = (int)(min(end, u.u1) - u.u0);
+    for (int64_t at = sh.begin; at < sh.end;) {
+        const Unit u = unit_at(a, sh.q, sh.s, sh.start, at);
+        const int t0 = (int)(at - u.u0), t1 = (int)(min(sh.end, u.u1) - u.u0);
         const int lim = plan::block_keys(u.q, u.block, a.rows, causal);
         const int all = seen_by_all(a, u);
         const Keys src = keys_of(a, u, lim);
@@ -628,9 +666,9 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
                 wl[wave][16 * r + l16] = lrun[r];
             }
         }
-        const bool whole = t0 == 0 && u.u1 <= end;
-        if (t0 == 0 && !whole) record = record_of(a, u, per);
-        float* slot = slot_of<BM>(a.ws, share, t0 > 0 ? 0 : 1);
+        const bool whole = t0 == 0 && u.u1 <= sh.end;
+        if (t0 == 0 && !whole) record = record_of(a, u, sh.per);
+        float* slot = slot_of<BM>(a.ws, sh.index, t0 > 0 ? 0 : 1);
         float* red = reinterpret_cast<float*>(&tiles[wave][0][0]);     // 16 rows of kRed
         const int orow = threadIdx.x >> 4, ocol = (threadIdx.x & 15) * 8;
         __syncthreads();
@@ -684,14 +722,9 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
             __syncthreads();
         }
         at = u.u0 + t1;
-        // the next unit of the line: another block or head, or a later sequence
-        const int64_t steps = uniform(seq_steps(a, u.q));
-        if (at >= start + steps) {
-            start += steps;
-            ++s;
-        }
+        next_seq(a, sh, at);
     }
-    leave_record(a, share, record);
+    leave_record(a, sh.index, record);
 }
 
 // Many rows: BM = 128, four waves of two 16-row blocks, keys in tiles of 64 that the
@@ -705,23 +738,12 @@ template <bool SMALL>
 __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
     constexpr int RB = 2;
     __shared__ __attribute__((aligned(16))) uint16_t tiles[2][2][WT * D];
-    __shared__ int64_t sums[NWAVE], found[2];
+    __shared__ int64_t lds[NWAVE + 2];
     const int lane = threadIdx.x & 63, g = lane >> 4, l16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool causal = a.mask == nullptr;
 
-    const Line ln = lay_out(a, sums);
-    const int64_t per = uniform(plan::share(ln.total, kGroups, kLeastSteps));
-    const int64_t used = uniform(quotient(ln.total + per - 1, per));
-    if (blockIdx.x >= used) {
-        leave_record(a, blockIdx.x, Record{-1, 0, 0, 0});
-        return;
-    }
-    const int64_t share = share_index(blockIdx.x, used);
-    const int64_t begin = share * per, end = min(begin + per, ln.total);
-    int s;
-    int64_t start;
-    find_seq(a, ln, begin, found, &s, &start);
+    Share sh = find_share(a, lds);
     Record record = {-1, 0, 0, 0};
 
     // copy round r fills tile rows 16 r + 4 wave + lane / 16, place lane % 16
@@ -736,13 +758,9 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
         const int r = 4 * g + (l16 >> 2), col = 16 * dt + 4 * (l16 & 3);
         vread[dt] = r * D + vpos(r, col >> 3) * 8 + (col & 7);
     }
-    for (int64_t at = begin; at < end;) {
-        if (seq_of(a, s).blocks == 0) {        // no new tokens: no steps either
-            ++s;
-            continue;
-        }
-        const Unit u = unit_at(a, s, start, at);
-        const int t0 = (int)(at - u.u0), t1 = (int)(min(end, u.u1) - u.u0);
+    for (int64_t at = sh.begin; at < sh.end;) {
+        const Unit u = unit_at(a, sh.q, sh.s, sh.start, at);
+        const int t0 = (int)(at - u.u0), t1 = (int)(min(sh.end, u.u1) - u.u0);
         const int lim = plan::block_keys(u.q, u.block, a.rows, causal);
         const int all = seen_by_all(a, u);
         const Keys src = keys_of(a, u, lim);
@@ -883,9 +901,9 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
             __syncthreads();
         }
 
-        const bool whole = t0 == 0 && u.u1 <= end;
-        if (t0 == 0 && !whole) record = record_of(a, u, per);
-        float* slot = slot_of<kWideRows>(a.ws, share, t0 > 0 ? 0 : 1);
+        const bool whole = t0 == 0 && u.u1 <= sh.end;
+        if (t0 == 0 && !whole) record = record_of(a, u, sh.per);
+        float* slot = slot_of<kWideRows>(a.ws, sh.index, t0 > 0 ? 0 : 1);
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
             const float l = row_sum4(lrun[r]);
@@ -912,14 +930,9 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
             }
         }
         at = u.u0 + t1;
-        // the next unit of the line: another block or head, or a later sequence
-        const int64_t steps = uniform(seq_steps(a, u.q));
-        if (at >= start + steps) {
-            start += steps;
-            ++s;
-        }
+        next_seq(a, sh, at);
     }
-    leave_record(a, share, record);
+    leave_record(a, sh.index, record);
 }
 
 // The unit that begins in share blockIdx.x and goes on behind it: its pieces are
