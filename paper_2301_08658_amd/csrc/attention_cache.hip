@@ -44,9 +44,6 @@ constexpr int KT = 32;                 // keys of a wave's tile
 constexpr int kGroups = 512;           // shares: two workgroups per CU on 256 CUs
 constexpr int kLeastSteps = 1;
 constexpr int kXcds = 8;
-// largest base-2 gain of a row maximum absorbed without rescaling (weights stay
-// below 2^8, exact in bf16's range)
-constexpr float kSlack = 8.f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -289,12 +286,12 @@ __device__ __forceinline__ Record record_of(const Args& a, const Unit& u, int64_
 struct Keys {
     const_ints table;
     int64_t head0, half;       // elements: the head in a page, and from keys to values
-    int lim, shift, max_pages, n_pages;
+    int lim, end, shift, max_pages, n_pages;   // keys that rows see; that the piece reads
     const uint16_t* pages;
-    // the page of a key that some row may see, -1 for none
+    // the page of a key of the piece, -1 for none
     __device__ __forceinline__ int page_at(int key) const {
         const int col = key >> shift;
-        const int e = key < lim && col < max_pages ? table[col] : -1;
+        const int e = key < end && col < max_pages ? table[col] : -1;
         return e >= 0 && e < n_pages ? e : -1;
     }
     // N keys of one page from `key` on, as buffer resources of keys and values: rows at
@@ -312,13 +309,14 @@ struct Keys {
                        dma::kRsrcWord3};
     }
 };
-__device__ __forceinline__ Keys keys_of(const Args& a, const Unit& u, int lim) {
+__device__ __forceinline__ Keys keys_of(const Args& a, const Unit& u, int lim, int end) {
     Keys k;
     k.shift = a.cache.page_shift;
     k.table = (const_ints)(uintptr_t)(a.batch.table + (int64_t)u.s * a.batch.ld_table);
     k.head0 = ((int64_t)u.head << k.shift) * D;
     k.half = ((int64_t)a.cache.kv_heads << k.shift) * D;
     k.lim = lim;
+    k.end = end;
     k.max_pages = a.batch.max_pages;
     k.n_pages = a.cache.n_pages;
     k.pages = a.cache.pages;
@@ -405,35 +403,48 @@ __device__ __forceinline__ void clear_odd(u32x4* chunk) {
     *chunk = v;
 }
 
-// Softmax of a row's new scores (N 16-key tiles, scaled to base 2): weights in sc,
-// running maximum, sum (the lane's own keys; joined at the end) and output moved.
+// Softmax of a row's new scores (N 16-key tiles): weights exp2(scale x - m) in sc,
+// running reference m, sum l (the lane's own keys; joined at the end) and output
+// moved.  The reference is a maximum of earlier scores and stays while it does: the
+// weights are formed first, and only where a lane's sum leaves kRoom (a weight above
+// 2^10: a score far above all before it; or a row without a reference yet) does the
+// wave look for maxima, move O and l and form them again.  O / l and m + log2 l do
+// not depend on the reference.  A maximum in every step took a fifth of the
+// kernel's vector instructions.
+constexpr float kRoom = 1024.f;
 template <int N>
 __device__ __forceinline__ void softmax_step(f32x4 (&sc)[N], float scale, float& m, float& l,
                                              f32x4 (&o)[8]) {
-    float mx = -INFINITY;
+    f32x4 p[N];
+    float rs;
+    auto weights = [&] {
+        const float msub = m == -INFINITY ? 0.f : m;
+        rs = 0.f;
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-        mx = fmaxf(mx, fmaxf(fmaxf(sc[j][0], sc[j][1]), fmaxf(sc[j][2], sc[j][3])));
-    const float mnew = fmaxf(m, row_max4(mx) * scale);
-    // the exponentials' reference moves when a row gains more than kSlack on it;
-    // results differ by rounding only
-    if (__builtin_amdgcn_ballot_w64(mnew > m + kSlack) != 0) {
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                p[j][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[j][e], scale, -msub));
+                rs += p[j][e];
+            }
+    };
+    weights();
+    if (__builtin_amdgcn_ballot_w64(!(rs <= kRoom) || m == -INFINITY) != 0) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            mx = fmaxf(mx, fmaxf(fmaxf(sc[j][0], sc[j][1]), fmaxf(sc[j][2], sc[j][3])));
+        const float mnew = fmaxf(m, row_max4(mx) * scale);
         const float alpha = weight_of(m, mnew);
         l *= alpha;
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) o[dt] *= alpha;
         m = mnew;
+        weights();
     }
-    const float msub = m == -INFINITY ? 0.f : m;
-    float rs = 0.f;
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            sc[j][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[j][e], scale, -msub));
-            rs += sc[j][e];
-        }
     l += rs;
+#pragma unroll
+    for (int j = 0; j < N; ++j) sc[j] = p[j];
 }
 
 // Weights of a 32-key slice as the products' operand, rounded to bf16 (half a step
@@ -501,7 +512,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
         const int t0 = (int)(at - u.u0), t1 = (int)(min(sh.end, u.u1) - u.u0);
         const int lim = plan::block_keys(u.q, u.block, a.rows, causal);
         const int all = seen_by_all(a, u);
-        const Keys src = keys_of(a, u, lim);
+        const Keys src = keys_of(a, u, lim, lim);
 
         // rows: token block * rows + r / group of the sequence, query head r % group
         int tok[RT];
@@ -763,7 +774,9 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
         const int t0 = (int)(at - u.u0), t1 = (int)(min(sh.end, u.u1) - u.u0);
         const int lim = plan::block_keys(u.q, u.block, a.rows, causal);
         const int all = seen_by_all(a, u);
-        const Keys src = keys_of(a, u, lim);
+        const int first = t0 * plan::kStep;
+        const int last = min(t1 * plan::kStep, lim);      // keys [first, last) of the piece
+        const Keys src = keys_of(a, u, lim, last);
         constexpr int P = SMALL ? 4 : 1, PK = WT / P;     // pages of a tile, keys of each
         auto look_up = [&](int base, int (&page)[P]) {
 #pragma unroll
@@ -802,8 +815,6 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
             for (int dt = 0; dt < 8; ++dt) o[r][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
 
-        const int first = t0 * plan::kStep;
-        const int last = min(t1 * plan::kStep, lim);      // keys [first, last) of the piece
         int page[P], ahead[P];            // of the tile at hand, of the one to be copied
         look_up(first, page);
         if (first < last) {
@@ -817,25 +828,32 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
         for (int base = first; base < last; base += WT, buf ^= 1) {
             const uint16_t* kt = tiles[buf][0];
             const uint16_t* vt = tiles[buf][1];
-            const bool next = base + WT < last;
             f32x4 sc[RB][4];
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int r = 0; r < RB; ++r) sc[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            // Fragments are read one slice of the head dimension ahead of their
+            // products.  The next tile's copies go into the other buffer, which was last
+            // read before the last barrier; behind the piece's end they find no page
+            // and fill zeros, which costs less than branches around them.
+            bf16x8 kf[2][4];
+            auto read = [&](int ks) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    kf[ks & 1][j] = *reinterpret_cast<const bf16x8*>(kt + 16 * j * D + kread[ks]);
+            };
+            read(0);
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks) {
+                if (ks < 3) read(ks + 1);
+                copy(base + WT, ahead, buf ^ 1, ks);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const bf16x8 kf =
-                        *reinterpret_cast<const bf16x8*>(kt + 16 * j * D + kread[ks]);
+                for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int r = 0; r < RB; ++r)
-                        sc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][ks], sc[r][j],
-                                                                           0, 0, 0);
-                }
-                // the other buffer was last read before the last barrier
-                if (next) copy(base + WT, ahead, buf ^ 1, ks);
+                        sc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks & 1][j], qf[r][ks],
+                                                                           sc[r][j], 0, 0, 0);
             }
             bool masked = base + WT > all || base + WT > lim;
 #pragma unroll

@@ -11,7 +11,10 @@
 // + 3 of its token for every head, and they are formed once per worker.
 //
 // Angles: position * inv_freq is formed in 64 bits and reduced to a fraction
-// of a turn there; 32 bits would lose 0.06 radians at position 10^6.
+// of a turn there; 32 bits would lose 0.06 radians at position 10^6.  The hardware's
+// sine and cosine take turns and are off by 1.3e-7 at most (measured over half a turn
+// either way; the library's sincospi by 5e-8, at ten times the instructions, which
+// is what bounded the kernels).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -95,7 +98,9 @@ struct Lane {
             if (turned) {
                 const double t = (double)position * ((double)inv_freq[4 * l + e] *
                                                      0.15915494309189533577);   // 1 / (2 pi)
-                sincospif(2.f * (float)(t - rint(t)), &s[e], &c[e]);
+                const float f = (float)(t - rint(t));
+                s[e] = __builtin_amdgcn_sinf(f);
+                c[e] = __builtin_amdgcn_cosf(f);
             }
         }
     }
@@ -165,6 +170,22 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(Args A) {
     const int part = (int)(w - t * A.parts);
     if (t >= A.tokens) return;
 
+    // the first heads are asked for before the token's place is looked up
+    Lane<INTER> ln;
+    ln.place(l, A.rot);
+    const uint16_t* xrow = A.x + t * A.ldx;
+    uint16_t* yrow = A.y + t * A.ldy;
+    constexpr int U = 4;
+    u32x2 ra[U], rb[U];
+    auto load = [&](int h0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int h = h0 + u * A.parts;
+            if (h < A.heads) ln.load(xrow + (int64_t)h * kHead, ra[u], rb[u]);
+        }
+    };
+    load(part);
+
     int position = 0;
     uint16_t *kdst = nullptr, *vdst = nullptr;      // the token's place of key head 0
     if constexpr (CACHED) {
@@ -183,24 +204,14 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(Args A) {
     } else {
         position = position_of(A, t);
     }
-    Lane<INTER> ln;
-    ln.place(l, A.rot);
     float wq[8], wk[8];
     ln.weight(A.qw, wq);
     ln.weight(A.kw, wk);
     ln.angles(l, A.inv_freq, position);
 
-    const uint16_t* xrow = A.x + t * A.ldx;
-    uint16_t* yrow = A.y + t * A.ldy;
     int kv = part / A.per_kv, r = part - kv * A.per_kv;
-    constexpr int U = 4;
     for (int h0 = part; h0 < A.heads; h0 += U * A.parts) {
-        u32x2 ra[U], rb[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int h = h0 + u * A.parts;
-            if (h < A.heads) ln.load(xrow + (int64_t)h * kHead, ra[u], rb[u]);
-        }
+        if (h0 != part) load(h0);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int h = h0 + u * A.parts;
@@ -364,16 +375,21 @@ __global__ __launch_bounds__(kSumThreads) void weight_sum_kernel(const float* pa
     }
 }
 
-// Workers of one token: as many as it takes to fill the chip (32 waves on each
-// of 256 CUs), in fours so that a wave reads consecutive heads.
+// Workers of one token: as many as it takes to fill the chip, in fours so that a
+// wave reads consecutive heads.  A worker looks its token up and forms its angles
+// before the first head, so more of them cost: 16 waves per CU take 52 us for 8192 tokens
+// of 60 heads (4.8 TB/s) and 15.8 for 1700 tokens of 48 into a cache, 8 waves 57 and
+// 15.0, 32 waves 52 and 16.7, 64 waves 56 and 22.
 int token_parts(int64_t tokens, int heads, int64_t want) {
     const int64_t need = (want + tokens - 1) / tokens;
     const int64_t p = need <= 1 ? 1 : (need + 3) / 4 * 4;
     return (int)std::min<int64_t>(p, heads);
 }
 
-constexpr int64_t kFwdWorkers = 256 * 32 * 4;
-constexpr int kBwdGroups = 1024;   // four workgroups per CU: 16 waves
+constexpr int64_t kFwdWorkers = 256 * 16 * 4;
+// four workgroups per CU: 8192 tokens of 60 heads take 77 us (4.9 TB/s; 512 groups 104, 768
+// 94, 1536 79, 2048 80)
+constexpr int kBwdGroups = 1024;
 
 Args common(const NormRope& f, const uint16_t* x, int64_t ldx, uint16_t* y, int64_t ldy,
             int64_t tokens, int64_t seq, int kv_heads, int group, int parts) {
