@@ -982,16 +982,16 @@ struct Joined {
         l = 0.f;
         v = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    __device__ __forceinline__ void add(const Joined& b) {
-        const float top = fmaxf(m, b.m), f = weight_of(m, top), g = weight_of(b.m, top);
+    __device__ __forceinline__ void add(float m2, float l2, const f32x4& v2) {
+        const float top = fmaxf(m, m2), f = weight_of(m, top), f2 = weight_of(m2, top);
         m = top;
-        l = l * f + b.l * g;
-        v = v * f + b.v * g;
+        l = l * f + l2 * f2;
+        v = v * f + v2 * f2;
     }
 };
 template <int BM, int R, int NT>
 __global__ __launch_bounds__(NT) void join_kernel(Args a) {
-    constexpr int H = NT / 32, AT_ONCE = 8;
+    constexpr int H = NT / 32;
     __shared__ float parts[H][D + 4];
     const int64_t share = blockIdx.x;
     const Record rec = reinterpret_cast<const Record*>(a.ws)[share];
@@ -999,10 +999,10 @@ __global__ __launch_bounds__(NT) void join_kernel(Args a) {
     const int hw = threadIdx.x / 32, l32 = threadIdx.x & 31;
     const int n = min(rec.tokens * a.group, BM);      // rows of the unit
     const int pieces = rec.last - (int)share + 1;
-    auto piece_of = [&](int i, int row) {
+    auto add_piece = [&](Joined& j, int i, int row) {
         const float* p = slot_of<BM>(a.ws, share + i, i == 0);
-        return Joined{p[BM * D + row], p[BM * D + BM + row],
-                      *reinterpret_cast<const f32x4*>(p + row * D + 4 * l32)};
+        j.add(p[BM * D + row], p[BM * D + BM + row],
+              *reinterpret_cast<const f32x4*>(p + row * D + 4 * l32));
     };
     auto finish = [&](const Joined& r, int row) {
         const int j = row / a.group, hq = rec.head * a.group + row - j * a.group;
@@ -1019,26 +1019,15 @@ __global__ __launch_bounds__(NT) void join_kernel(Args a) {
             for (int row = row0 + hw; row < row1; row += H) {
                 j.clear();
 #pragma unroll 2
-                for (int i = 0; i < pieces; ++i) j.add(piece_of(i, row));
+                for (int i = 0; i < pieces; ++i) add_piece(j, i, row);
                 finish(j, row);
             }
             continue;
         }
         for (int row = row0; row < row1; ++row) {
             j.clear();
-            // eight pieces are under way at a time: 256 of them (one token over 131000
-            // cached ones, eight rows) took 39 us with the attention when they were added
-            // as they came, 34 so, 39 with 512 threads, 51 with 1024
-            for (int i0 = hw; i0 < pieces; i0 += AT_ONCE * H) {
-                Joined next[AT_ONCE];
-#pragma unroll
-                for (int k = 0; k < AT_ONCE; ++k) {
-                    next[k].clear();
-                    if (i0 + k * H < pieces) next[k] = piece_of(i0 + k * H, row);
-                }
-#pragma unroll
-                for (int k = 0; k < AT_ONCE; ++k) j.add(next[k]);
-            }
+#pragma unroll 4
+            for (int i = hw; i < pieces; i += H) add_piece(j, i, row);
             *reinterpret_cast<f32x4*>(&parts[hw][4 * l32]) = j.v;
             if (l32 == 0) {
                 parts[hw][D] = j.m;
@@ -1049,8 +1038,8 @@ __global__ __launch_bounds__(NT) void join_kernel(Args a) {
                 j.clear();
 #pragma unroll
                 for (int i = 0; i < H; ++i)
-                    j.add(Joined{parts[i][D], parts[i][D + 1],
-                                 *reinterpret_cast<const f32x4*>(&parts[i][4 * l32])});
+                    j.add(parts[i][D], parts[i][D + 1],
+                          *reinterpret_cast<const f32x4*>(&parts[i][4 * l32]));
                 finish(j, row);
             }
             __syncthreads();
@@ -1106,10 +1095,10 @@ hipError_t launch_cache_attention(const CacheAttentionProblem& p, hipStream_t s)
     const int64_t rows = (int64_t)p.group * p.max_new;
     const int shift = p.cache.page_shift;
     if (bm == 16)
-        return launch<16, 1, 256>(shift < 5 ? attention_cache_kernel<1, true>
+        return launch<16, 1, 512>(shift < 5 ? attention_cache_kernel<1, true>
                                             : attention_cache_kernel<1, false>, a, grid, rows, s);
     if (bm == 32)
-        return launch<32, 1, 256>(shift < 5 ? attention_cache_kernel<2, true>
+        return launch<32, 1, 512>(shift < 5 ? attention_cache_kernel<2, true>
                                             : attention_cache_kernel<2, false>, a, grid, rows, s);
     return launch<kWideRows, 16, 256>(shift < 6 ? attention_cache_wide_kernel<true>
                                                 : attention_cache_wide_kernel<false>, a, grid, rows,
