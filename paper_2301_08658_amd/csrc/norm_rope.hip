@@ -43,6 +43,7 @@ struct Args {
     int norm, rot, heads, per_kv, group;   // heads: kv_heads * per_kv, per_kv = group + 2
     int parts, step_kv, step_r;            // a worker's next head: parts = step_kv * per_kv + step_r
     int copy_v;
+    int64_t stride;                        // tokens between a worker's visits (backward)
     float* part;                           // weight-gradient partials, nullable
     CacheView cache;
     BatchView batch;
@@ -252,8 +253,8 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(Args A) {
 }
 
 // dx = r (g - x r mean(g o x r)), g = w o (dy turned back); dw = sum of
-// (dy turned back) o x r.  A worker walks tokens W apart (W workers' slots in
-// the grid) and keeps its lanes' share of both weight gradients in registers;
+// (dy turned back) o x r.  A worker walks tokens `stride` apart and keeps its lanes'
+// share of both weight gradients in registers;
 // the workgroup adds its workers in order and leaves 256 partial sums, which
 // weight_sum_kernel adds in order.  The grid is a function of the sizes alone,
 // so the sums are too.
@@ -262,7 +263,6 @@ __global__ __launch_bounds__(kThreads) void norm_rope_bwd_kernel(Args A) {
     __shared__ float red[kWorkers][2 * kHead];
     const int lane = threadIdx.x & 63, l = lane & 15;
     const int64_t w = (int64_t)blockIdx.x * kWorkers + threadIdx.x / 16;
-    const int64_t stride = (int64_t)gridDim.x * kWorkers / A.parts;   // tokens between visits
     const int part = (int)(w % A.parts);
     Lane<INTER> ln;
     ln.place(l, A.rot);
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(kThreads) void norm_rope_bwd_kernel(Args A) {
     for (int e = 0; e < 8; ++e) gq[e] = gk[e] = 0.f;
 
     // workers past the last whole token slot have nothing
-    for (int64_t t = w / A.parts; t < A.tokens && w / A.parts < stride; t += stride) {
+    for (int64_t t = w / A.parts; t < A.tokens && w / A.parts < A.stride; t += A.stride) {
         ln.angles(l, A.inv_freq, position_of(A, t));
         const uint16_t* xrow = A.x + t * A.ldx;
         const uint16_t* grow = A.dy + t * A.lddy;
@@ -387,8 +387,8 @@ int token_parts(int64_t tokens, int heads, int64_t want) {
 }
 
 constexpr int64_t kFwdWorkers = 256 * 16 * 4;
-// four workgroups per CU: 8192 tokens of 60 heads take 77 us (4.9 TB/s; 512 groups 104, 768
-// 94, 1536 79, 2048 80)
+// Most groups of the backward: four workgroups per CU (8192 tokens of 60 heads take 77 us,
+// 4.9 TB/s; 512 groups 104, 768 94, 1536 79, 2048 80).
 constexpr int kBwdGroups = 1024;
 
 Args common(const NormRope& f, const uint16_t* x, int64_t ldx, uint16_t* y, int64_t ldy,
@@ -413,13 +413,36 @@ Args common(const NormRope& f, const uint16_t* x, int64_t ldx, uint16_t* y, int6
     return a;
 }
 
-int64_t bwd_groups(int64_t tokens) {   // at most 16 heads' workers per token
-    return std::min<int64_t>(kBwdGroups, tokens);
+// The backward's grid: parts of a token's heads (in fours, so that a wave reads
+// consecutive heads) and the tokens between a worker's visits.  A visit costs about two
+// heads beside its heads (the angles), and all workers get the same number of visits:
+// 5001 tokens of 45 heads from memory take 67 us, 75 where a fifth of the workers had
+// a second token.
+struct BwdPlan {
+    int parts;
+    int64_t stride, groups;
+};
+int64_t most_groups(int64_t tokens) { return std::min<int64_t>(kBwdGroups, tokens); }
+BwdPlan bwd_plan(int64_t tokens, int heads) {
+    const int64_t workers = most_groups(tokens) * kWorkers;
+    BwdPlan best = {1, 1, 1};
+    int64_t least = INT64_MAX;
+    for (int p = std::min(4, heads); p <= heads && p <= workers; p += 4) {
+        const int64_t at_once = workers / p, visits = (tokens + at_once - 1) / at_once;
+        const int64_t cost = visits * ((heads + p - 1) / p + 2);
+        if (cost < least) {
+            least = cost;
+            best.parts = p;
+            best.stride = (tokens + visits - 1) / visits;
+        }
+    }
+    best.groups = (best.stride * best.parts + kWorkers - 1) / kWorkers;
+    return best;
 }
 
 }  // namespace
 
-int64_t norm_rope_ws_floats(int64_t tokens) { return bwd_groups(tokens) * 2 * kHead; }
+int64_t norm_rope_ws_floats(int64_t tokens) { return most_groups(tokens) * 2 * kHead; }
 
 hipError_t launch_norm_rope(const NormRopeProblem& p, hipStream_t s) {
     const int parts = token_parts(p.tokens, p.kv_heads * (p.group + 2), kFwdWorkers);
@@ -441,11 +464,11 @@ hipError_t launch_norm_rope_bwd(const NormRopeBwdProblem& p, hipStream_t s) {
         weight_sum_kernel<<<16, kSumThreads, 0, s>>>(nullptr, 0, p.dqw, p.dkw);
         return hipGetLastError();
     }
-    const int heads = p.kv_heads * (p.group + 2);
-    const int64_t grid = bwd_groups(p.tokens);
-    const int parts = (int)std::min<int64_t>(
-        token_parts(p.tokens, heads, grid * kWorkers), grid * kWorkers);
-    Args a = common(p.f, p.x, p.ldx, p.dx, p.lddx, p.tokens, p.seq, p.kv_heads, p.group, parts);
+    const BwdPlan plan = bwd_plan(p.tokens, p.kv_heads * (p.group + 2));
+    const int64_t grid = plan.groups;
+    Args a = common(p.f, p.x, p.ldx, p.dx, p.lddx, p.tokens, p.seq, p.kv_heads, p.group,
+                    plan.parts);
+    a.stride = plan.stride;
     a.dy = p.dy;
     a.lddy = p.lddy;
     a.copy_v = p.dy != p.dx;
