@@ -783,8 +783,10 @@ atp_status check_matrix(const void* p, int64_t rows, int64_t ld, int64_t cols, c
 }
 atp_status check_vector(const void* p, const char* name) { return check_vec(p, name); }
 atp_status run_timed(const char* name, double flops, double bytes, hipStream_t s,
-                     const std::function<hipError_t()>& launch) {
-    return timed(name, flops, bytes, s, launch);
+                     hipError_t (*launch)(void*), void* arg) {
+    if (g_prof_on) return timed(name, flops, bytes, s, [&] { return launch(arg); });
+    const hipError_t e = launch(arg);
+    return e == hipSuccess ? ATP_OK : hip_fail(e, name);
 }
 }  // namespace abi
 }  // namespace atp

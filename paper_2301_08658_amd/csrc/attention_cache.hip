@@ -257,8 +257,12 @@ __device__ __forceinline__ void next_seq(const Args& a, Share& sh, int64_t at) {
     if (at < sh.start + steps) return;
     sh.start += steps;
     if (at >= sh.end) return;
-    do sh.q = seq_of(a, ++sh.s);
-    while (sh.q.blocks == 0);
+    // lengths that change under a running kernel must not lead it astray
+    while (sh.s + 1 < a.batch.n_seqs) {
+        sh.q = seq_of(a, ++sh.s);
+        if (sh.q.blocks > 0) return;
+    }
+    sh.end = at;
 }
 
 // The workspace: a record of every share, then two slots per share.  The record
@@ -509,6 +513,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
     }
     for (int64_t at = sh.begin; at < sh.end;) {
         const Unit u = unit_at(a, sh.q, sh.s, sh.start, at);
+        if (u.u1 <= at || u.u0 > at) break;     // as above
         const int t0 = (int)(at - u.u0), t1 = (int)(min(sh.end, u.u1) - u.u0);
         const int lim = plan::block_keys(u.q, u.block, a.rows, causal);
         const int all = seen_by_all(a, u);
@@ -771,6 +776,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
     }
     for (int64_t at = sh.begin; at < sh.end;) {
         const Unit u = unit_at(a, sh.q, sh.s, sh.start, at);
+        if (u.u1 <= at || u.u0 > at) break;     // as above
         const int t0 = (int)(at - u.u0), t1 = (int)(min(sh.end, u.u1) - u.u0);
         const int lim = plan::block_keys(u.q, u.block, a.rows, causal);
         const int all = seen_by_all(a, u);
@@ -1060,7 +1066,7 @@ hipError_t launch(void (*kernel)(Args), const Args& a, unsigned grid, int64_t ro
                   hipStream_t s) {
     kernel<<<grid, NTHR, 0, s>>>(a);
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || grid <= 1) return e;
+    if (e != hipSuccess) return e;
     const unsigned per = (unsigned)((std::min<int64_t>(rows, BM) + R - 1) / R);
     join_kernel<BM, R, NT><<<dim3(grid, per), NT, 0, s>>>(a);
     return hipGetLastError();

@@ -194,8 +194,10 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(Args A) {
         if (s < 0 || s >= A.batch.n_seqs) return;    // a padding row
         const int64_t at = (int64_t)max(A.batch.ctx[s], 0) + (t - A.batch.cu[s]);
         position = A.pos ? A.pos[t] : (int)at;
+        // (a list that does not ascend can put a token before its sequence)
         const int64_t col = at >> A.cache.page_shift;
-        const int page = col < A.batch.max_pages ? A.batch.table[s * A.batch.ld_table + col] : -1;
+        const int page = col >= 0 && col < A.batch.max_pages
+                             ? A.batch.table[s * A.batch.ld_table + col] : -1;
         if (page >= 0 && page < A.cache.n_pages) {
             const int64_t slot = at & ((1 << A.cache.page_shift) - 1);
             const int64_t half = (int64_t)A.cache.kv_heads << A.cache.page_shift;

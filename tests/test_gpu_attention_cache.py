@@ -262,3 +262,21 @@ def test_repeats_and_streams():
     assert torch.equal(out, again) and torch.equal(lse, l2)
     again, l2 = c.run(with_lse=False)
     assert torch.equal(out, again) and (l2 == 9).all()
+
+
+def test_lists_that_do_not_ascend_stay_inside():
+    """cu_new and ctx values that the contract forbids: whatever the rows then are,
+    only rows of the step are written."""
+    pool = torch.randn((4, 2, 1, 16, D), generator=torch.Generator().manual_seed(1)).to(BF).to(DEV)
+    q = torch.randn((40, D), generator=torch.Generator().manual_seed(2)).to(BF).to(DEV)
+    out = torch.full((60, D), 9.0, dtype=BF, device=DEV)
+    for cu, ctx in (([0, 100, 5, 8], [0, 0, 0]), ([7, 3, 9, 1], [5, -9, 2 ** 31 - 1]),
+                    ([-4, 2, 2, 6], [31, 30, 0])):
+        for max_new in (1, 20, 40):
+            ws = torch.empty(atp.atp_attention_cache_workspace_bytes(1, 1, max_new),
+                             dtype=torch.uint8, device=DEV)
+            batch = atp.kv_batch(torch.tensor([[0, 1], [1, 0], [1, 9]], dtype=torch.int32,
+                                              device=DEV), ints(ctx), ints(cu))
+            atp.atp_attention_cache_fwd(atp.kv_cache(pool), batch, 40, 1, max_new, q, out[10:50],
+                                        workspace=ws)
+    assert (out[:10] == 9).all() and (out[50:] == 9).all()

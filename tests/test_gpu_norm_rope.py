@@ -219,6 +219,22 @@ def test_append(page, kv, group, tree):
     assert torch.equal(pool.cpu()[~touched], before.cpu()[~touched])
 
 
+def test_lists_that_do_not_ascend_stay_inside():
+    """cu_new and ctx values that the contract forbids: whatever the rows then are,
+    nothing outside the pool and q is written."""
+    i32 = dict(dtype=torch.int32, device=DEV)
+    gpu, _ = setup()
+    buf = torch.zeros((6, 2, 1, 16, D), dtype=BF, device=DEV)
+    pool = buf[2:4]
+    q = torch.zeros((12, D), dtype=BF, device=DEV)
+    for cu, ctx in (([0, 100, 5, 8], [0, 0, 0]), ([7, 3, 9, 1], [5, -9, 2 ** 31 - 1]),
+                    ([-4, 2, 2, 6], [31, 30, 0])):
+        batch = atp.kv_batch(torch.tensor([[0, 1], [1, 0], [1, 9]], **i32),
+                             torch.tensor(ctx, **i32), torch.tensor(cu, **i32))
+        atp.atp_qk_norm_rope_cache(atp.kv_cache(pool), batch, 8, 1, gpu, block(8, 1, 1, 3), q[2:10])
+    assert not buf[:2].any() and not buf[4:].any() and not q[:2].any() and not q[10:].any()
+
+
 def test_same_bits_with_the_block_and_the_cache():
     """The cached form's queries and keys are the block form's, bit for bit."""
     kv, group, t = 2, 2, 70
