@@ -327,9 +327,19 @@ __device__ __forceinline__ Keys keys_of(const Args& a, const Unit& u, int lim, i
     return k;
 }
 
-// Keys below this one are seen by every row of a unit.
-__device__ __forceinline__ int seen_by_all(const Args& a, const Unit& u) {
-    return u.q.ctx + (a.mask == nullptr ? min(u.block * a.rows + 1, u.q.fresh) : 0);
+// Rows [row0, row1) of a unit: keys below `all` are seen by every one of them, keys from
+// `none` on by none (no row there: 0).
+struct Sight {
+    int all, none;
+};
+__device__ __forceinline__ Sight sight_of(const Args& a, const Unit& u, int row0, int row1,
+                                          int lim) {
+    const int tok = u.block * a.rows;
+    const int first = row0 / a.group;
+    const int last = min(min((row1 - 1) / a.group, a.rows - 1), u.q.fresh - tok - 1);
+    if (first > last) return Sight{0, 0};
+    if (a.mask != nullptr) return Sight{u.q.ctx, lim};
+    return Sight{u.q.ctx + tok + first + 1, min(u.q.ctx + tok + last + 1, lim)};
 }
 
 // Bit i: new token `tok` of the unit's sequence (-1: no row) sees key base + i.
@@ -349,14 +359,16 @@ __device__ __forceinline__ uint64_t sees_keys(const Args& a, const Unit& u, int 
     return v;
 }
 
-// Infinities and NaN among the bf16 values of 16 bytes.
-__device__ __forceinline__ bool any_odd(const u32x4& v) {
-    bool odd = false;
+// Infinities and NaN among bf16 values (their exponent is all ones, and one more carries
+// into the sign's place): seen = 0 to begin with, has_odd at the end.
+__device__ __forceinline__ void look_for_odd(const u32x4& v, uint32_t& seen) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        odd |= (v[e] & 0x7f80u) == 0x7f80u || (v[e] & 0x7f800000u) == 0x7f800000u;
-    return odd;
+    for (int e = 0; e < 4; ++e) seen |= (v[e] & 0x7f807f80u) + 0x00800080u;
 }
+__device__ __forceinline__ bool has_odd(uint32_t seen) {    // in any lane
+    return __builtin_amdgcn_ballot_w64((seen & 0x80008000u) != 0) != 0;
+}
+
 // V^T's fragment of a 32-key slice: two transposing reads 16 rows apart.
 __device__ __forceinline__ bf16x8 v_fragment(const uint16_t* p) {
     const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p);
@@ -397,14 +409,14 @@ __device__ __forceinline__ void add_odd(const uint16_t* vt, const bf16x8& pf, ui
         }
     }
 }
-__device__ __forceinline__ void clear_odd(u32x4* chunk) {
-    u32x4 v = *chunk;
+__device__ __forceinline__ void clear_odd(bf16x8& chunk) {
+    u32x4 v = __builtin_bit_cast(u32x4, chunk);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         if ((v[e] & 0x7f80u) == 0x7f80u) v[e] &= 0xffff0000u;
         if ((v[e] & 0x7f800000u) == 0x7f800000u) v[e] &= 0xffffu;
     }
-    *chunk = v;
+    chunk = __builtin_bit_cast(bf16x8, v);
 }
 
 // Softmax of a row's new scores (N 16-key tiles): weights exp2(scale x - m) in sc,
@@ -516,7 +528,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
         if (u.u1 <= at || u.u0 > at) break;     // as above
         const int t0 = (int)(at - u.u0), t1 = (int)(min(sh.end, u.u1) - u.u0);
         const int lim = plan::block_keys(u.q, u.block, a.rows, causal);
-        const int all = seen_by_all(a, u);
+        const int all = sight_of(a, u, 0, BM, lim).all;
         const Keys src = keys_of(a, u, lim, lim);
 
         // rows: token block * rows + r / group of the sequence, query head r % group
@@ -645,16 +657,17 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
             // a masked place may hold anything
             bool odd = false;
             if (masked) {
+                uint32_t seen = 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    odd |= any_odd(*reinterpret_cast<const u32x4*>(vt + (i * 64 + lane) * 8));
-                odd = __builtin_amdgcn_ballot_w64(odd) != 0;
+                    look_for_odd(*reinterpret_cast<const u32x4*>(vt + (i * 64 + lane) * 8), seen);
+                odd = has_odd(seen);
             }
             if (odd) {
 #pragma unroll
                 for (int r = 0; r < RT; ++r) add_odd(vt, pf[r], sees[r], o[r]);
                 for (int i = 0; i < 8; ++i)
-                    clear_odd(reinterpret_cast<u32x4*>(vt + (i * 64 + lane) * 8));
+                    clear_odd(*reinterpret_cast<bf16x8*>(vt + (i * 64 + lane) * 8));
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             }
 #pragma unroll
@@ -779,7 +792,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
         if (u.u1 <= at || u.u0 > at) break;     // as above
         const int t0 = (int)(at - u.u0), t1 = (int)(min(sh.end, u.u1) - u.u0);
         const int lim = plan::block_keys(u.q, u.block, a.rows, causal);
-        const int all = seen_by_all(a, u);
+        const Sight sight = sight_of(a, u, 32 * wave, 32 * wave + 32, lim);
         const int first = t0 * plan::kStep;
         const int last = min(t1 * plan::kStep, lim);      // keys [first, last) of the piece
         const Keys src = keys_of(a, u, lim, last);
@@ -830,10 +843,23 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
         look_up(first + WT, ahead);
         dma::wait_vmcnt<0>();
         __syncthreads();
+        auto advance = [&](int base) {
+#pragma unroll
+            for (int h = 0; h < P; ++h) page[h] = ahead[h];
+            look_up(base + 2 * WT, ahead);
+            dma::wait_vmcnt<0>();
+            __syncthreads();
+        };
         int buf = 0;
         for (int base = first; base < last; base += WT, buf ^= 1) {
             const uint16_t* kt = tiles[buf][0];
             const uint16_t* vt = tiles[buf][1];
+            if (base >= sight.none) {     // nothing here for this wave's rows: it only copies
+#pragma unroll
+                for (int r = 0; r < 4; ++r) copy(base + WT, ahead, buf ^ 1, r);
+                advance(base);
+                continue;
+            }
             f32x4 sc[RB][4];
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -861,7 +887,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
                         sc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks & 1][j], qf[r][ks],
                                                                            sc[r][j], 0, 0, 0);
             }
-            bool masked = base + WT > all || base + WT > lim;
+            bool masked = base + WT > sight.all || base + WT > lim;
 #pragma unroll
             for (int h = 0; h < P; ++h) masked |= page[h] < 0;
             uint64_t sees[RB];
@@ -882,10 +908,11 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
                             if (!(sees[r] >> (16 * j + 4 * g + e) & 1)) sc[r][j][e] = -INFINITY;
                 }
                 // a masked place may hold anything
+                uint32_t seen = 0;
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    odd |= any_odd(*reinterpret_cast<const u32x4*>(vt + (i * 64 + lane) * 8));
-                odd = __builtin_amdgcn_ballot_w64(odd) != 0;
+                    look_for_odd(*reinterpret_cast<const u32x4*>(vt + (i * 64 + lane) * 8), seen);
+                odd = has_odd(seen);
             }
             // V^T's fragments in four groups of four, read a group ahead of their products (a
             // product pair takes 32 cycles, a read four times that; read a pair ahead, trees
@@ -904,23 +931,22 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
                 for (int sl = 0; sl < 2; ++sl)
                     pf[sl][r] = round_weights(sc[r][2 * sl], sc[r][2 * sl + 1]);
             }
-            if (odd) {                    // the same in all four waves: one tile
+            if (odd) {
 #pragma unroll
                 for (int sl = 0; sl < 2; ++sl)
 #pragma unroll
                     for (int r = 0; r < RB; ++r)
                         add_odd(vt + 32 * sl * D, pf[sl][r], (uint32_t)(sees[r] >> (32 * sl)),
                                 o[r]);
-                __syncthreads();
-                for (int i = 0; i < 4; ++i)
-                    clear_odd(reinterpret_cast<u32x4*>(tiles[buf][1] +
-                                                       (i * NTHR + (int)threadIdx.x) * 8));
-                __syncthreads();
             }
             read_values(0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (i < 3) read_values(i + 1);
+                if (odd) {
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) clear_odd(vf[i & 1][d]);
+                }
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
@@ -932,11 +958,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
                     }
                 __builtin_amdgcn_sched_barrier(0);
             }
-#pragma unroll
-            for (int h = 0; h < P; ++h) page[h] = ahead[h];
-            look_up(base + 2 * WT, ahead);
-            dma::wait_vmcnt<0>();
-            __syncthreads();
+            advance(base);
         }
 
         const bool whole = t0 == 0 && u.u1 <= sh.end;
@@ -975,9 +997,10 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
 
 // The unit that begins in share blockIdx.x and goes on behind it: its pieces are
 // slot 1 of that share and slot 0 of the following ones, added in order with a
-// running maximum.  A half wave holds a row, four values per lane.  Few pieces: it
-// takes a row's pieces by itself (a unit of 128 rows is cut in two as a rule, and the
-// rows under way count).  Many (a long context, few rows): the workgroup takes its R
+// running maximum.  A half wave holds a row, four values per lane.  Few pieces, or a row
+// for every half wave: it takes a row's pieces by itself (66 tokens of two sequences, 25
+// pieces per unit of 126 rows: 39 us with the attention, 87 where the workgroup took the
+// rows one by one).  Many pieces of few rows (a long context): the workgroup takes its R
 // rows one by one, its half waves every H-th piece each.
 constexpr int kManyPieces = 16;
 struct Joined {
@@ -1021,10 +1044,10 @@ __global__ __launch_bounds__(NT) void join_kernel(Args a) {
     for (int row0 = blockIdx.y * R; row0 < n; row0 += gridDim.y * R) {
         const int row1 = min(row0 + R, n);
         Joined j;
-        if (pieces <= kManyPieces) {
+        if (R >= H || pieces <= kManyPieces) {
             for (int row = row0 + hw; row < row1; row += H) {
                 j.clear();
-#pragma unroll 2
+#pragma unroll 4
                 for (int i = 0; i < pieces; ++i) add_piece(j, i, row);
                 finish(j, row);
             }
@@ -1106,7 +1129,7 @@ hipError_t launch_cache_attention(const CacheAttentionProblem& p, hipStream_t s)
     if (bm == 32)
         return launch<32, 1, 512>(shift < 5 ? attention_cache_kernel<2, true>
                                             : attention_cache_kernel<2, false>, a, grid, rows, s);
-    return launch<kWideRows, 16, 256>(shift < 6 ? attention_cache_wide_kernel<true>
+    return launch<kWideRows, 8, 256>(shift < 6 ? attention_cache_wide_kernel<true>
                                                 : attention_cache_wide_kernel<false>, a, grid, rows,
                                       s);
 }
