@@ -359,6 +359,18 @@ __device__ __forceinline__ uint64_t sees_keys(const Args& a, const Unit& u, int 
     return v;
 }
 
+// Scores of keys that a row does not see become -inf; a lane's are keys 16 j + 4 g + e.
+template <int N>
+__device__ __forceinline__ void hide(uint64_t sees, int g, f32x4 (&sc)[N]) {
+    const uint64_t mine = sees >> (4 * g);       // once; then bits at fixed places
+    const uint32_t half[2] = {(uint32_t)mine, (uint32_t)(mine >> 32)};
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (!(half[j >> 1] & (1u << (16 * (j & 1) + e)))) sc[j][e] = -INFINITY;
+}
+
 // Infinities and NaN among bf16 values (their exponent is all ones, and one more carries
 // into the sign's place): seen = 0 to begin with, has_odd at the end.
 __device__ __forceinline__ void look_for_odd(const u32x4& v, uint32_t& seen) {
@@ -637,11 +649,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
                     sees[r] = (uint32_t)sees_keys(a, u, tok[r], base) & there;
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (!(sees[r] >> (16 * j + 4 * g + e) & 1)) sc[r][j][e] = -INFINITY;
+                    hide<2>(sees[r], g, sc[r]);
                 }
             }
             // the products have time to spare here: the weights' second halves too
@@ -901,11 +909,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
 #pragma unroll
                 for (int r = 0; r < RB; ++r) {
                     sees[r] = sees_keys(a, u, tok[r], base) & on;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (!(sees[r] >> (16 * j + 4 * g + e) & 1)) sc[r][j][e] = -INFINITY;
+                    hide<4>(sees[r], g, sc[r]);
                 }
                 // a masked place may hold anything
                 uint32_t seen = 0;
