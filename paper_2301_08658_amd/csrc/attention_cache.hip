@@ -4,8 +4,8 @@
 // query heads.
 //
 // A unit is 16 RT rows (tokens' query heads of one key/value head) against a
-// sequence's keys; workgroup w takes an equal share of all units' steps of 128
-// keys (cache_plan.h).  A unit that lies inside one share is finished there; one
+// sequence's keys; workgroup w takes an equal share of all units' keys
+// (cache_plan.h).  A unit that lies inside one share is finished there; one
 // that is cut leaves its pieces' maxima, sums and outputs in the workspace, and
 // join_kernel adds them in order.
 //
@@ -42,7 +42,11 @@ constexpr int NWAVE = 4;
 constexpr int NTHR = 64 * NWAVE;
 constexpr int KT = 32;                 // keys of a wave's tile
 constexpr int kGroups = 512;           // shares: two workgroups per CU on 256 CUs
-constexpr int kLeastSteps = 1;
+constexpr int kLeast = plan::kTile;    // fewest keys of a share
+// What a unit costs beside its keys, in keys: 32 sequences of 4 drafts 57 us without it, 44
+// so (64: 44, 256: 42.5), 300 short contexts' tokens 67 and 53 (57, 54); with 128 rows,
+// trees 122 without it, 105 so (128: 110, 448: 106), prompt chunks 95 and 80.5 (86, 80.5).
+constexpr int kExtra = 128, kWideExtra = 320;
 constexpr int kXcds = 8;
 constexpr float kLn2 = 0.69314718055994530942f;
 
@@ -110,6 +114,7 @@ struct Args {
     float* lse;
     float* ws;
     int tokens, group, rows;     // rows: tokens of a row block
+    int extra;                   // of a unit (plan::Seq)
     int64_t cap;                 // max_pages * page size
     float scale_log2;
 };
@@ -117,14 +122,14 @@ struct Args {
 __device__ __forceinline__ plan::Seq seq_of(const Args& a, int s) {
     const const_ints cu = (const_ints)(uintptr_t)a.batch.cu;
     return plan::make_seq(((const_ints)(uintptr_t)a.batch.ctx)[s], cu[s], cu[s + 1], a.tokens,
-                          a.cap, a.rows);
+                          a.cap, a.rows, a.extra);
 }
-__device__ __forceinline__ int64_t seq_steps(const Args& a, const plan::Seq& q) {
-    return plan::steps_before(q, q.blocks, a.rows, a.mask == nullptr) * a.cache.kv_heads;
+__device__ __forceinline__ int64_t seq_line(const Args& a, const plan::Seq& q) {
+    return plan::line_of(q, q.blocks, a.rows, a.mask == nullptr) * a.cache.kv_heads;
 }
 
-// A workgroup's share of the line: steps [begin, end), the sequence of step `begin`
-// and the step that sequence starts at.  None: begin == end.
+// A workgroup's share of the line: keys [begin, end), the sequence of key `begin`
+// and the key that sequence starts at.  None: begin == end.
 struct Share {
     int64_t index, per, begin, end, start;
     int s;
@@ -133,7 +138,7 @@ struct Share {
 // Shares are numbered so that consecutive ones run on one XCD (workgroups go
 // round the eight dies): the row blocks of a head share its keys in that L2.
 __device__ __forceinline__ bool take_share(int64_t total, Share& sh) {
-    sh.per = uniform(plan::share(total, kGroups, kLeastSteps));
+    sh.per = uniform(plan::share(total, kGroups, kLeast));
     const int64_t used = uniform(quotient(total + sh.per - 1, sh.per));
     const int bid = blockIdx.x;
     if (bid >= used) {
@@ -165,7 +170,8 @@ __device__ __forceinline__ uint32_t wave_prefix(uint32_t v) {
 }
 
 __device__ __forceinline__ plan::Seq load_seq(const Args& a, int s) {
-    return plan::make_seq(a.batch.ctx[s], a.batch.cu[s], a.batch.cu[s + 1], a.tokens, a.cap, a.rows);
+    return plan::make_seq(a.batch.ctx[s], a.batch.cu[s], a.batch.cu[s + 1], a.tokens, a.cap, a.rows,
+                          a.extra);
 }
 
 // Every workgroup lays out the batch for itself: reading a few lengths costs less
@@ -178,8 +184,8 @@ __device__ __forceinline__ Share find_share(const Args& a, int64_t* lds) {
     if (n <= 64) {
         plan::Seq q = {0, 0, 0, 0, 0};
         if (lane < n) q = load_seq(a, lane);
-        const int64_t mine = lane < n ? seq_steps(a, q) : 0;
-        if (__builtin_amdgcn_ballot_w64(mine >> 25 != 0) == 0) {
+        const int64_t mine = lane < n ? seq_line(a, q) : 0;
+        if (__builtin_amdgcn_ballot_w64(mine >> 26 != 0) == 0) {
             const uint32_t upto = wave_prefix((uint32_t)mine);
             const uint32_t total = __builtin_amdgcn_readlane(upto, 63);
             if (!take_share(total, sh)) return sh;
@@ -196,7 +202,7 @@ __device__ __forceinline__ Share find_share(const Args& a, int64_t* lds) {
     }
     const int run = (n + NTHR - 1) / NTHR;
     int64_t mine = 0;
-    for (int i = tid * run; i < min((tid + 1) * run, n); ++i) mine += seq_steps(a, load_seq(a, i));
+    for (int i = tid * run; i < min((tid + 1) * run, n); ++i) mine += seq_line(a, load_seq(a, i));
     int64_t inc = mine;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -215,7 +221,7 @@ __device__ __forceinline__ Share find_share(const Args& a, int64_t* lds) {
     if (mine > 0 && before <= sh.begin && sh.begin < before + mine) {
         int i = tid * run;
         for (;; ++i) {
-            const int64_t m = seq_steps(a, load_seq(a, i));
+            const int64_t m = seq_line(a, load_seq(a, i));
             if (sh.begin < before + m || i + 1 >= n) break;
             before += m;
         }
@@ -229,7 +235,7 @@ __device__ __forceinline__ Share find_share(const Args& a, int64_t* lds) {
     return sh;
 }
 
-// One row block of one head of one sequence, and its steps [u0, u1) of the line.
+// One row block of one head of one sequence, and its keys [u0, u1) of the line.
 struct Unit {
     plan::Seq q;
     int s, head, block;
@@ -241,21 +247,21 @@ __device__ __forceinline__ Unit unit_at(const Args& a, const plan::Seq& q, int s
     const bool causal = a.mask == nullptr;
     u.s = s;
     u.q = q;
-    const int64_t head = plan::steps_before(q, q.blocks, a.rows, causal);
+    const int64_t head = plan::line_of(q, q.blocks, a.rows, causal);
     u.head = __builtin_amdgcn_readfirstlane((int)quotient(at - start, head));
     const int64_t h0 = start + u.head * head;
     u.block = __builtin_amdgcn_readfirstlane(plan::block_of(q, at - h0, a.rows, causal));
-    u.u0 = uniform(h0 + plan::steps_before(q, u.block, a.rows, causal));
-    u.u1 = uniform(h0 + plan::steps_before(q, u.block + 1, a.rows, causal));
+    u.u0 = uniform(h0 + plan::line_of(q, u.block, a.rows, causal));
+    u.u1 = uniform(h0 + plan::line_of(q, u.block + 1, a.rows, causal));
     return u;
 }
 
-// Moves a share on to the sequence of step `at` (sequences without new tokens have no
-// steps).
+// Moves a share on to the sequence of key `at` (sequences without new tokens have
+// none).
 __device__ __forceinline__ void next_seq(const Args& a, Share& sh, int64_t at) {
-    const int64_t steps = uniform(seq_steps(a, sh.q));
-    if (at < sh.start + steps) return;
-    sh.start += steps;
+    const int64_t line = uniform(seq_line(a, sh.q));
+    if (at < sh.start + line) return;
+    sh.start += line;
     if (at >= sh.end) return;
     // lengths that change under a running kernel must not lead it astray
     while (sh.s + 1 < a.batch.n_seqs) {
@@ -281,9 +287,11 @@ __device__ __forceinline__ float* slot_of(float* ws, int64_t share, int slot) {
 __device__ __forceinline__ void leave_record(const Args& a, int64_t share, const Record& r) {
     if (threadIdx.x == 0) reinterpret_cast<Record*>(a.ws)[share] = r;
 }
-__device__ __forceinline__ Record record_of(const Args& a, const Unit& u, int64_t per) {
+__device__ __forceinline__ Record record_of(const Args& a, const Unit& u, int64_t per, int lim,
+                                            int tile) {
     const int tok = u.block * a.rows;
-    return Record{(int)quotient(u.u1 - 1, per), u.q.first + tok, min(a.rows, u.q.fresh - tok), u.head};
+    return Record{(int)plan::last_share(u.u0, u.u1, per, a.extra, lim, tile), u.q.first + tok,
+                  min(a.rows, u.q.fresh - tok), u.head};
 }
 
 // Where a unit's keys are: the table row, and a head's place in a page.
@@ -505,7 +513,7 @@ __device__ __forceinline__ float log_sum(float m, float l) {
 // SMALL: pages of 16 tokens, so that a wave's tile of 32 keys spans two.
 template <int RT, bool SMALL>
 __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
-    constexpr int BM = 16 * RT;
+    constexpr int BM = 16 * RT, TILE = NWAVE * KT;
     constexpr int kRed = D + 4;      // padded row of the merge
     __shared__ __attribute__((aligned(16))) uint16_t tiles[NWAVE][2][KT * D];
     __shared__ float wm[NWAVE][BM], wl[NWAVE][BM];
@@ -538,10 +546,17 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
     for (int64_t at = sh.begin; at < sh.end;) {
         const Unit u = unit_at(a, sh.q, sh.s, sh.start, at);
         if (u.u1 <= at || u.u0 > at) break;     // as above
-        const int t0 = (int)(at - u.u0), t1 = (int)(min(sh.end, u.u1) - u.u0);
         const int lim = plan::block_keys(u.q, u.block, a.rows, causal);
         const int all = sight_of(a, u, 0, BM, lim).all;
-        const Keys src = keys_of(a, u, lim, lim);
+        const int64_t upto = min(sh.end, u.u1);
+        const plan::Piece piece =
+            plan::piece_keys(at - u.u0, upto - u.u0, a.extra, upto == u.u1, lim, TILE);
+        if (piece.first >= piece.last) {        // a cut that leaves nothing here
+            at = upto;
+            next_seq(a, sh, at);
+            continue;
+        }
+        const Keys src = keys_of(a, u, lim, piece.last);
 
         // rows: token block * rows + r / group of the sequence, query head r % group
         int tok[RT];
@@ -570,8 +585,8 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
             for (int dt = 0; dt < 8; ++dt) o[r][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
 
-        // the wave's tiles: keys [base, base + 32) of every step
-        auto base_of = [&](int t) { return t * plan::kStep + KT * wave; };
+        // the wave's tiles: 32 keys of every 128
+        constexpr int STEP = TILE;
         constexpr int P = SMALL ? 2 : 1, PK = KT / P;     // pages of a tile, keys of each
         struct Tile {
             int page[P];
@@ -603,23 +618,22 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
                                voffs[i & 1] +
                                    (uint32_t)(((SMALL ? i & 3 : i) >> 1) * 8 * D * 2), 0u);
         };
-        int t = t0;
-        bool more = t < t1 && base_of(t) < lim;
+        int base = piece.first + KT * wave;
+        bool more = base < piece.last;
         Tile cur;
         int ahead[P];                              // pages of the tile after the next copy
-        look_up(base_of(t), ahead);
+        look_up(base, ahead);
         if (more) {
-            cur = aim(base_of(t), ahead);
+            cur = aim(base, ahead);
             copy_keys(cur);
             copy_values(cur);
         }
-        look_up(base_of(t + 1), ahead);
+        look_up(base + STEP, ahead);
         while (more) {
-            const int base = base_of(t);
-            const bool next = t + 1 < t1 && base_of(t + 1) < lim;
+            const bool next = base + STEP < piece.last;
             Tile nxt = cur;
-            if (next) nxt = aim(base_of(t + 1), ahead);
-            look_up(base_of(t + 2), ahead);
+            if (next) nxt = aim(base + STEP, ahead);
+            look_up(base + 2 * STEP, ahead);
             dma::wait_vmcnt<8>();                       // K has landed, V may be under way
             f32x4 sc[RT][2];
 #pragma unroll
@@ -691,7 +705,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
             if (next) copy_values(nxt);
             cur = nxt;
             more = next;
-            ++t;
+            base += STEP;
         }
 
         // the four waves' results of this piece, row block by row block
@@ -703,9 +717,9 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
                 wl[wave][16 * r + l16] = lrun[r];
             }
         }
-        const bool whole = t0 == 0 && u.u1 <= sh.end;
-        if (t0 == 0 && !whole) record = record_of(a, u, sh.per);
-        float* slot = slot_of<BM>(a.ws, sh.index, t0 > 0 ? 0 : 1);
+        const bool begins = piece.first == 0, whole = begins && piece.last == lim;
+        if (begins && !whole) record = record_of(a, u, sh.per, lim, TILE);
+        float* slot = slot_of<BM>(a.ws, sh.index, begins ? 1 : 0);
         float* red = reinterpret_cast<float*>(&tiles[wave][0][0]);     // 16 rows of kRed
         const int orow = threadIdx.x >> 4, ocol = (threadIdx.x & 15) * 8;
         __syncthreads();
@@ -758,7 +772,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
             }
             __syncthreads();
         }
-        at = u.u0 + t1;
+        at = upto;
         next_seq(a, sh, at);
     }
     leave_record(a, sh.index, record);
@@ -773,7 +787,7 @@ constexpr int WT = 64;                 // keys of a tile
 // SMALL: pages of fewer than 64 tokens; a tile's quarters are looked up one by one.
 template <bool SMALL>
 __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
-    constexpr int RB = 2;
+    constexpr int RB = 2, TILE = WT;
     __shared__ __attribute__((aligned(16))) uint16_t tiles[2][2][WT * D];
     __shared__ int64_t lds[NWAVE + 2];
     const int lane = threadIdx.x & 63, g = lane >> 4, l16 = lane & 15;
@@ -798,11 +812,17 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
     for (int64_t at = sh.begin; at < sh.end;) {
         const Unit u = unit_at(a, sh.q, sh.s, sh.start, at);
         if (u.u1 <= at || u.u0 > at) break;     // as above
-        const int t0 = (int)(at - u.u0), t1 = (int)(min(sh.end, u.u1) - u.u0);
         const int lim = plan::block_keys(u.q, u.block, a.rows, causal);
         const Sight sight = sight_of(a, u, 32 * wave, 32 * wave + 32, lim);
-        const int first = t0 * plan::kStep;
-        const int last = min(t1 * plan::kStep, lim);      // keys [first, last) of the piece
+        const int64_t upto = min(sh.end, u.u1);
+        const plan::Piece piece =
+            plan::piece_keys(at - u.u0, upto - u.u0, a.extra, upto == u.u1, lim, TILE);
+        if (piece.first >= piece.last) {        // a cut that leaves nothing here
+            at = upto;
+            next_seq(a, sh, at);
+            continue;
+        }
+        const int first = piece.first, last = piece.last;
         const Keys src = keys_of(a, u, lim, last);
         constexpr int P = SMALL ? 4 : 1, PK = WT / P;     // pages of a tile, keys of each
         auto look_up = [&](int base, int (&page)[P]) {
@@ -819,6 +839,14 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
             dma::lds_dma16(rv, dst + WT * D, voff + down, 0u);
         };
 
+        // the first tile is on its way while the rows are read
+        int page[P], ahead[P];            // of the tile at hand, of the one to be copied
+        look_up(first, page);
+        if (first < last) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) copy(first, page, 0, r);
+        }
+        look_up(first + WT, ahead);
         int tok[RB], hq[RB];
         bf16x8 qf[RB][4];
         f32x4 o[RB][8];
@@ -842,13 +870,6 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
             for (int dt = 0; dt < 8; ++dt) o[r][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
 
-        int page[P], ahead[P];            // of the tile at hand, of the one to be copied
-        look_up(first, page);
-        if (first < last) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) copy(first, page, 0, r);
-        }
-        look_up(first + WT, ahead);
         dma::wait_vmcnt<0>();
         __syncthreads();
         auto advance = [&](int base) {
@@ -965,9 +986,9 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
             advance(base);
         }
 
-        const bool whole = t0 == 0 && u.u1 <= sh.end;
-        if (t0 == 0 && !whole) record = record_of(a, u, sh.per);
-        float* slot = slot_of<kWideRows>(a.ws, sh.index, t0 > 0 ? 0 : 1);
+        const bool begins = piece.first == 0, whole = begins && piece.last == lim;
+        if (begins && !whole) record = record_of(a, u, sh.per, lim, TILE);
+        float* slot = slot_of<kWideRows>(a.ws, sh.index, begins ? 1 : 0);
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
             const float l = row_sum4(lrun[r]);
@@ -993,7 +1014,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
                 }
             }
         }
-        at = u.u0 + t1;
+        at = upto;
         next_seq(a, sh, at);
     }
     leave_record(a, sh.index, record);
@@ -1118,12 +1139,13 @@ hipError_t launch_cache_attention(const CacheAttentionProblem& p, hipStream_t s)
     a.tokens = (int)p.tokens;
     a.group = p.group;
     a.rows = bm / p.group;
+    a.extra = bm == kWideRows ? kWideExtra : kExtra;
     a.cap = (int64_t)p.batch.max_pages << p.cache.page_shift;
     a.scale_log2 = 1.4426950408889634f / sqrtf((float)D);
-    // no batch of these sizes has more steps than this
+    // no batch of these sizes has more shares than this
     const int64_t units = std::min<int64_t>(p.batch.n_seqs, p.tokens) + p.tokens / a.rows;
-    const int64_t steps = 2 * ((a.cap + p.tokens) / plan::kStep) + 5;
-    const int64_t most = std::min<int64_t>(units * p.cache.kv_heads, 1 << 20) * steps;
+    const int64_t most = std::min<int64_t>(units * p.cache.kv_heads, 1 << 20) *
+                         ((a.cap + p.tokens + a.rows + a.extra) / kLeast + 2);
     const unsigned grid = (unsigned)std::min<int64_t>(kGroups, most);
     const int64_t rows = (int64_t)p.group * p.max_new;
     const int shift = p.cache.page_shift;

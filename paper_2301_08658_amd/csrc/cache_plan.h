@@ -2,10 +2,11 @@
 // that the kernels run and the host can run too (no HIP types).
 //
 // A unit is one row block (up to `rows` tokens' query heads of one key/value
-// head) of one sequence; its keys are walked in steps of 128.  All units of a
-// batch are laid end to end, sequence by sequence, head by head, block by
-// block, and workgroup w of the plan takes steps [w * per, (w + 1) * per) of that
-// line: no workgroup waits for a long sequence, whatever the lengths are.
+// head) of one sequence, as long as the keys that it sees.  All units of a batch
+// are laid end to end, sequence by sequence, head by head, block by block, and
+// workgroup w of the plan takes keys [w * per, (w + 1) * per) of that line: no
+// workgroup waits for a long sequence, whatever the lengths are.  A unit also counts
+// what it costs beside its keys (reading its rows, its first tiles' latency, its end).
 #pragma once
 #include <stdint.h>
 
@@ -18,18 +19,21 @@
 namespace atp {
 namespace plan {
 
-constexpr int kStep = 128;     // keys per step: 32 for each of four waves
+constexpr int kTile = 128;     // keys that shares are cut at, where a unit's line is whole tiles
+
+ATP_PLAN_FN int64_t whole_tiles(int64_t keys) { return (keys + kTile - 1) / kTile * kTile; }
 
 struct Seq {
     int first, fresh;          // its rows of the step's buffers
     int ctx, keys;             // cached before the step; with the new ones
     int blocks;                // row blocks of a head
+    int extra;                 // keys' worth of work that a unit costs beside its keys
 };
 
 // ctx, c0, c1: the sequence's ctx, cu_new[s], cu_new[s + 1] as they stand in device
 // memory; tokens and cap (max_pages * page_size, <= 2^30) bound what they may name.
 ATP_PLAN_FN Seq make_seq(int64_t ctx, int64_t c0, int64_t c1, int64_t tokens, int64_t cap,
-                         int rows) {
+                         int rows, int extra) {
     Seq q;
     c0 = c0 < 0 ? 0 : (c0 > tokens ? tokens : c0);
     c1 = c1 < c0 ? c0 : (c1 > tokens ? tokens : c1);
@@ -39,6 +43,7 @@ ATP_PLAN_FN Seq make_seq(int64_t ctx, int64_t c0, int64_t c1, int64_t tokens, in
     q.ctx = (int)ctx;
     q.keys = (int)(ctx + q.fresh > cap ? cap : ctx + q.fresh);
     q.blocks = (q.fresh + rows - 1) / rows;
+    q.extra = extra;
     return q;
 }
 
@@ -49,41 +54,54 @@ ATP_PLAN_FN int block_keys(const Seq& q, int i, int rows, bool causal) {
     return last < q.keys ? (int)last : q.keys;
 }
 
-// sum_{j = 1 .. m} ceil(j / q)
-ATP_PLAN_FN int64_t ceil_sum(int64_t m, int64_t q) {
-    const int64_t k = m / q, r = m - k * q;
-    return q * (k * (k + 1) / 2) + r * (k + 1);
+// Length on the line of the first n row blocks of a head: whole tiles of keys, so that
+// short units are cut where tiles end; causal blocks of a sequence with several count ctx
+// + (i + 1) * rows keys, the last one (or one beyond the table) more than it sees.  No
+// division: workgroups find their units by this.
+ATP_PLAN_FN int64_t line_of(const Seq& q, int64_t n, int rows, bool causal) {
+    if (!causal || q.blocks <= 1) return n * (q.extra + whole_tiles(q.keys));
+    return n * (q.extra + q.ctx) + rows * (n * (n + 1) / 2);
 }
 
-// Steps of the first n row blocks of a head.  A causal sequence of several blocks
-// counts A + ceil((a + j) / q) for block j = 1, 2, .. with ctx = 128 A + a', a =
-// ceil(a' / rows) and q = floor(128 / rows): never less than the block's keys
-// need, and its sum has a closed form.  The new tokens count up to 128 / 120 of
-// what they need (rows = 12), the cached ones exactly.
-ATP_PLAN_FN int64_t steps_before(const Seq& q, int64_t n, int rows, bool causal) {
-    if (!causal || q.blocks <= 1) {
-        const int64_t one = (q.keys + kStep - 1) / kStep;
-        return n * (one > 0 ? one : 1);
-    }
-    const int64_t A = q.ctx / kStep, a = (q.ctx % kStep + rows - 1) / rows, w = kStep / rows;
-    return n * A + ceil_sum(a + n, w) - ceil_sum(a, w);
-}
-
-// The row block of step `at` of a head (0 <= at < steps_before(blocks)).
+// The row block of key `at` of a head's line (0 <= at < line_of(blocks)).
 ATP_PLAN_FN int block_of(const Seq& q, int64_t at, int rows, bool causal) {
     int lo = 0, hi = q.blocks - 1;      // last block whose start is <= at
     while (lo < hi) {
         const int mid = lo + (hi - lo + 1) / 2;
-        if (steps_before(q, mid, rows, causal) <= at) lo = mid;
+        if (line_of(q, mid, rows, causal) <= at) lo = mid;
         else hi = mid - 1;
     }
     return lo;
 }
 
-// Steps of a workgroup.
+// Keys of a workgroup.
 ATP_PLAN_FN int64_t share(int64_t total, int groups, int least) {
     const int64_t per = (total + groups - 1) / groups;
-    return per > least ? per : least;
+    return whole_tiles(per > least ? per : least);
+}
+
+// The key of a unit at which a cut at `at` of its line falls: the line begins with the unit's
+// extra work, and cuts move up to whole tiles and to what the block sees (lim).
+ATP_PLAN_FN int cut_key(int64_t at, int extra, int lim, int tile) {
+    const int64_t k = at > extra ? (at - extra + tile - 1) / tile * tile : 0;
+    return (int)(k < lim ? k : lim);
+}
+
+// Keys [first, last) that a piece [p0, p1) of a unit's line reads; `ends`: p1 is the line's
+// end.  A cut that leaves nothing on one side is none: the piece there is empty and nobody
+// takes it.
+struct Piece {
+    int first, last;
+};
+ATP_PLAN_FN Piece piece_keys(int64_t p0, int64_t p1, int extra, bool ends, int lim, int tile) {
+    return Piece{cut_key(p0, extra, lim, tile), ends ? lim : cut_key(p1, extra, lim, tile)};
+}
+
+// The share that reads the last keys of a unit whose line is [u0, u1).
+ATP_PLAN_FN int64_t last_share(int64_t u0, int64_t u1, int64_t per, int extra, int lim, int tile) {
+    int64_t w = (u1 - 1) / per;
+    while (w * per > u0 && cut_key(w * per - u0, extra, lim, tile) >= lim) --w;
+    return w;
 }
 
 }  // namespace plan
