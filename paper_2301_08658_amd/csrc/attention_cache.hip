@@ -9,16 +9,21 @@
 // that is cut leaves its pieces' maxima, sums and outputs in the workspace, and
 // join_kernel adds them in order.
 //
-// Few rows (up to 32): the four waves take 32 keys of every step each, with
-// their own running maximum, sum and output, and meet only at the end of a piece:
-// no barrier stands in the key loop.  A wave's K and V tiles (8 KB each) go straight
+// Few rows (up to 32): the four waves take 32 keys of every 128 each, with their
+// own reference (a running maximum), sum and output, and meet only at the end of a
+// piece: no barrier stands in the key loop.  A wave's K and V tiles (8 KB each) go straight
 // to LDS; K's next tile is asked for as soon as the score products have read this
 // one and V's after the second products, so 8 to 16 KB per wave are under way at
-// any time, 64 to 128 KB per CU.  The time is the cache's bytes.
+// any time, 64 to 128 KB per CU.  The time is the cache's bytes: one token of each of
+// 64 sequences, 20 heads, 2.67 GB of keys and values take 450 us, 5.9 TB/s (a copy on
+// this chip moves 5.2).
 //
 // Many rows (128 per unit): the waves take 32 rows each and share double-buffered
-// tiles of 64 keys, so every fragment read from LDS feeds two products; the time is
-// the products'.
+// tiles of 64 keys, so every fragment read from LDS feeds two products.  A tile takes
+// 3500 to 4000 cycles with two workgroups on a CU, 2048 of which the products fill: the
+// chain of LDS reads, products, softmax and barrier in a wave bounds it (prompt chunks
+// of 500 to 1024 tokens, 49 GFLOP, 82 us: 600 TFLOP/s with the joining), and with several
+// row blocks per head also the keys, read once for each.
 //
 // Products (layouts as in attention.hip): a lane of S^T = K Q^T holds row lane %
 // 16 and keys 4 (lane / 16) + e of 16-key tiles, its probabilities are the right
@@ -176,13 +181,13 @@ __device__ __forceinline__ plan::Seq load_seq(const Args& a, int s) {
 
 // Every workgroup lays out the batch for itself: reading a few lengths costs less
 // than a launch that would do it once.  Up to 64 sequences: one per lane, each wave by
-// itself, nothing but registers (8.7 -> 7.0 us for one sequence's token).  More: runs of
+// itself, nothing but registers (8.7 -> 7.6 us for one sequence's token).  More: runs of
 // consecutive sequences per thread, added up through LDS.
 __device__ __forceinline__ Share find_share(const Args& a, int64_t* lds) {
     Share sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = a.batch.n_seqs;
     if (n <= 64) {
-        plan::Seq q = {0, 0, 0, 0, 0};
+        plan::Seq q = {};
         if (lane < n) q = load_seq(a, lane);
         const int64_t mine = lane < n ? seq_line(a, q) : 0;
         if (__builtin_amdgcn_ballot_w64(mine >> 26 != 0) == 0) {
@@ -197,6 +202,7 @@ __device__ __forceinline__ Share find_share(const Args& a, int64_t* lds) {
             sh.q.ctx = __builtin_amdgcn_readlane(q.ctx, sh.s);
             sh.q.keys = __builtin_amdgcn_readlane(q.keys, sh.s);
             sh.q.blocks = __builtin_amdgcn_readlane(q.blocks, sh.s);
+            sh.q.extra = a.extra;
             return sh;
         }
     }
@@ -273,7 +279,7 @@ __device__ __forceinline__ void next_seq(const Args& a, Share& sh, int64_t at) {
 
 // The workspace: a record of every share, then two slots per share.  The record
 // tells join_kernel of the unit that begins in the share and goes on behind it (last:
-// the share of its last step, -1 for no such unit).  A slot holds a piece's
+// the share of its last keys, -1 for no such unit).  A slot holds a piece's
 // results, BM rows of 128 sums, BM maxima (base 2), BM sums of weights: slot 0 for a
 // unit that began before the share, 1 for the one that goes on behind it.
 struct Record {
@@ -483,8 +489,9 @@ __device__ __forceinline__ void softmax_step(f32x4 (&sc)[N], float scale, float&
     for (int j = 0; j < N; ++j) sc[j] = p[j];
 }
 
-// Weights of a 32-key slice as the products' operand, rounded to bf16 (half a step
-// is 2^-9 of a weight, as in attention.hip; their sum is not rounded).
+// Weights of a 32-key slice as the products' operand, rounded to bf16 (by at most 2^-8 of
+// a weight, as in attention.hip; their sum is not rounded): the matrix cores take 16
+// bits, and with many rows a second product for the rest would cost a quarter.
 __device__ __forceinline__ bf16x8 round_weights(const f32x4& a, const f32x4& b) {
     return __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]),
                                             pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])});
@@ -545,7 +552,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
     }
     for (int64_t at = sh.begin; at < sh.end;) {
         const Unit u = unit_at(a, sh.q, sh.s, sh.start, at);
-        if (u.u1 <= at || u.u0 > at) break;     // as above
+        if (u.u1 <= at || u.u0 > at) break;     // lengths that changed: see next_seq
         const int lim = plan::block_keys(u.q, u.block, a.rows, causal);
         const int all = sight_of(a, u, 0, BM, lim).all;
         const int64_t upto = min(sh.end, u.u1);
@@ -666,7 +673,9 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
                     hide<2>(sees[r], g, sc[r]);
                 }
             }
-            // the products have time to spare here: the weights' second halves too
+            // the bytes bound this kernel and the products have time to spare: the weights'
+            // second halves too (2.3e-3 -> 1.7e-3 from the 64-bit result, the output's own
+            // rounding)
             bf16x8 pf[RT], pl[RT];
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
@@ -781,7 +790,10 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
 // Many rows: BM = 128, four waves of two 16-row blocks, keys in tiles of 64 that the
 // waves copy together, two buffers, one barrier per tile.  The copies of the next
 // tile are issued between the score products, a quarter (16 keys: one page) at a
-// time.
+// time.  Other shapes tried on prompt chunks (92 us then): eight waves of 256 rows on a
+// ring of four buffers, half of them half a tile behind (135); keys copied two tiles
+// ahead behind a second barrier (94); values lagging a tile behind so that their product
+// and the next weights share the time (97: 26 registers spilled).
 constexpr int kWideRows = 128;
 constexpr int WT = 64;                 // keys of a tile
 // SMALL: pages of fewer than 64 tokens; a tile's quarters are looked up one by one.
@@ -811,7 +823,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
     }
     for (int64_t at = sh.begin; at < sh.end;) {
         const Unit u = unit_at(a, sh.q, sh.s, sh.start, at);
-        if (u.u1 <= at || u.u0 > at) break;     // as above
+        if (u.u1 <= at || u.u0 > at) break;     // lengths that changed: see next_seq
         const int lim = plan::block_keys(u.q, u.block, a.rows, causal);
         const Sight sight = sight_of(a, u, 32 * wave, 32 * wave + 32, lim);
         const int64_t upto = min(sh.end, u.u1);
