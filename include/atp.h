@@ -731,7 +731,7 @@ atp_status atp_cache_release(int32_t n_pages, int32_t page_size, int32_t* refs,
  * and values of every head, are copied to page dst[i].  An entry with rows[i]
  * <= 0, an index outside the pool or src[i] == dst[i] does nothing.  A page
  * that is a destination must not appear a second time among src and dst (its
- * content is undefined then). */
+ * content is undefined then).  n is at most 2^23. */
 atp_status atp_cache_copy_pages(const atp_kv_cache* cache, int32_t n, const int32_t* src,
                                 const int32_t* dst, const int32_t* rows, void* stream);
 
@@ -749,7 +749,8 @@ atp_status atp_cache_compact(const atp_kv_cache* cache, const atp_kv_batch* batc
 
 /* Attention of the step's new tokens over the cache, which holds them already
  * (atp_qk_norm_rope_cache): softmax(q k^T / sqrt(128)) v over what each token
- * sees, in fp32 (weights rounded to bf16 for the product with v).  New token
+ * sees, in fp32 (for the product with v weights are rounded to 16 significant
+ * bits, to 8 where group * max_new is above 32).  New token
  * j of sequence s sees the ctx[s] cached tokens and, of the new ones, 0 .. j
  * (tree_mask NULL: a decode step, a chunk of a prompt) or those whose bit is
  * set in its row of tree_mask (uint64 [tokens][mask_words]; bit i % 64 of word
@@ -760,11 +761,11 @@ atp_status atp_cache_compact(const atp_kv_cache* cache, const atp_kv_batch* batc
  * q, out: bf16 [tokens, kv_heads * group * 128], no overlap.  lse (nullable):
  * fp32 [kv_heads * group][tokens], the natural log-sum-exp of each row's
  * scaled scores.  max_new: the most new tokens a sequence is expected to have;
- * it chooses the kernel's tile, not the result.  workspace: caller-owned,
+ * it chooses the kernel's tile (a sequence may have more).  workspace: caller-owned,
  * atp_attention_cache_workspace_bytes(kv_heads, group, max_new) bytes,
  * scratch.  Long contexts are split over workgroups and joined in a fixed
- * order: repeats give the same bits; another batch around a sequence can
- * change its results by fp32 rounding.
+ * order: repeats give the same bits; another batch around a sequence or
+ * another max_new can change its results by the roundings above.
  * Errors as atp_qk_norm_rope_cache; INVALID_ARGUMENT for max_new < 1,
  * mask_words < 1 with a mask, a short workspace. */
 atp_status atp_attention_cache_fwd(const atp_kv_cache* cache, const atp_kv_batch* batch,

@@ -25,6 +25,7 @@ using atp::abi::run_timed;
 constexpr int64_t kMaxTokens = 1 << 24;
 constexpr int64_t kMaxPlaces = 1 << 30;    // tokens that a table row can hold
 constexpr int32_t kMaxPool = 1 << 28;
+constexpr int32_t kMaxCopies = 1 << 23;    // workgroups of 256 threads in a row of a grid
 constexpr int32_t kMaxSeqs = 1 << 16;
 constexpr int64_t kMaxLd = 1 << 22;
 
@@ -360,7 +361,7 @@ atp_status atp_cache_copy_pages(const atp_kv_cache* cache, int32_t n, const int3
                                 const int32_t* dst, const int32_t* rows, void* stream) {
     ATP_CHECK(check_cache(cache));
     if (n < 0) return set_error(ATP_ERR_INVALID_ARGUMENT, "n %d", n);
-    if (n > kMaxPool) return set_error(ATP_ERR_UNSUPPORTED, "n %d: at most 2^28", n);
+    if (n > kMaxCopies) return set_error(ATP_ERR_UNSUPPORTED, "n %d: at most 2^23", n);
     if (n == 0) return ATP_OK;
     ATP_CHECK(check_vector(src, "src"));
     ATP_CHECK(check_vector(dst, "dst"));

@@ -200,3 +200,8 @@ def test_binding_checks_sizes_and_devices():
         atp.qk_norm_rope(rotary_dims=64)
     with pytest.raises(ValueError, match="GPU"):
         atp.qk_norm_rope(q_weight=torch.ones(128, dtype=torch.bfloat16))
+
+
+def test_copy_list_length():
+    """More entries than a grid has workgroups are refused before anything is launched."""
+    assert copy(n=(1 << 23) + 1) == UNS and copy(n=-1) == INV and copy(n=0, s=None) == OK
