@@ -19,11 +19,13 @@
 // this chip moves 5.2).
 //
 // Many rows (128 per unit): the waves take 32 rows each and share double-buffered
-// tiles of 64 keys, so every fragment read from LDS feeds two products.  A tile takes
-// 3500 to 4000 cycles with two workgroups on a CU, 2048 of which the products fill: the
-// chain of LDS reads, products, softmax and barrier in a wave bounds it (prompt chunks
-// of 500 to 1024 tokens, 49 GFLOP, 82 us: 600 TFLOP/s with the joining), and with several
-// row blocks per head also the keys, read once for each.
+// tiles of 64 keys, so every fragment read from LDS feeds two products.  Prompt chunks of
+// 500 to 1024 tokens, 49 GFLOP, take 82 us with the joining (600 TFLOP/s), 4096 tokens
+// behind 4000 860 TFLOP/s.  Two waves on a SIMD take 5900 cycles for a tile each, one wave
+// alone 3500; 1024 of a wave's are products and about 900 vector instructions.  What
+// bounds it is that these hardly overlap: left out one by one, weights, copies and second
+// product shorten a tile by 15, 21 and 20%, while more waves, fewer LDS reads per product
+// or keys that are all in L2 (trees 104 -> 97 us, chunks 82 -> 81) change little.
 //
 // Products (layouts as in attention.hip): a lane of S^T = K Q^T holds row lane %
 // 16 and keys 4 (lane / 16) + e of 16-key tiles, its probabilities are the right
@@ -793,7 +795,10 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
 // time.  Other shapes tried on prompt chunks (92 us then): eight waves of 256 rows on a
 // ring of four buffers, half of them half a tile behind (135); keys copied two tiles
 // ahead behind a second barrier (94); values lagging a tile behind so that their product
-// and the next weights share the time (97: 26 registers spilled).
+// and the next weights share the time (97: 26 registers spilled).  Beside the present 82:
+// 32-key tiles (86), also with three waves per SIMD (90), with 192 rows (96), with 256 rows
+// and one wave per SIMD (128); the row blocks apart, one's products beside the other's
+// weights (92).
 constexpr int kWideRows = 128;
 constexpr int WT = 64;                 // keys of a tile
 // SMALL: pages of fewer than 64 tokens; a tile's quarters are looked up one by one.
