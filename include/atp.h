@@ -756,8 +756,10 @@ atp_status atp_cache_compact(const atp_kv_cache* cache, const atp_kv_batch* batc
  * set in its row of tree_mask (uint64 [tokens][mask_words]; bit i % 64 of word
  * i / 64 is new token i of its sequence, itself included; tokens beyond the
  * words are not seen).  Whatever a masked or empty place holds does not reach
- * the result.  A token that sees nothing gets zeros and a log-sum-exp of
- * -inf.
+ * the result; an infinity or NaN among the values that a token sees reaches that
+ * value of its result alone (a weight below 2^-100 of the largest may count as
+ * 0, which gives NaN there).  A token that sees nothing gets zeros and a
+ * log-sum-exp of -inf.
  * q, out: bf16 [tokens, kv_heads * group * 128], no overlap.  lse (nullable):
  * fp32 [kv_heads * group][tokens], the natural log-sum-exp of each row's
  * scaled scores.  max_new: the most new tokens a sequence is expected to have;

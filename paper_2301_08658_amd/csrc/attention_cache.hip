@@ -586,13 +586,6 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
         }
         f32x4 o[RT][8];
         float mrun[RT], lrun[RT];
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            mrun[r] = -INFINITY;
-            lrun[r] = 0.f;
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt) o[r][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
 
         // the wave's tiles: 32 keys of every 128
         constexpr int STEP = TILE;
@@ -627,6 +620,20 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
                                voffs[i & 1] +
                                    (uint32_t)(((SMALL ? i & 3 : i) >> 1) * 8 * D * 2), 0u);
         };
+        // Where every row sees a whole tile, nothing looks for infinities and NaN among its
+        // values: one that stands there leaves NaN in a sum (a weight's second part, below, is
+        // zero or negative for most of them), and then the wave takes its keys of the piece once
+        // more as if each tile had a masked place.  32 or 64 additions per piece; a look at
+        // every tile would cost 64 vector instructions and 8 KB of LDS reads each.
+        bool careful = false;
+    again:
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            mrun[r] = -INFINITY;
+            lrun[r] = 0.f;
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) o[r][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
         int base = piece.first + KT * wave;
         bool more = base < piece.last;
         Tile cur;
@@ -662,8 +669,8 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
             if (next) copy_keys(nxt);
 
             // what the rows see of these 32 keys, where that is not everything
-            const bool masked =
-                base + KT > all || base + KT > lim || cur.page[0] < 0 || cur.page[P - 1] < 0;
+            const bool masked = careful || base + KT > all || base + KT > lim ||
+                                cur.page[0] < 0 || cur.page[P - 1] < 0;
             uint32_t sees[RT];
             if (masked) {
                 uint32_t there = (cur.page[0] < 0 ? 0u : 0xffffu) |
@@ -717,6 +724,17 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
             cur = nxt;
             more = next;
             base += STEP;
+        }
+        if (!careful) {
+            float all_of_it = 0.f;
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) all_of_it += o[r][dt][e];
+            careful = __builtin_amdgcn_ballot_w64(all_of_it != all_of_it) != 0;
+            if (careful) goto again;
         }
 
         // the four waves' results of this piece, row block by row block
