@@ -449,13 +449,13 @@ __device__ __forceinline__ void clear_odd(bf16x8& chunk) {
 
 // Softmax of a row's new scores (N 16-key tiles): weights exp2(scale x - m) in sc,
 // running reference m, sum l (the lane's own keys; joined at the end) and output
-// moved.  The reference is a maximum of earlier scores and stays while it does: the
-// weights are formed first, and only where a lane's sum leaves kRoom (a weight above
-// 2^10: a score far above all before it; or a row without a reference yet) does the
-// wave look for maxima, move O and l and form them again.  O / l and m + log2 l do
-// not depend on the reference.  A maximum in every step took a fifth of the
-// kernel's vector instructions.
-constexpr float kRoom = 1024.f;
+// moved.  The reference lies kRise above a maximum of earlier scores and stays while it does:
+// the weights are formed first, and only where a lane's sum leaves 1 (a score kRise above
+// all before it; or a row without a reference yet) does the wave look for maxima, move O and
+// l and form them again.  O / l and m + log2 l do not depend on the reference.  A maximum in
+// every step took a fifth of the kernel's vector instructions.  No weight is above 1, so the
+// sums hold whatever values the sums of a softmax with its true maximum would.
+constexpr float kRise = 10.f;
 template <int N>
 __device__ __forceinline__ void softmax_step(f32x4 (&sc)[N], float scale, float& m, float& l,
                                              f32x4 (&o)[8]) {
@@ -473,12 +473,12 @@ __device__ __forceinline__ void softmax_step(f32x4 (&sc)[N], float scale, float&
             }
     };
     weights();
-    if (__builtin_amdgcn_ballot_w64(!(rs <= kRoom) || m == -INFINITY) != 0) {
+    if (__builtin_amdgcn_ballot_w64(!(rs <= 1.f) || m == -INFINITY) != 0) {
         float mx = -INFINITY;
 #pragma unroll
         for (int j = 0; j < N; ++j)
             mx = fmaxf(mx, fmaxf(fmaxf(sc[j][0], sc[j][1]), fmaxf(sc[j][2], sc[j][3])));
-        const float mnew = fmaxf(m, row_max4(mx) * scale);
+        const float mnew = fmaxf(m, __builtin_fmaf(row_max4(mx), scale, kRise));
         const float alpha = weight_of(m, mnew);
         l *= alpha;
 #pragma unroll
@@ -516,7 +516,8 @@ __device__ __forceinline__ float inverse_sum(float l) {   // 0 for a row that sa
     return l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);       // NaN stays
 }
 __device__ __forceinline__ float log_sum(float m, float l) {
-    return l == 0.f ? -INFINITY : kLn2 * m + logf(l);
+    constexpr float kUp = 1 << (int)kRise;      // l is about 1 / kUp: both terms small again
+    return l == 0.f ? -INFINITY : kLn2 * (m - kRise) + logf(l * kUp);
 }
 
 // SMALL: pages of 16 tokens, so that a wave's tile of 32 keys spans two.

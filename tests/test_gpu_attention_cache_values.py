@@ -1,5 +1,5 @@
 """Attention over the paged cache where the values leave the ordinary range: infinities and
-NaN that every row of a tile sees."""
+NaN that every row of a tile sees, and finite values near the end of the range."""
 import math
 
 import pytest
@@ -73,3 +73,23 @@ def test_infinities_beside_drafts_that_do_not_see_them():
         put(c, 0, 153, 1, 0, 2, -math.inf)
         put(c, 0, 152, 1, 0, 3, math.nan)
         c.check()
+
+
+@pytest.mark.parametrize("new,group", UNITS)
+def test_values_near_the_end_of_the_range(new, group):
+    """Finite values whose sum with weights of at most 1 fits give finite results, also
+    where single keys behind the first 128 have scores of 6.9 above all others, 987 times
+    their weight: the twelve of them sum values of 1e35 to 1.2e36, and to 1.2e39 if the
+    first keys' weights were 1.  Units of few rows are cut every 128 keys unless there are
+    many of them."""
+    seqs = 600 if new[0] * group <= 32 else 1
+    c = Case([290] * seqs, new * seqs, 1, group, 32, seed=25)
+    c.q[:, :] = 1.0
+    k, v = c.pool[:, 0], c.pool[:, 1]
+    c.pool[:, 0] = torch.where(torch.isnan(k), k, torch.zeros_like(k))
+    for key in range(128, 290):
+        if key % 64 in (0, 4, 8, 12):
+            c.pool[c.table[:, key // 32].long(), 0, 0, key % 32] = 39 / 64      # x sqrt(128)
+    c.pool[:, 1] = torch.where(torch.isnan(v), v, ((1 + v.float() / 16) * 1e35).to(BF))
+    out, _ = c.check()
+    assert torch.isfinite(out.float()).all()
