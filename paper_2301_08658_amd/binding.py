@@ -785,6 +785,8 @@ def _list(t, n: int, name: str, dev: int, dtype=torch.int32):
 
 
 def _bytes(workspace, dev: int):
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace: needs contiguous memory")    # nbytes would count other bytes
     if workspace is not None and workspace.get_device() == dev:
         return workspace.data_ptr(), workspace.nbytes
     return _workspace(workspace)
