@@ -26,13 +26,15 @@ constexpr int64_t kFar = 1 << 30;    // a rank that no pool holds (at most 2^28 
 
 __device__ __forceinline__ bool names_page(int32_t e, int n_pages) { return e >= 0 && e < n_pages; }
 
-// Exclusive prefix of v over the workgroup's threads, and the total.
-__device__ __forceinline__ int64_t block_prefix(int v, int* waves, int64_t* total) {
+// Exclusive prefix of v over the workgroup's threads, and the total.  A wave's sum is below
+// 2^32 whatever the lists hold: a sequence wants at most 2^26 pages, and 32-bit lists cannot
+// give five neighbours the 2^30 new tokens each that it takes.
+__device__ __forceinline__ int64_t block_prefix(uint32_t v, uint32_t* waves, int64_t* total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int inc = v;
+    uint32_t inc = v;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const int up = __shfl_up(inc, d);
+        const uint32_t up = __shfl_up(inc, d);
         if (lane >= d) inc += up;
     }
     if (lane == 63) waves[wave] = inc;
@@ -45,7 +47,7 @@ __device__ __forceinline__ int64_t block_prefix(int v, int* waves, int64_t* tota
     }
     __syncthreads();
     *total = all;
-    return before + inc - v;
+    return before + (inc - v);
 }
 
 struct Span {      // table columns [lo, hi) that a sequence's new tokens go to
@@ -71,7 +73,7 @@ __global__ __launch_bounds__(kPlan) void reserve_kernel(int n_pages, int shift, 
                                                         BatchView b, int32_t* missing, int32_t* src,
                                                         int32_t* dst, int32_t* rows, int32_t* want,
                                                         int32_t* free_list) {
-    __shared__ int waves[kPlanWaves];
+    __shared__ uint32_t waves[kPlanWaves];
     __shared__ int given;
     const int tid = threadIdx.x, lane = tid & 63;
     auto wanted = [&](int32_t e) { return !names_page(e, n_pages) || refs[e] > 1; };
