@@ -48,12 +48,8 @@ constexpr int D = kHead;
 constexpr int NWAVE = 4;
 constexpr int NTHR = 64 * NWAVE;
 constexpr int KT = 32;                 // keys of a wave's tile
-constexpr int kGroups = 512;           // shares: two workgroups per CU on 256 CUs
-constexpr int kLeast = plan::kTile;    // fewest keys of a share
-// What a unit costs beside its keys, in keys: 32 sequences of 4 drafts 57 us without it, 44
-// so (64: 44, 256: 42.5), 300 short contexts' tokens 67 and 53 (57, 54); with 128 rows,
-// trees 122 without it, 105 so (128: 110, 448: 106), prompt chunks 95 and 80.5 (86, 80.5).
-constexpr int kExtra = 128, kWideExtra = 320;
+using plan::kGroups;
+using plan::kLeast;
 constexpr int kXcds = 8;
 constexpr float kLn2 = 0.69314718055994530942f;
 
@@ -523,7 +519,8 @@ __device__ __forceinline__ float log_sum(float m, float l) {
 // SMALL: pages of 16 tokens, so that a wave's tile of 32 keys spans two.
 template <int RT, bool SMALL>
 __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
-    constexpr int BM = 16 * RT, TILE = NWAVE * KT;
+    constexpr int BM = 16 * RT, TILE = plan::kFewTile;
+    static_assert(TILE == NWAVE * KT, "a tile of every wave");
     constexpr int kRed = D + 4;      // padded row of the merge
     __shared__ __attribute__((aligned(16))) uint16_t tiles[NWAVE][2][KT * D];
     __shared__ float wm[NWAVE][BM], wl[NWAVE][BM];
@@ -819,7 +816,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
 // and one wave per SIMD (128); the row blocks apart, one's products beside the other's
 // weights (92).
 constexpr int kWideRows = 128;
-constexpr int WT = 64;                 // keys of a tile
+constexpr int WT = plan::kWideTile;    // keys of a tile
 // SMALL: pages of fewer than 64 tokens; a tile's quarters are looked up one by one.
 template <bool SMALL>
 __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
@@ -1175,7 +1172,7 @@ hipError_t launch_cache_attention(const CacheAttentionProblem& p, hipStream_t s)
     a.tokens = (int)p.tokens;
     a.group = p.group;
     a.rows = bm / p.group;
-    a.extra = bm == kWideRows ? kWideExtra : kExtra;
+    a.extra = bm == kWideRows ? plan::kWideExtra : plan::kFewExtra;
     a.cap = (int64_t)p.batch.max_pages << p.cache.page_shift;
     a.scale_log2 = 1.4426950408889634f / sqrtf((float)D);
     // no batch of these sizes has more shares than this

@@ -20,6 +20,15 @@ namespace atp {
 namespace plan {
 
 constexpr int kTile = 128;     // keys that shares are cut at, where a unit's line is whole tiles
+constexpr int kGroups = 512;   // shares: two workgroups per CU on 256 CUs
+constexpr int kLeast = kTile;  // fewest keys of a share
+// Units of up to 32 rows and of 128: the keys of a tile, and what a unit costs beside its
+// keys, in keys.  Without it 300 short contexts' tokens (8 heads, 10 to 200 keys) take 55 us,
+// 51 so (64: 52, 256: 51), 32 sequences of 4 drafts 53 and 52 (52, 49), 16 sequences' 24 rows
+// 81 and 79 (83, 81); with 128 rows 24 drafted trees 131 and 116 (128: 124, 448: 116), prompt
+// chunks 99 and 87 (94, 88), 128 rows over 131000 keys 183 and 131 (131, 127).
+constexpr int kFewTile = 128, kFewExtra = 128;
+constexpr int kWideTile = 64, kWideExtra = 320;
 
 ATP_PLAN_FN int64_t whole_tiles(int64_t keys) { return (keys + kTile - 1) / kTile * kTile; }
 
