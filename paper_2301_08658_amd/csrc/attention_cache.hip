@@ -524,6 +524,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
     constexpr int kRed = D + 4;      // padded row of the merge
     __shared__ __attribute__((aligned(16))) uint16_t tiles[NWAVE][2][KT * D];
     __shared__ float wm[NWAVE][BM], wl[NWAVE][BM];
+    __shared__ int wnan[NWAVE];
     __shared__ int64_t lds[NWAVE + 2];
     const int lane = threadIdx.x & 63, g = lane >> 4, l16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -550,11 +551,12 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
         const int r = 4 * g + (l16 >> 2), col = 16 * dt + 4 * (l16 & 3);
         vread[dt] = r * D + vpos(r, col >> 3) * 8 + (col & 7);
     }
+    bool careful = false;            // every tile is taken as if it had a masked place
     for (int64_t at = sh.begin; at < sh.end;) {
         const Unit u = unit_at(a, sh.q, sh.s, sh.start, at);
         if (u.u1 <= at || u.u0 > at) break;     // lengths that changed: see next_seq
         const int lim = plan::block_keys(u.q, u.block, a.rows, causal);
-        const int all = sight_of(a, u, 0, BM, lim).all;
+        const int all = careful ? 0 : sight_of(a, u, 0, BM, lim).all;
         const int64_t upto = min(sh.end, u.u1);
         const plan::Piece piece =
             plan::piece_keys(at - u.u0, upto - u.u0, a.extra, upto == u.u1, lim, TILE);
@@ -584,6 +586,13 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
         }
         f32x4 o[RT][8];
         float mrun[RT], lrun[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            mrun[r] = -INFINITY;
+            lrun[r] = 0.f;
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) o[r][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
 
         // the wave's tiles: 32 keys of every 128
         constexpr int STEP = TILE;
@@ -618,20 +627,6 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
                                voffs[i & 1] +
                                    (uint32_t)(((SMALL ? i & 3 : i) >> 1) * 8 * D * 2), 0u);
         };
-        // Where every row sees a whole tile, nothing looks for infinities and NaN among its
-        // values: one that stands there leaves NaN in a sum (a weight's second part, below, is
-        // zero or negative for most of them), and then the wave takes its keys of the piece once
-        // more as if each tile had a masked place.  32 or 64 additions per piece; a look at
-        // every tile would cost 64 vector instructions and 8 KB of LDS reads each.
-        bool careful = false;
-    again:
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            mrun[r] = -INFINITY;
-            lrun[r] = 0.f;
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt) o[r][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
         int base = piece.first + KT * wave;
         bool more = base < piece.last;
         Tile cur;
@@ -667,8 +662,8 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
             if (next) copy_keys(nxt);
 
             // what the rows see of these 32 keys, where that is not everything
-            const bool masked = careful || base + KT > all || base + KT > lim ||
-                                cur.page[0] < 0 || cur.page[P - 1] < 0;
+            const bool masked =
+                base + KT > all || base + KT > lim || cur.page[0] < 0 || cur.page[P - 1] < 0;
             uint32_t sees[RT];
             if (masked) {
                 uint32_t there = (cur.page[0] < 0 ? 0u : 0xffffu) |
@@ -723,17 +718,6 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
             more = next;
             base += STEP;
         }
-        if (!careful) {
-            float all_of_it = 0.f;
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int dt = 0; dt < 8; ++dt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) all_of_it += o[r][dt][e];
-            careful = __builtin_amdgcn_ballot_w64(all_of_it != all_of_it) != 0;
-            if (careful) goto again;
-        }
 
         // the four waves' results of this piece, row block by row block
 #pragma unroll
@@ -744,12 +728,32 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
                 wl[wave][16 * r + l16] = lrun[r];
             }
         }
+        // Where every row sees a whole tile, nothing looks for infinities and NaN among its
+        // values: one that stands there leaves NaN in a wave's sums (a weight's second part,
+        // above, is zero or negative for most of them), and then the piece is taken once more
+        // with the values of every tile looked through.  32 or 64 additions per piece; looking
+        // at every tile at once would cost 64 vector instructions and 8 KB of LDS reads each.
+        f32x4 of4 = o[0][0];
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int dt = r == 0; dt < 8; ++dt) of4 += o[r][dt];
+        const float of_all = (of4[0] + of4[1]) + (of4[2] + of4[3]);
+        const bool nan = __builtin_amdgcn_ballot_w64(of_all != of_all) != 0;
+        if (lane == 0) wnan[wave] = nan;
         const bool begins = piece.first == 0, whole = begins && piece.last == lim;
         if (begins && !whole) record = record_of(a, u, sh.per, lim, TILE);
         float* slot = slot_of<BM>(a.ws, sh.index, begins ? 1 : 0);
         float* red = reinterpret_cast<float*>(&tiles[wave][0][0]);     // 16 rows of kRed
         const int orow = threadIdx.x >> 4, ocol = (threadIdx.x & 15) * 8;
         __syncthreads();
+        if (!careful &&
+            __builtin_amdgcn_readfirstlane(wnan[0] | wnan[1] | wnan[2] | wnan[3]) != 0) {
+            careful = true;
+            __syncthreads();                 // wm, wl and wnan have been read
+            continue;
+        }
+        careful = false;
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             float top = -INFINITY;
