@@ -581,6 +581,10 @@ atp_status atp_attention_bwd_noalloc(const atp_mesh* mesh, int32_t block_mode, i
  * host cannot see is checked by the kernels: a table entry outside
  * [0, n_pages) holds no tokens, rows and columns stay inside the sizes given
  * here, and nothing is read or written elsewhere.
+ *
+ * Buffers overlap when their bytes from the first element of the first row to
+ * the last of the last do, with what lies between the rows: two column runs of
+ * one buffer count as overlapping.
  * ------------------------------------------------------------------------ */
 #define ATP_MAX_QUERY_GROUP 64
 #define ATP_MAX_FORKS 4096
@@ -695,10 +699,14 @@ atp_status atp_qk_norm_rope_cache(const atp_kv_cache* cache, const atp_kv_batch*
  * ctx[s] % page_size the tokens (-1, -1, 0 for no copy), for
  * atp_cache_copy_pages on every layer before the next call that gives pages
  * out.  Pages are given in ascending order to the sequences in ascending
- * order.  A sequence gets all it needs or nothing: missing[s] is 0, or how
- * many pages it lacks when the pool (after the sequences before it) or the
- * table's columns cannot hold it; such a sequence changes nothing, and the
- * sequences behind it that need pages get none either if it was the pool.
+ * order.  What is shared is decided by the counts at the call's start: all
+ * holders of a page that write to it get a copy, the last one too, and the page
+ * falls free.  A sequence gets all it needs or nothing: missing[s] is 0, or how
+ * many pages it needs (all of them, free ones counted) when the pool (after the
+ * sequences before it) or the table's columns cannot hold it; such a sequence
+ * changes nothing, and the sequences behind it that need pages get none either
+ * if it was the pool.  The time grows with the pages in front of the last free
+ * one that is given.
  * workspace: atp_cache_workspace_bytes(n_pages, n_seqs) bytes, scratch.
  * missing, copy_src, copy_dst, copy_rows: int32 [n_seqs], written. */
 atp_status atp_cache_reserve(int32_t n_pages, int32_t page_size, int32_t* refs,

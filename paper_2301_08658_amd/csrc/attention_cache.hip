@@ -260,8 +260,8 @@ __device__ __forceinline__ Unit unit_at(const Args& a, const plan::Seq& q, int s
     return u;
 }
 
-// Moves a share on to the sequence of key `at` (sequences without new tokens have
-// none).
+// Moves a share on to the sequence of key `at`.  Sequences without new tokens have
+// none; they are stepped over one by one, a dependent trip to memory each.
 __device__ __forceinline__ void next_seq(const Args& a, Share& sh, int64_t at) {
     const int64_t line = uniform(seq_line(a, sh.q));
     if (at < sh.start + line) return;
@@ -931,10 +931,12 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int r = 0; r < RB; ++r) sc[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-            // Fragments are read one slice of the head dimension ahead of their
-            // products.  The next tile's copies go into the other buffer, which was last
-            // read before the last barrier; behind the piece's end they find no page
-            // and fill zeros, which costs less than branches around them.
+            // Fragments are asked for one slice of the head dimension ahead of their
+            // products; as built, slices 0 and 1 are read so, and 2 and 3 two fragments at a
+            // time, because no read passes a copy issued before it.  The next tile's copies
+            // go into the other buffer, which was last read before the last barrier; behind
+            // the piece's end they find no page and fill zeros, which costs less than
+            // branches around them.
             bf16x8 kf[2][4];
             auto read = [&](int ks) {
 #pragma unroll
@@ -1063,7 +1065,9 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
 // for every half wave: it takes a row's pieces by itself (66 tokens of two sequences, 25
 // pieces per unit of 126 rows: 39 us with the attention, 87 where the workgroup took the
 // rows one by one).  Many pieces of few rows (a long context): the workgroup takes its R
-// rows one by one, its half waves every H-th piece each.
+// rows one by one, its half waves every H-th piece each.  128-row units never do: one unit
+// over 131000 keys (8 drafts of 16 heads) is cut into some 500 pieces, each half wave adds its
+// row's alone, and the joining takes 109 us, the attention 27.
 constexpr int kManyPieces = 16;
 struct Joined {
     float m, l;

@@ -3,8 +3,10 @@
 // tables and reference counts whose results do not depend on the order in which
 // threads run: pages are handed out by rank (free pages in ascending order
 // to the wanted places in ascending order), counts change by additions.  It is
-// bound by a few dependent trips to memory, not by bandwidth; copying and
-// compacting move 16 bytes per lane and are bound by the rows in flight.
+// bound by dependent trips to memory, not by bandwidth: a few of them, and in
+// reserving one more, with two barriers, per 4096 pages in front of the last free
+// one that it gives (n_pages / 4096 of them in a pool that is nearly full).
+// Copying and compacting move 16 bytes per lane and are bound by the rows in flight.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
