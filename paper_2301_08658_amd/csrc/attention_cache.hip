@@ -20,7 +20,7 @@
 //
 // Many rows (128 per unit): the waves take 32 rows each and share double-buffered
 // tiles of 64 keys, so every fragment read from LDS feeds two products.  Prompt chunks of
-// 500 to 1024 tokens, 49 GFLOP, take 82 us with the joining (600 TFLOP/s), 4096 tokens
+// 500 to 1024 tokens, 49 GFLOP, take 81 us with the joining (604 TFLOP/s), 4096 tokens
 // behind 4000 860 TFLOP/s.  Two waves on a SIMD take 5900 cycles for a tile each, one wave
 // alone 3500; 1024 of a wave's are products and about 900 vector instructions.  What
 // bounds it is that these hardly overlap: left out one by one, weights, copies and second
