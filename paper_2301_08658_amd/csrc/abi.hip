@@ -43,12 +43,6 @@ atp_status hip_fail(hipError_t e, const char* what) {
     return set_error(ATP_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
 }
 
-#define ATP_CHECK(expr)                                   \
-    do {                                                  \
-        atp_status _s = (expr);                           \
-        if (_s != ATP_OK) return _s;                      \
-    } while (0)
-
 #define HIP_CHECK(expr, what)                             \
     do {                                                  \
         hipError_t _e = (expr);                           \

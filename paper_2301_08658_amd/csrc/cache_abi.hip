@@ -11,57 +11,13 @@
 
 namespace {
 
+using namespace atp::abi;
 using atp::set_error;
-using atp::abi::check_matrix;
-using atp::abi::check_vector;
-using atp::abi::run_timed;
 
-#define ATP_CHECK(expr)                                   \
-    do {                                                  \
-        atp_status _s = (expr);                           \
-        if (_s != ATP_OK) return _s;                      \
-    } while (0)
-
-constexpr int64_t kMaxTokens = 1 << 24;
 constexpr int64_t kMaxPlaces = 1 << 30;    // tokens that a table row can hold
 constexpr int32_t kMaxPool = 1 << 28;
 constexpr int32_t kMaxCopies = 1 << 23;    // workgroups of 256 threads in a row of a grid
 constexpr int32_t kMaxSeqs = 1 << 16;
-constexpr int64_t kMaxLd = 1 << 22;
-
-// Bytes [0, extent) that a matrix of these rows takes from its first element.
-int64_t extent(int64_t rows, int64_t ld, int64_t cols) {
-    return rows > 0 ? ((rows - 1) * ld + cols) * 2 : 0;
-}
-bool share_bytes(const void* a, int64_t na, const void* b, int64_t nb) {
-    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
-    return na > 0 && nb > 0 && a0 < b0 + (uintptr_t)nb && b0 < a0 + (uintptr_t)na;
-}
-
-atp_status check_heads(int64_t kv_heads, int32_t group) {
-    if (kv_heads < 1 || group < 1)
-        return set_error(ATP_ERR_INVALID_ARGUMENT, "kv_heads %lld and group %d must be positive",
-                         (long long)kv_heads, group);
-    if (group > ATP_MAX_QUERY_GROUP)
-        return set_error(ATP_ERR_UNSUPPORTED, "group %d: at most %d query heads per key head",
-                         group, ATP_MAX_QUERY_GROUP);
-    if (kv_heads * (group + 2) * atp::kHead > kMaxLd)
-        return set_error(ATP_ERR_UNSUPPORTED, "%lld heads of group %d: rows above 4M elements",
-                         (long long)kv_heads, group);
-    return ATP_OK;
-}
-
-atp_status check_tokens(int64_t tokens) {
-    if (tokens < 0) return set_error(ATP_ERR_INVALID_ARGUMENT, "negative number of tokens");
-    if (tokens > kMaxTokens)
-        return set_error(ATP_ERR_UNSUPPORTED, "%lld tokens: at most 2^24", (long long)tokens);
-    return ATP_OK;
-}
-
-// Aligned like every vector; NULL allowed.
-atp_status check_optional(const void* p, const char* name) {
-    return p ? check_vector(p, name) : ATP_OK;
-}
 
 atp_status check_params(const atp_qk_norm_rope* p) {
     if (!p) return set_error(ATP_ERR_INVALID_ARGUMENT, "params is NULL");
@@ -153,18 +109,6 @@ atp::CacheView view(const atp_kv_cache* c) {
 atp::BatchView view(const atp_kv_batch* b) {
     return atp::BatchView{b->table, b->ld_table, b->max_pages, b->n_seqs, b->ctx, b->cu_new};
 }
-
-atp_status check_workspace(const void* ws, size_t have, size_t need) {
-    if (need == 0) return ATP_OK;
-    ATP_CHECK(check_vector(ws, "workspace"));
-    if (have < need)
-        return set_error(ATP_ERR_INVALID_ARGUMENT, "workspace of %zu bytes: needs %zu", have, need);
-    return ATP_OK;
-}
-
-const uint16_t* bits(const void* p) { return static_cast<const uint16_t*>(p); }
-uint16_t* bits(void* p) { return static_cast<uint16_t*>(p); }
-hipStream_t stream_of(void* s) { return static_cast<hipStream_t>(s); }
 
 // A training call's sizes: rows and row width of its blocks.
 atp_status check_block(int64_t batch, int64_t seq, int32_t kv_heads, int32_t group, int64_t* T,
