@@ -786,6 +786,199 @@ atp_status atp_attention_cache_fwd(const atp_kv_cache* cache, const atp_kv_batch
 /* 0 for sizes below 1 or a group above ATP_MAX_QUERY_GROUP. */
 size_t atp_attention_cache_workspace_bytes(int32_t kv_heads, int32_t group, int32_t max_new);
 
+/* ------------------------------------------------------------------------
+ * Around the layers, for training on packed documents: the embedding of the
+ * tokens, layer norms, the attention within documents, and the norm and
+ * clipping of the gradients.
+ *
+ * Tables of a group's buffers (stats, sums) are host arrays of red_size device
+ * pointers, as the partial tables are: this device's entry is written by its
+ * own call before, the others hold the peers' data.  They are added in group
+ * order, so every member gets the same bits.  Nothing is added by atomics:
+ * repeats give the same bits.
+ * ------------------------------------------------------------------------ */
+
+/* Embedding on this device's rows [vocab_off, vocab_off + vocab_loc) of the
+ * vocabulary and `cols` of its columns: Y = X W with one-hot rows X, W
+ * row-first (Sec. 3.2), so where the vocabulary lies on several devices out is
+ * Partial(SUM) over them (atp_chunked_partial_reduce):
+ *   out[t, :] = scale * table[ids[t] - vocab_off, :], formed in fp32 and rounded
+ *   once; zeros for a token outside this device's rows.
+ * ids: int32 [tokens], any value.  table: bf16 [vocab_loc, cols].  out: fp32 or
+ * bf16 [tokens, cols].
+ * Errors: INVALID_ARGUMENT for negative sizes, vocab_loc or cols < 1, a negative
+ * vocab_off, a non-finite scale, NULL buffers, out sharing memory with table;
+ * UNSUPPORTED for more than 2^24 tokens or rows, cols not a multiple of 8,
+ * misalignment. */
+atp_status atp_embedding_fwd(int64_t tokens, const int32_t* ids, int64_t vocab_loc,
+                             int64_t vocab_off, int64_t cols, const void* table, int64_t ld_table,
+                             float scale, void* out, int32_t out_dtype, int64_t ld_out,
+                             void* stream);
+
+/* Gradient of the table (Sec. 4.2, dW = X^T dY):
+ *   dtable[v, :] = scale * sum over t with ids[t] = vocab_off + v of dy[t, :],
+ * the sum in fp32 over ascending t, in pieces that depend on `tokens` and the ids
+ * alone.  dy: bf16 [tokens, cols].  dtable: fp32 [vocab_loc, cols]; accumulate 0:
+ * every row is written (zeros for rows without tokens); 1: the sums are added to
+ * it and rows without tokens are not touched (a table that is the output
+ * layer's weight too).  workspace: atp_embedding_workspace_bytes() bytes,
+ * scratch.  Errors as atp_embedding_fwd; INVALID_ARGUMENT for another accumulate,
+ * a short workspace, dtable sharing memory with dy. */
+atp_status atp_embedding_bwd(int64_t tokens, const int32_t* ids, int64_t vocab_loc,
+                             int64_t vocab_off, int64_t cols, const void* dy, int64_t ld_dy,
+                             float scale, float* dtable, int64_t ld_dtable, int32_t accumulate,
+                             void* workspace, size_t ws_bytes, void* stream);
+/* 0 for sizes that the call refuses (and for 0 tokens). */
+size_t atp_embedding_workspace_bytes(int64_t tokens, int64_t vocab_loc, int64_t cols);
+
+/* Layer norm of rows: y = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) o weight
+ * + bias.  weight, bias: bf16 [cols], this device's columns, nullable (ones,
+ * zeros). */
+typedef struct {
+    const void* weight;
+    const void* bias;
+    float eps;
+} atp_layer_norm;
+
+/* The norm of x (atp_dtype `dtype`, [tokens, cols], the residual stream), or with
+ * add (bf16 [tokens, cols], a linear's reduced output) of x_out = x + add, which is
+ * formed in fp32, rounded to `dtype` and stored; the norm is that of the stored
+ * values.  x_out may be x itself (same pointer and ld).  y: bf16 [tokens, cols].
+ * mean, rstd: fp32 [tokens], written for the backward.
+ * Rows whose columns lie on several devices (h / d2 or h / d1 columns each, all the
+ * same number): red_size devices, `cols` the local columns, stats the table of their
+ * statistics (fp32 [tokens][2]: mean and sum of centred squares of the local
+ * columns), each written by atp_layer_norm_stats, which also forms the sum: add
+ * and x_out are then NULL and x is the stored sum.  red_size 1 and stats NULL:
+ * whole rows, one call.
+ * Statistics in fp32, of values centred first.  An infinity or NaN stays in its row.
+ * Errors: INVALID_ARGUMENT for negative sizes, cols < 1, a bad dtype, a negative or
+ * non-finite eps, NULL buffers, add without x_out or with stats, buffers that
+ * overlap otherwise than above, red_size < 1; UNSUPPORTED for more than 2^24
+ * tokens or 32768 columns, cols not a multiple of 8, misalignment, red_size above
+ * ATP_MAX_GROUP. */
+atp_status atp_layer_norm_fwd(int64_t tokens, int64_t cols, int32_t dtype,
+                              const atp_layer_norm* norm, const void* x, int64_t ldx,
+                              const void* add, int64_t ld_add, void* x_out, int64_t ld_xout,
+                              int32_t red_size, const float* const* stats, void* y, int64_t ld_y,
+                              float* mean, float* rstd, void* stream);
+atp_status atp_layer_norm_stats(int64_t tokens, int64_t cols, int32_t dtype, const void* x,
+                                int64_t ldx, const void* add, int64_t ld_add, void* x_out,
+                                int64_t ld_xout, float* stats, void* stream);
+
+/* Gradient of atp_layer_norm_fwd.  x: the normed values (x, or x_out where there was an
+ * add); mean, rstd: the forward's; dy: bf16 gradient of y.  With xh = (x - mean) rstd
+ * and g = weight o dy, over the whole row:
+ *   dx = rstd (g - mean(g) - xh mean(g o xh)) + d_res,
+ *   dweight = sum over rows of dy o xh,  dbias = sum over rows of dy.
+ * d_res: the gradient that reaches x_out past the norm (`dtype`, nullable).  dx:
+ * `dtype`, may be d_res itself (same pointer and ld); it is the gradient of x and of
+ * add.  d_add (nullable): dx rounded to bf16 from fp32, for the linear that add came
+ * from.  dweight, dbias: fp32 [cols], nullable; they need a workspace of
+ * atp_layer_norm_workspace_bytes(tokens, cols) bytes.
+ * Rows on several devices: sums is the table of the devices' two row sums (fp32
+ * [tokens][2]: g and g o xh over the local columns), each written by
+ * atp_layer_norm_bwd_sums.  Errors as atp_layer_norm_fwd; INVALID_ARGUMENT for a
+ * short workspace. */
+atp_status atp_layer_norm_bwd(int64_t tokens, int64_t cols, int32_t dtype,
+                              const atp_layer_norm* norm, const void* x, int64_t ldx,
+                              const float* mean, const float* rstd, const void* dy, int64_t ld_dy,
+                              const void* d_res, int64_t ld_dres, int32_t red_size,
+                              const float* const* sums, void* dx, int64_t ld_dx, void* d_add,
+                              int64_t ld_dadd, float* dweight, float* dbias, void* workspace,
+                              size_t ws_bytes, void* stream);
+atp_status atp_layer_norm_bwd_sums(int64_t tokens, int64_t cols, int32_t dtype,
+                                   const atp_layer_norm* norm, const void* x, int64_t ldx,
+                                   const float* mean, const float* rstd, const void* dy,
+                                   int64_t ld_dy, float* sums, void* stream);
+/* 0 for sizes that the call refuses (and for 0 tokens). */
+size_t atp_layer_norm_workspace_bytes(int64_t tokens, int64_t cols);
+
+/* Documents of packed rows.  Rows [cu_docs[d], cu_docs[d + 1]) are document d (int32
+ * [n_docs + 1], ascending, device memory; a document may be empty); rows outside
+ * all documents are padding, neither read nor written.  Row i of a document of n
+ * rows sees its rows j <= i, and the first prefix[d] rows (int32 [n_docs], nullable;
+ * cut to [0, n]).  Scores: x = q . k / sqrt(128), with cap > 0 cap * tanh(x / cap), then
+ * minus slopes[head] * |i - j| (fp32 [kv_heads * group], nullable; constants: they
+ * get no gradient).  At most 65536 documents.  Lists that do not ascend or leave
+ * the rows give undefined results, but no access outside the buffers. */
+typedef struct {
+    const int32_t* cu_docs;
+    const int32_t* prefix;
+    const float* slopes;
+    int32_t n_docs;
+    float cap;
+} atp_attention_docs;
+
+/* Attention of the device's run of heads within documents, for training.  qkv: bf16
+ * [tokens, kv_heads * (group + 2) * 128] in the head layout of
+ * atp_qk_norm_rope_fwd (what it writes).  out: bf16 [tokens, kv_heads * group *
+ * 128]; lse: fp32 [kv_heads * group][tokens], the natural log-sum-exp of each row's
+ * scores.  Scores, softmax and sums in fp32; weights are rounded to bf16 for the
+ * product with v.  Whatever other documents, padding or, in the forward, rows that a
+ * row does not see hold does not reach its result.
+ * Errors: INVALID_ARGUMENT for negative sizes, kv_heads or group < 1, NULL buffers,
+ * a negative or non-finite cap, overlap; UNSUPPORTED for more than 2^24 tokens, the
+ * limits above, 2^31 tiles of 64 rows and heads, misalignment. */
+atp_status atp_attention_docs_fwd(int64_t tokens, int32_t kv_heads, int32_t group,
+                                  const atp_attention_docs* docs, const void* qkv, int64_t ld_qkv,
+                                  void* out, int64_t ld_out, float* lse, void* stream);
+
+/* Gradient of atp_attention_docs_fwd: out and lse are the forward's, d_out (bf16) the
+ * gradient of out, d_qkv (bf16) receives dq, dk, dv of the documents' rows in qkv's
+ * layout and must not overlap qkv, out or d_out.  dk and dv are summed in fp32 over the
+ * group's query heads.  An infinity or NaN in a document may reach all gradients of that
+ * document, and no other.  workspace: atp_attention_docs_workspace_bytes() bytes,
+ * scratch.  Errors as atp_attention_docs_fwd; INVALID_ARGUMENT for a short
+ * workspace. */
+atp_status atp_attention_docs_bwd(int64_t tokens, int32_t kv_heads, int32_t group,
+                                  const atp_attention_docs* docs, const void* qkv, int64_t ld_qkv,
+                                  const void* out, int64_t ld_out, const float* lse,
+                                  const void* d_out, int64_t ld_dout, void* d_qkv, int64_t ld_dqkv,
+                                  void* workspace, size_t ws_bytes, void* stream);
+/* 0 for sizes that the call refuses (and for 0 tokens). */
+size_t atp_attention_docs_workspace_bytes(int64_t tokens, int32_t kv_heads, int32_t group);
+
+/* One gradient: src [rows, cols], fp32 or bf16 (ld_src elements between rows; for one
+ * row, or rows without gaps, cols and ld may be any number, else leading dimensions
+ * are multiples of 8), and where its clipped values go: dst, of either type, or src
+ * itself. */
+typedef struct {
+    const void* src;
+    void* dst;
+    int64_t rows, cols, ld_src, ld_dst;
+    int32_t src_dtype, dst_dtype;
+} atp_grad;
+
+/* *sum = sum of the squares of all values of n gradients, in 64 bits and a fixed
+ * order (device memory, 8-byte aligned, written; 0 for none).  dst is not looked
+ * at.  Where a gradient is held by several devices, list it on one of them.
+ * grads is read during the call only.  workspace:
+ * atp_grad_workspace_bytes(n, grads) bytes, scratch.
+ * Errors: INVALID_ARGUMENT for NULL pointers, negative sizes, bad dtypes, ld < cols, a
+ * short workspace; UNSUPPORTED for misalignment, leading dimensions above, more than
+ * 2^31 - 1 rows or 2^40 values. */
+atp_status atp_grad_sq_sum(int32_t n, const atp_grad* grads, double* sum, void* workspace,
+                           size_t ws_bytes, void* stream);
+/* 0 for a list that the calls refuse (and for no values). */
+size_t atp_grad_workspace_bytes(int32_t n, const atp_grad* grads);
+
+/* Clipping by the norm over all devices: with S the sum of the red_size devices' sums
+ * (sums: host table of device pointers, 8-byte aligned, added in group order),
+ *   norm = scale * sqrt(S),  factor = scale * (norm > max_norm ? max_norm / norm : 1),
+ *   dst = factor * src, rounded once, for each gradient.
+ * scale: what the gradients are to be multiplied by in any case (1 / loss scale, 1 /
+ * number of accumulated batches).  norm: fp32 [2], 8-byte aligned, receives norm and
+ * factor.  An infinite norm gives factor 0 (NaN where the gradient is infinite), a NaN
+ * one NaN everywhere: look at norm before using dst.  A dst must be its src itself
+ * (type and leading dimension too) or overlap no src, and no other dst (the call
+ * looks at pairs of one gradient alone).  Errors as atp_grad_sq_sum; INVALID_ARGUMENT
+ * for scale or max_norm not positive (max_norm may be infinite), red_size < 1;
+ * UNSUPPORTED for red_size above ATP_MAX_GROUP. */
+atp_status atp_grad_clip(int32_t n, const atp_grad* grads, int32_t red_size,
+                         const double* const* sums, float scale, float max_norm, float* norm,
+                         void* stream);
+
 /* Per-kernel timing of the library's own launches.  When enabled, every
  * kernel the library enqueues is bracketed by HIP events on its stream;
  * atp_profile_collect synchronises those events, fills up to `max`

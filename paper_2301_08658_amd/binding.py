@@ -144,6 +144,21 @@ class atp_kv_batch(ctypes.Structure):
                 ("n_seqs", ctypes.c_int32), ("ctx", _vp), ("cu_new", _vp)]
 
 
+class atp_layer_norm(ctypes.Structure):
+    _fields_ = [("weight", _vp), ("bias", _vp), ("eps", ctypes.c_float)]
+
+
+class atp_attention_docs(ctypes.Structure):
+    _fields_ = [("cu_docs", _vp), ("prefix", _vp), ("slopes", _vp), ("n_docs", ctypes.c_int32),
+                ("cap", ctypes.c_float)]
+
+
+class atp_grad(ctypes.Structure):
+    _fields_ = [("src", _vp), ("dst", _vp), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("ld_src", ctypes.c_int64), ("ld_dst", ctypes.c_int64),
+                ("src_dtype", ctypes.c_int32), ("dst_dtype", ctypes.c_int32)]
+
+
 class atp_kernel_stat(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 64), ("launches", ctypes.c_int64),
                 ("total_ms", ctypes.c_double), ("flops", ctypes.c_double),
@@ -181,6 +196,11 @@ EXPORTS = (
     "atp_qk_norm_rope_workspace_bytes", "atp_qk_norm_rope_cache", "atp_cache_reserve",
     "atp_cache_workspace_bytes", "atp_cache_fork", "atp_cache_release", "atp_cache_copy_pages",
     "atp_cache_compact", "atp_attention_cache_fwd", "atp_attention_cache_workspace_bytes",
+    "atp_embedding_fwd", "atp_embedding_bwd", "atp_embedding_workspace_bytes",
+    "atp_layer_norm_fwd", "atp_layer_norm_stats", "atp_layer_norm_bwd", "atp_layer_norm_bwd_sums",
+    "atp_layer_norm_workspace_bytes", "atp_attention_docs_fwd", "atp_attention_docs_bwd",
+    "atp_attention_docs_workspace_bytes", "atp_grad_sq_sum", "atp_grad_clip",
+    "atp_grad_workspace_bytes",
 )
 ATP_MAX_QUERY_GROUP = 64
 ATP_MAX_FORKS = 4096
@@ -279,6 +299,28 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.atp_attention_cache_fwd.argtypes = [kcp, kbp, i64, i32, i32, _vp, i64, _vp, i32, _vp, i64,
                                             _vp, _vp, sz, _vp]
     lib.atp_attention_cache_workspace_bytes.argtypes = [i32, i32, i32]
+    f32 = ctypes.c_float
+    lnp, adp, gp = (ctypes.POINTER(atp_layer_norm), ctypes.POINTER(atp_attention_docs),
+                    ctypes.POINTER(atp_grad))
+    lib.atp_embedding_fwd.argtypes = [i64, _vp, i64, i64, i64, _vp, i64, f32, _vp, i32, i64, _vp]
+    lib.atp_embedding_bwd.argtypes = [i64, _vp, i64, i64, i64, _vp, i64, f32, _vp, i64, i32, _vp,
+                                      sz, _vp]
+    lib.atp_embedding_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.atp_layer_norm_stats.argtypes = [i64, i64, i32, _vp, i64, _vp, i64, _vp, i64, _vp, _vp]
+    lib.atp_layer_norm_fwd.argtypes = [i64, i64, i32, lnp, _vp, i64, _vp, i64, _vp, i64, i32, _fpp,
+                                       _vp, i64, _vp, _vp, _vp]
+    lib.atp_layer_norm_bwd_sums.argtypes = [i64, i64, i32, lnp, _vp, i64, _vp, _vp, _vp, i64, _vp,
+                                            _vp]
+    lib.atp_layer_norm_bwd.argtypes = [i64, i64, i32, lnp, _vp, i64, _vp, _vp, _vp, i64, _vp, i64,
+                                       i32, _fpp, _vp, i64, _vp, i64, _vp, _vp, _vp, sz, _vp]
+    lib.atp_layer_norm_workspace_bytes.argtypes = [i64, i64]
+    lib.atp_attention_docs_fwd.argtypes = [i64, i32, i32, adp, _vp, i64, _vp, i64, _vp, _vp]
+    lib.atp_attention_docs_bwd.argtypes = [i64, i32, i32, adp, _vp, i64, _vp, i64, _vp, _vp, i64,
+                                           _vp, i64, _vp, sz, _vp]
+    lib.atp_attention_docs_workspace_bytes.argtypes = [i64, i32, i32]
+    lib.atp_grad_sq_sum.argtypes = [i32, gp, _vp, _vp, sz, _vp]
+    lib.atp_grad_clip.argtypes = [i32, gp, i32, _fpp, f32, f32, _vp, _vp]
+    lib.atp_grad_workspace_bytes.argtypes = [i32, gp]
     for name in EXPORTS[EXPORTS.index("atp_qk_norm_rope_fwd"):]:
         getattr(lib, name).restype = sz if name.endswith("_bytes") else i32
     hp, dp, cp = (ctypes.POINTER(atp_hcm_layer), ctypes.POINTER(atp_model_dims),
@@ -1001,6 +1043,317 @@ def atp_attention_cache_fwd(cache: kv_cache, batch: kv_batch, tokens: int, group
         cache.ref(dev), batch.ref(dev), int(tokens), int(group), int(max_new), qp, ldq, mp, words,
         op, ldo, _list(lse, cache.kv_heads * group * tokens, "lse", dev, torch.float32), wsp, wsb,
         _stream(stream, dev)))
+
+
+# ------------------------------------------------ around the layers, for training
+def _stream_mat(t, rows: int, cols: int, dtype, name: str, dev: int):
+    """(pointer, ld) of a matrix of the residual stream's type."""
+    if dtype is torch.bfloat16:
+        return _rows(t, rows, cols, name, dev)
+    return _mat(t, rows, cols, dtype, name)
+
+
+def _float_dtype(t, name: str):
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"{name}: expected torch.float32 or torch.bfloat16, got {t.dtype}")
+    return t.dtype, (ATP_F32 if t.dtype is torch.float32 else ATP_BF16)
+
+
+def atp_embedding_fwd(tokens: int, ids, table, out, scale: float = 1.0, vocab_off: int = 0,
+                      stream=None):
+    """out[t] = scale * table[ids[t] - vocab_off], zeros for tokens of other
+    devices.  ids: int32 [tokens]; table: bf16 [vocab_loc, cols]; out: float32 or
+    bf16 [tokens, cols]."""
+    dev = torch.cuda.current_device()
+    if table.dim() != 2:
+        raise ValueError("table: needs a 2-D row-major tensor")
+    vocab, cols = table.shape
+    odt, code = _float_dtype(out, "out")
+    tp, ldt = _rows(table, vocab, cols, "table", dev)
+    op, ldo = _stream_mat(out, tokens, cols, odt, "out", dev)
+    _check(load_library().atp_embedding_fwd(
+        int(tokens), _list(ids, tokens, "ids", dev), vocab, int(vocab_off), cols, tp, ldt,
+        float(scale), op, code, ldo, _stream(stream, dev)))
+
+
+def atp_embedding_workspace_bytes(tokens: int, vocab_loc: int, cols: int) -> int:
+    return load_library().atp_embedding_workspace_bytes(int(tokens), int(vocab_loc), int(cols))
+
+
+def atp_embedding_bwd(tokens: int, ids, dy, dtable, workspace, scale: float = 1.0,
+                      vocab_off: int = 0, accumulate: bool = False, stream=None):
+    """dtable[v] (float32 [vocab_loc, cols]) = or, with accumulate, += scale * the
+    sum of dy (bf16 [tokens, cols]) over the tokens with that id; workspace:
+    atp_embedding_workspace_bytes(tokens, vocab_loc, cols) bytes."""
+    dev = torch.cuda.current_device()
+    if dtable.dim() != 2:
+        raise ValueError("dtable: needs a 2-D row-major tensor")
+    vocab, cols = dtable.shape
+    yp, ldy = _rows(dy, tokens, cols, "dy", dev)
+    tp, ldt = _mat(dtable, vocab, cols, torch.float32, "dtable")
+    wsp, wsb = _bytes(workspace, dev)
+    _check(load_library().atp_embedding_bwd(
+        int(tokens), _list(ids, tokens, "ids", dev), vocab, int(vocab_off), cols, yp, ldy,
+        float(scale), tp, ldt, int(accumulate), wsp, wsb, _stream(stream, dev)))
+
+
+class layer_norm(_Held):
+    """Parameters of a layer norm (atp_layer_norm in include/atp.h); keeps its
+    tensors alive.  weight, bias: bf16, this device's columns, or None."""
+
+    def __init__(self, weight=None, bias=None, eps: float = 1e-5):
+        self.cols = None
+        for t, name in ((weight, "weight"), (bias, "bias")):
+            if t is None:
+                continue
+            if self.cols not in (None, t.numel()):
+                raise ValueError(f"{name}: {t.numel()} values, weight has {self.cols}")
+            self.cols = t.numel()
+        self._hold(atp_layer_norm(
+            _vec(weight, self.cols or 0, torch.bfloat16, "weight"),
+            _vec(bias, self.cols or 0, torch.bfloat16, "bias"), float(eps)),
+            weight=weight, bias=bias)
+
+    def of(self, cols: int, dev: int):
+        if self.cols not in (None, cols):
+            raise ValueError(f"norm: {self.cols} parameters for rows of {cols}")
+        return self.ref(dev)
+
+
+def _row_tables(ts, tokens: int, name: str, dev: int):
+    """(red_size, host array) of a group's float32 [tokens, 2] tables."""
+    if ts is None:
+        return 1, None
+    arr = (ctypes.c_void_p * max(1, len(ts)))()
+    for j, t in enumerate(ts):
+        arr[j] = _list(t, 2 * tokens, f"{name}[{j}]", dev, torch.float32)
+    return len(ts), arr
+
+
+def _summed(tokens: int, x, add, x_out, dev: int):
+    """Sizes and arguments of the sum that a norm is of."""
+    if x.dim() != 2:
+        raise ValueError("x: needs a 2-D row-major tensor")
+    cols = x.size(1)
+    dt, code = _float_dtype(x, "x")
+    xp, ldx = _stream_mat(x, tokens, cols, dt, "x", dev)
+    ap, lda = _rows(add, tokens, cols, "add", dev) if add is not None else (None, 0)
+    op, ldo = (_stream_mat(x_out, tokens, cols, dt, "x_out", dev) if x_out is not None
+               else (None, 0))
+    return cols, code, (xp, ldx, ap, lda, op, ldo)
+
+
+def atp_layer_norm_stats(tokens: int, x, stats, add=None, x_out=None, stream=None):
+    """x_out = x + add (both or neither), and the statistics of this device's
+    columns of it into stats, float32 [tokens, 2]."""
+    dev = torch.cuda.current_device()
+    cols, code, args = _summed(tokens, x, add, x_out, dev)
+    _check(load_library().atp_layer_norm_stats(
+        int(tokens), cols, code, *args, _list(stats, 2 * tokens, "stats", dev, torch.float32),
+        _stream(stream, dev)))
+
+
+def atp_layer_norm_fwd(tokens: int, norm: layer_norm, x, y, mean, rstd, add=None, x_out=None,
+                       stats=None, stream=None):
+    """y (bf16) = the norm of x (float32 or bf16 [tokens, cols]) or of x_out = x +
+    add; mean, rstd: float32 [tokens], written.  stats: the group's statistics
+    (a list of float32 [tokens, 2]) where the rows' columns lie on several devices."""
+    dev = torch.cuda.current_device()
+    cols, code, args = _summed(tokens, x, add, x_out, dev)
+    n, tab = _row_tables(stats, tokens, "stats", dev)
+    yp, ldy = _rows(y, tokens, cols, "y", dev)
+    _check(load_library().atp_layer_norm_fwd(
+        int(tokens), cols, code, norm.of(cols, dev), *args, n, tab, yp, ldy,
+        _list(mean, tokens, "mean", dev, torch.float32),
+        _list(rstd, tokens, "rstd", dev, torch.float32), _stream(stream, dev)))
+
+
+def _normed(tokens: int, norm, x, mean, rstd, dy, dev: int):
+    """Sizes and the arguments that both calls of the backward share."""
+    if x.dim() != 2:
+        raise ValueError("x: needs a 2-D row-major tensor")
+    cols = x.size(1)
+    dt, code = _float_dtype(x, "x")
+    xp, ldx = _stream_mat(x, tokens, cols, dt, "x", dev)
+    gp, ldg = _rows(dy, tokens, cols, "dy", dev)
+    return cols, dt, (int(tokens), cols, code, norm.of(cols, dev), xp, ldx,
+                      _list(mean, tokens, "mean", dev, torch.float32),
+                      _list(rstd, tokens, "rstd", dev, torch.float32), gp, ldg)
+
+
+def atp_layer_norm_bwd_sums(tokens: int, norm: layer_norm, x, mean, rstd, dy, sums, stream=None):
+    """The row sums of this device's columns that the others need, into sums
+    (float32 [tokens, 2])."""
+    dev = torch.cuda.current_device()
+    _, _, args = _normed(tokens, norm, x, mean, rstd, dy, dev)
+    _check(load_library().atp_layer_norm_bwd_sums(
+        *args, _list(sums, 2 * tokens, "sums", dev, torch.float32), _stream(stream, dev)))
+
+
+def atp_layer_norm_workspace_bytes(tokens: int, cols: int) -> int:
+    return load_library().atp_layer_norm_workspace_bytes(int(tokens), int(cols))
+
+
+def atp_layer_norm_bwd(tokens: int, norm: layer_norm, x, mean, rstd, dy, dx, d_res=None,
+                       d_add=None, sums=None, dweight=None, dbias=None, workspace=None,
+                       stream=None):
+    """Gradient of atp_layer_norm_fwd: dx (x's type; may be d_res, the gradient that
+    goes past the norm), d_add (bf16 copy of dx), dweight, dbias (float32 [cols]; they
+    need a workspace of atp_layer_norm_workspace_bytes(tokens, cols) bytes).  x: the
+    normed values; sums: the group's row sums, as stats in the forward."""
+    dev = torch.cuda.current_device()
+    cols, dt, args = _normed(tokens, norm, x, mean, rstd, dy, dev)
+    rp, ldr = (_stream_mat(d_res, tokens, cols, dt, "d_res", dev) if d_res is not None
+               else (None, 0))
+    n, tab = _row_tables(sums, tokens, "sums", dev)
+    dp_, ldd = _stream_mat(dx, tokens, cols, dt, "dx", dev)
+    ap, lda = _rows(d_add, tokens, cols, "d_add", dev) if d_add is not None else (None, 0)
+    wsp, wsb = _bytes(workspace, dev)
+    _check(load_library().atp_layer_norm_bwd(
+        *args, rp, ldr, n, tab, dp_, ldd, ap, lda,
+        _list(dweight, cols, "dweight", dev, torch.float32),
+        _list(dbias, cols, "dbias", dev, torch.float32), wsp, wsb, _stream(stream, dev)))
+
+
+class attention_docs(_Held):
+    """Documents of packed rows and what is done to their scores
+    (atp_attention_docs in include/atp.h): cu_docs int32 [n_docs + 1], prefix int32
+    [n_docs] or None, slopes float32 [query heads] or None, cap (0: none).  The
+    tensors are read when a call's kernels run."""
+
+    def __init__(self, cu_docs: torch.Tensor, prefix=None, slopes=None, cap: float = 0.0):
+        if cu_docs.numel() < 1:
+            raise ValueError("cu_docs: needs n_docs + 1 values")
+        self.n_docs = cu_docs.numel() - 1
+        self.heads = None if slopes is None else slopes.numel()
+        self._hold(atp_attention_docs(
+            _vec(cu_docs, self.n_docs + 1, torch.int32, "cu_docs"),
+            _vec(prefix, self.n_docs, torch.int32, "prefix"),
+            _vec(slopes, self.heads or 0, torch.float32, "slopes"), self.n_docs, float(cap)),
+            cu_docs=cu_docs, prefix=prefix, slopes=slopes)
+
+    def of(self, heads: int, dev: int):
+        if self.heads is not None and self.heads < heads:
+            raise ValueError(f"slopes: {self.heads} for {heads} query heads")
+        return self.ref(dev)
+
+
+def atp_attention_docs_fwd(tokens: int, kv_heads: int, group: int, docs: attention_docs, qkv, out,
+                           lse, stream=None):
+    """Attention within documents: qkv bf16 [tokens, kv_heads*(group+2)*128], out bf16
+    [tokens, kv_heads*group*128], lse float32 [kv_heads*group, tokens]."""
+    dev = torch.cuda.current_device()
+    heads = kv_heads * group
+    qp, ldq = _rows(qkv, tokens, kv_heads * (group + 2) * HEAD_DIM, "qkv", dev)
+    op, ldo = _rows(out, tokens, heads * HEAD_DIM, "out", dev)
+    _check(load_library().atp_attention_docs_fwd(
+        int(tokens), int(kv_heads), int(group), docs.of(heads, dev), qp, ldq, op, ldo,
+        _list(lse, heads * tokens, "lse", dev, torch.float32), _stream(stream, dev)))
+
+
+def atp_attention_docs_workspace_bytes(tokens: int, kv_heads: int, group: int) -> int:
+    return load_library().atp_attention_docs_workspace_bytes(int(tokens), int(kv_heads),
+                                                             int(group))
+
+
+def atp_attention_docs_bwd(tokens: int, kv_heads: int, group: int, docs: attention_docs, qkv, out,
+                           lse, d_out, d_qkv, workspace, stream=None):
+    """Gradient of atp_attention_docs_fwd into d_qkv (qkv's shape); workspace:
+    atp_attention_docs_workspace_bytes(tokens, kv_heads, group) bytes."""
+    dev = torch.cuda.current_device()
+    heads, cols = kv_heads * group, kv_heads * (group + 2) * HEAD_DIM
+    qp, ldq = _rows(qkv, tokens, cols, "qkv", dev)
+    op, ldo = _rows(out, tokens, heads * HEAD_DIM, "out", dev)
+    gp, ldg = _rows(d_out, tokens, heads * HEAD_DIM, "d_out", dev)
+    dp_, ldd = _rows(d_qkv, tokens, cols, "d_qkv", dev)
+    wsp, wsb = _bytes(workspace, dev)
+    _check(load_library().atp_attention_docs_bwd(
+        int(tokens), int(kv_heads), int(group), docs.of(heads, dev), qp, ldq, op, ldo,
+        _list(lse, heads * tokens, "lse", dev, torch.float32), gp, ldg, dp_, ldd, wsp, wsb,
+        _stream(stream, dev)))
+
+
+class grad_list:
+    """Gradients and where their clipped values go (an array of atp_grad; keeps the
+    tensors alive).  src: float32 or bf16 tensors, contiguous or 2-D with gaps between
+    rows; dst: as many of the same sizes, or None for src itself."""
+
+    def __init__(self, src: Sequence[torch.Tensor], dst: Optional[Sequence] = None):
+        dst = list(src) if dst is None else list(dst)
+        self._tensors = (list(src), dst)
+        if len(dst) != len(self._tensors[0]):
+            raise ValueError(f"dst: {len(dst)} tensors for {len(self._tensors[0])} gradients")
+        self.n = len(dst)
+        self.device = None
+        self.c = (atp_grad * max(1, self.n))()
+        spans = []
+        for i, (s, d) in enumerate(zip(*self._tensors)):
+            if s.numel() != d.numel():
+                raise ValueError(f"dst[{i}]: {tuple(d.shape)} for {tuple(s.shape)}")
+            rows, cols = self._matrix(s, f"src[{i}]")
+            if self._matrix(d, f"dst[{i}]") != (rows, cols):
+                # one of them has gaps between its rows: both are taken as matrices
+                if s.shape != d.shape or s.dim() != 2:
+                    raise ValueError(f"dst[{i}]: {tuple(d.shape)} for {tuple(s.shape)}")
+                rows, cols = s.shape
+            g = self.c[i]
+            for t, side in ((s, "src"), (d, "dst")):
+                _on_device(t, f"{side}[{i}]")
+                setattr(g, side, t.data_ptr())
+                gaps = t.dim() == 2 and rows == t.size(0) and rows > 1
+                setattr(g, "ld_" + side, t.stride(0) if gaps else cols)
+                setattr(g, side + "_dtype", _float_dtype(t, f"{side}[{i}]")[1])
+                if t.numel():
+                    end = (rows - 1) * getattr(g, "ld_" + side) + cols
+                    spans.append((t.data_ptr(), t.data_ptr() + end * t.element_size(), i, side))
+            g.rows, g.cols = rows, cols
+            self.device = s.device.index
+        # a result must not land in another gradient or result
+        spans.sort()
+        for (_, e0, i, a), (b1, _, j, b) in zip(spans, spans[1:]):
+            if b1 < e0 and i != j and "dst" in (a, b):
+                raise ValueError(f"{a}[{i}] and {b}[{j}] overlap")
+
+    @staticmethod
+    def _matrix(t: torch.Tensor, name: str):
+        if t.is_contiguous():
+            return 1, t.numel()
+        if t.dim() == 2 and (t.size(1) <= 1 or t.stride(1) == 1) and t.stride(0) >= t.size(1):
+            return tuple(t.shape)
+        raise ValueError(f"{name}: needs a contiguous tensor or rows with gaps")
+
+    def at(self, dev: int):
+        if self.n and self.device != dev:
+            raise ValueError(f"gradients: on cuda:{self.device}, but the current device is "
+                             f"cuda:{dev}")
+        return self.c
+
+
+def atp_grad_workspace_bytes(grads: grad_list) -> int:
+    return load_library().atp_grad_workspace_bytes(grads.n, grads.c)
+
+
+def atp_grad_sq_sum(grads: grad_list, total, workspace=None, stream=None):
+    """total (float64, one value) = the sum of the squares of all gradients;
+    workspace: atp_grad_workspace_bytes(grads) bytes."""
+    dev = torch.cuda.current_device()
+    wsp, wsb = _bytes(workspace, dev)
+    _check(load_library().atp_grad_sq_sum(
+        grads.n, grads.at(dev), _list(total, 1, "total", dev, torch.float64), wsp, wsb,
+        _stream(stream, dev)))
+
+
+def atp_grad_clip(grads: grad_list, sums, norm, max_norm: float, scale: float = 1.0, stream=None):
+    """Scales the gradients into their destinations by scale * min(1, max_norm / norm)
+    with norm = scale * sqrt(sum of `sums`), a list of the devices' totals (float64, one
+    value each); norm: float32 [2], receives the norm and the factor."""
+    dev = torch.cuda.current_device()
+    arr = (ctypes.c_void_p * max(1, len(sums)))()
+    for j, t in enumerate(sums):
+        arr[j] = _list(t, 1, f"sums[{j}]", dev, torch.float64)
+    _check(load_library().atp_grad_clip(
+        grads.n, grads.at(dev), len(sums), arr, float(scale), float(max_norm),
+        _list(norm, 2, "norm", dev, torch.float32), _stream(stream, dev)))
 
 
 def _attn_weights(G, w, b, layout: int):

@@ -12,7 +12,8 @@ ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libatp.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["gemm.hip", "reduce.hip", "transpose.hip", "attention.hip", "abi.hip",
-           "norm_rope.hip", "cache.hip", "attention_cache.hip", "cache_abi.hip"]
+           "norm_rope.hip", "cache.hip", "attention_cache.hip", "cache_abi.hip", "embedding.hip",
+           "layer_norm.hip", "grad_clip.hip", "attention_docs.hip", "train_abi.hip"]
 HOST_SOURCES = ["planner.cpp"]
 ARCH = "gfx950"
 

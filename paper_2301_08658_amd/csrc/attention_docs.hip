@@ -1,0 +1,951 @@
+// Causal attention within documents of packed rows, for training: forward and
+// backward, with key/value heads shared by `group` query heads, a prefix of each
+// document that all of its rows see, scores capped by a tanh and a bias by distance.
+//
+//   x_ij = cap tanh(q_i . k_j / (cap sqrt(d))) - slope |i - j|,
+//   o_i = sum_j softmax_j(x_ij) v_j over j in [start, max(i + 1, start + prefix))
+//
+// with start the first row of i's document.  Tiles of rows and keys begin at a
+// document's start and end at its end, so a tile never holds two documents: what
+// another document or the padding holds is not read, and inside a tile all is as in
+// the causal core (attention.hip describes tiles, fragments and the running softmax).
+// A row sees an interval of its document from the first key on, so the tiles that
+// need a mask are those that reach past the first row's limit.
+//
+// Documents are found without a list of tiles: document d's tiles of Q rows take the
+// slots from cu[d] / Q + d on.  They do not overlap (floor(a + b) >= floor(a) +
+// floor(b), and a document of n rows has at most floor(n / Q) + 1 tiles), the slots
+// end at cu[n] / Q + n, and a workgroup finds its document by a search over cu alone;
+// slots without a tile end at once.
+//
+// Backward: P from the saved log-sum-exps, delta_i = dO_i . O_i,
+//   dS = P o (dO V^T - delta) o (1 - tanh^2), dQ = dS K / sqrt(d), dK = dS^T Q / sqrt(d),
+//   dV = P^T dO.  A workgroup of the dK/dV kernel walks the query tiles of all query
+// heads of its key head; where that leaves too few workgroups the heads are divided
+// over several, which leave fp32 sums that are added in order.
+//
+// Bound by the matrix cores and the exponentials together, as the causal core is.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "attention_tiles.h"
+#include "train_kernels.h"
+#include "wave_ops.h"
+
+namespace atp {
+namespace {
+
+using namespace tiles;
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+struct Common {
+    const uint16_t* qkv; int64_t ldq;
+    const int32_t* cu;
+    const int32_t* prefix;
+    const float* slopes;
+    int64_t tokens;
+    int n_docs, kv_heads, group, slots;
+    float scale_log2;                    // log2(e) / sqrt(D)
+    float cap_in, cap_log2;              // 2 log2(e) / (sqrt(D) cap), cap log2(e)
+};
+
+struct Doc {
+    int64_t tok0;                        // first row
+    int len, tile, prefix;               // rows, this slot's tile, rows that all see
+};
+
+// The document and tile of a slot of 2^SHIFT rows; false for a slot without one.
+// Lists that do not ascend or leave the rows give tiles inside the rows all the same.
+template <int SHIFT>
+__device__ __forceinline__ bool find_tile(const Common& a, int slot, Doc& doc) {
+    const int lane = threadIdx.x & 63;
+    int lo = 0, span = a.n_docs;         // the document is in [lo, lo + span)
+    for (;;) {
+        const int step = (span + 63) >> 6;
+        const int i = lo + lane * step;
+        const bool le = lane * step < span && (a.cu[i] >> SHIFT) + i <= slot;
+        const int n = __popcll(__builtin_amdgcn_ballot_w64(le));
+        if (n == 0) return false;
+        const int skip = (n - 1) * step;
+        lo += skip;
+        span = min(step, span - skip);
+        if (step == 1) break;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    const int64_t c0 = a.cu[lo];
+    const int64_t start = c0 < 0 ? 0 : (c0 > a.tokens ? a.tokens : c0);
+    int64_t end = a.cu[lo + 1];
+    end = end > a.tokens ? a.tokens : end;
+    doc.tok0 = start;
+    doc.len = end > start ? (int)(end - start) : 0;
+    doc.tile = slot - (int)(c0 >> SHIFT) - lo;
+    doc.prefix = 0;
+    if (a.prefix) doc.prefix = max(0, min(a.prefix[lo], doc.len));
+    return doc.tile >= 0 && ((int64_t)doc.tile << SHIFT) < doc.len;
+}
+
+// Scores in base 2 from raw products.  Without cap and bias they stay raw and are
+// scaled in the exponential's argument.
+template <bool CAP, bool BIAS>
+struct Score {
+    static constexpr bool kRaw = !CAP && !BIAS;
+    float scale, cap_in, cap_log2, slope;
+    __device__ __forceinline__ Score(const Common& a, int head)
+        : scale(a.scale_log2), cap_in(a.cap_in), cap_log2(a.cap_log2), slope(0.f) {
+        if constexpr (BIAS) slope = a.slopes[head] * kLog2e;
+    }
+    // tanh(y) = 1 - 2 / (1 + e^(2 y)): off by 2^-23 of 1 at most, which moves a score of
+    // cap 50 by 6e-6
+    __device__ __forceinline__ float tanh_of(float raw) const {
+        return 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(raw * cap_in));
+    }
+    __device__ __forceinline__ float bias(float x, float dist) const {
+        if constexpr (BIAS) return __builtin_fmaf(-slope, __builtin_fabsf(dist), x);
+        return x;
+    }
+    __device__ __forceinline__ float operator()(float raw, float dist) const {
+        if constexpr (kRaw) return raw;
+        return bias(CAP ? cap_log2 * tanh_of(raw) : raw * scale, dist);
+    }
+    __device__ __forceinline__ float factor() const { return kRaw ? scale : 1.f; }
+};
+
+// ---------------------------------------------------------------------------
+// forward
+// ---------------------------------------------------------------------------
+struct FwdArgs : Common {
+    uint16_t* out; int64_t ldo;
+    float* lse;                          // [heads][tokens]
+};
+
+// bf16 pairs with an exponent of all ones have bit 15 of their half set in this.
+__device__ __forceinline__ uint32_t odd_bits(uint32_t w) {
+    return (w & 0x7f807f80u) + 0x00800080u;
+}
+
+// Values of a masked tile may be infinite or NaN where no row of the tile, or only
+// some, see them, and 0 times such a value is NaN.  These values are left out of the
+// products and added to the rows that see them (as their sum with anything is what
+// the weighted sum gives too).
+template <int RB>
+__device__ void odd_values(const uint16_t* vs, int n_first, const int (&limit)[RB], int g,
+                           f32x4 (&o)[RB][8]) {
+    for (int n = 0; n < BN; ++n) {
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) {
+            const int c = 16 * dt + 4 * g;
+            const u32x2 w =
+                *reinterpret_cast<const u32x2*>(vs + n * D + vpos(n, c >> 3) * 8 + (c & 7));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float v = __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+                const bool odd = (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u;
+#pragma unroll
+                for (int r = 0; r < RB; ++r)
+                    if (odd && n_first + n < limit[r]) o[r][dt][e] += v;
+            }
+        }
+    }
+}
+
+template <int RB, int KG, bool CAP, bool BIAS>
+__global__ __launch_bounds__(NTHR * KG + (KG > 1 ? NTHR : 0), KG > 1 ? 3 : 2)
+void docs_fwd_kernel(FwdArgs a) {
+    constexpr int QT = 64 * RB;
+    constexpr bool PRODUCERS = KG > 1;
+    __shared__ __attribute__((aligned(16))) uint16_t kv[KG][2][2][BN * D];   // [group][buf][K|V]
+    __shared__ float mls[KG > 1 ? NWAVE * RB * 2 * 64 : 1];                // group 1's m, l
+    const int lane = threadIdx.x & 63;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool producer = PRODUCERS && wv >= KG * NWAVE;
+    const int grp = producer ? 0 : wv / NWAVE, wave = wv % NWAVE;
+    // the last slots first: a document's long rows lead
+    const int heads = a.kv_heads * a.group;
+    const int head = blockIdx.x % heads, kvh = head / a.group;
+    Doc doc;
+    if (!find_tile<RB == 2 ? 7 : 6>(a, a.slots - 1 - (int)(blockIdx.x / heads), doc)) return;
+    const int qt = doc.tile;
+    const int64_t tok0 = doc.tok0;
+    const int64_t hc = (int64_t)kvh * (a.group + 2) * D;
+    const int64_t qc = hc + (int64_t)(head - kvh * a.group) * D;
+
+    const int last = min(qt * QT + QT, doc.len) - 1;
+    const int nkt = (max(last + 1, doc.prefix) + BN - 1) / BN;
+    const int half = KG > 1 ? (nkt + 1) / 2 : nkt;
+    const int kt0 = grp == 0 ? 0 : half;
+    const int mine = grp == 0 ? half : nkt - half;   // <= half
+    uint16_t(*buf)[2][BN * D] = kv[grp];
+    TileDma2<true> cp;
+    cp.init(a.ldq, a.ldq, wave, lane);
+    const uint16_t* kbase = a.qkv + hc + (int64_t)a.group * D;
+    const uint16_t* vbase = kbase + D;
+    if constexpr (PRODUCERS) {
+        if (producer) {
+            produce<KG>(cp, kbase, vbase, a.ldq, tok0, nkt, doc.len, kv, wave);
+            return;
+        }
+    } else {
+        if (mine > 0)
+            cp.issue(kbase, a.ldq, vbase, a.ldq, tok0, kt0 * BN, doc.len, buf[0][0], buf[0][1],
+                     wave);
+        dma::wait_vmcnt<0>();
+    }
+    int mrow[RB], limit[RB];             // rows in the document, keys that they see
+    bf16x8 qf[RB][4];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        mrow[r] = qt * QT + 64 * r + wave * 16 + (lane & 15);
+        limit[r] = max(mrow[r] + 1, doc.prefix);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            if (mrow[r] < doc.len)
+                qf[r][ks] = *reinterpret_cast<const bf16x8*>(
+                    a.qkv + (tok0 + mrow[r]) * a.ldq + qc + 32 * ks + 8 * (lane >> 4));
+            else
+                qf[r][ks] = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+        }
+    }
+    const Score<CAP, BIAS> score(a, head);
+    const float factor = score.factor();
+
+    f32x4 o[RB][8];
+    float mrun[RB], lrun[RB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) o[r][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        mrun[r] = -INFINITY;
+        lrun[r] = 0.f;
+    }
+
+    __syncthreads();
+    const int g = lane >> 4, l16 = lane & 15;
+    int koff[4], voff[8];
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) koff[ks] = l16 * D + kpos(l16, 4 * ks + g) * 8;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) voff[dt] = tr_offset(lane, dt);
+    const int clear = max(qt * QT + 1, doc.prefix);   // keys that every row sees
+    for (int i = 0; i < half; ++i) {
+        if (i < mine) {
+            const int kt = kt0 + i;
+            const uint16_t* ks_ = buf[i & 1][0];
+            const uint16_t* vs_ = buf[i & 1][1];
+            const bool more = !PRODUCERS && i + 1 < mine;
+            const auto next = cp.rounds(kbase, a.ldq, vbase, a.ldq, tok0, (kt + 1) * BN, doc.len,
+                                        buf[(i + 1) & 1][0], buf[(i + 1) & 1][1]);
+            f32x4 s[RB][4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int r = 0; r < RB; ++r) s[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bf16x8 kf =
+                        *reinterpret_cast<const bf16x8*>(ks_ + 16 * j * D + koff[ks]);
+#pragma unroll
+                    for (int r = 0; r < RB; ++r)
+                        s[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][ks], s[r][j],
+                                                                          0, 0, 0);
+                    if (j == 3 && more) cp.round(next, ks, wave);
+                }
+            if constexpr (!Score<CAP, BIAS>::kRaw) {
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    const float ahead = (float)(mrow[r] - kt * BN - 4 * g);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            s[r][j][e] = score(s[r][j][e], ahead - (float)(16 * j + e));
+                }
+            }
+            // keys past the document are past every limit of its rows
+            const bool masked = (kt + 1) * BN > clear;
+            bool odd = false;
+            if (masked) {
+#pragma unroll
+                for (int r = 0; r < RB; ++r)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (kt * BN + 16 * j + 4 * g + e >= limit[r]) s[r][j][e] = -INFINITY;
+                uint32_t seen = 0;
+#pragma unroll
+                for (int c = 0; c < BN * D / 512; ++c) {
+                    const u32x4 w = *reinterpret_cast<const u32x4*>(vs_ + (c * 64 + lane) * 8);
+                    seen |= odd_bits(w[0]) | odd_bits(w[1]) | odd_bits(w[2]) | odd_bits(w[3]);
+                }
+                odd = __builtin_amdgcn_ballot_w64((seen & 0x80008000u) != 0) != 0;
+            }
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                float mx = max16(s[r]);
+                mx = row_max4(mx);
+                const float mnew = fmaxf(mrun[r], mx * factor);
+                if (__builtin_amdgcn_ballot_w64(mnew > mrun[r] + kSlack) != 0) {
+                    const float alpha =
+                        __builtin_amdgcn_exp2f(mrun[r] - (mnew == -INFINITY ? 0.f : mnew));
+                    lrun[r] *= alpha;
+#pragma unroll
+                    for (int dt = 0; dt < 8; ++dt) o[r][dt] *= alpha;
+                    mrun[r] = mnew;
+                }
+                const float msub = mrun[r] == -INFINITY ? 0.f : mrun[r];
+                float rs = 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float p =
+                            __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][j][e], factor, -msub));
+                        s[r][j][e] = p;
+                        rs += p;
+                    }
+                lrun[r] += row_sum4(rs);
+            }
+
+            // O += P V over two 32-key slices
+            auto add_values = [&](auto clean) {
+#pragma unroll
+                for (int sl = 0; sl < 2; ++sl) {
+                    bf16x8 pf[RB];
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) pf[r] = pack_pair(s[r][2 * sl], s[r][2 * sl + 1]);
+#pragma unroll
+                    for (int dt = 0; dt < 8; ++dt) {
+                        bf16x8 vf = frag_tr_at(vs_ + 32 * sl * D + voff[dt]);
+                        if constexpr (decltype(clean)::value) {
+                            u32x4 w = __builtin_bit_cast(u32x4, vf);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                w[k] &= ~(((odd_bits(w[k]) & 0x80008000u) >> 15) * 0xffffu);
+                            vf = __builtin_bit_cast(bf16x8, w);
+                        }
+#pragma unroll
+                        for (int r = 0; r < RB; ++r)
+                            o[r][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r], o[r][dt],
+                                                                               0, 0, 0);
+                    }
+                }
+            };
+            if (odd) {
+                add_values(std::true_type{});
+                odd_values<RB>(vs_, kt * BN, limit, g, o);
+            } else {
+                add_values(std::false_type{});
+            }
+        }
+        dma::wait_vmcnt<0>();
+        __syncthreads();
+    }
+
+    if constexpr (KG > 1) {
+        f32x4* ox = reinterpret_cast<f32x4*>(&kv[1][0][0][0]);
+        if (grp == 1) {
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) ox[((wave * RB + r) * 8 + dt) * 64 + lane] = o[r][dt];
+                mls[((wave * RB + r) * 2 + 0) * 64 + lane] = mrun[r];
+                mls[((wave * RB + r) * 2 + 1) * 64 + lane] = lrun[r];
+            }
+        }
+        __syncthreads();
+        if (grp == 1) return;
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            const float m1 = mls[((wave * RB + r) * 2 + 0) * 64 + lane];
+            const float l1 = mls[((wave * RB + r) * 2 + 1) * 64 + lane];
+            const float mn = fmaxf(mrun[r], m1);          // key 0 is group 0's
+            const float a0 = __builtin_amdgcn_exp2f(mrun[r] - mn);
+            const float a1 = __builtin_amdgcn_exp2f(m1 - mn);   // 0 when m1 = -inf
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt)
+                o[r][dt] = o[r][dt] * a0 + ox[((wave * RB + r) * 8 + dt) * 64 + lane] * a1;
+            lrun[r] = lrun[r] * a0 + l1 * a1;
+            mrun[r] = mn;
+        }
+    }
+
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        if (mrow[r] >= doc.len) continue;
+        const float inv = 1.0f / lrun[r];
+        uint16_t* orow = a.out + (tok0 + mrow[r]) * a.ldo + (int64_t)head * D;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) {
+            const u32x2 w = {pack_bf16x2(o[r][dt][0] * inv, o[r][dt][1] * inv),
+                             pack_bf16x2(o[r][dt][2] * inv, o[r][dt][3] * inv)};
+            *reinterpret_cast<u32x2*>(orow + 16 * dt + 4 * g) = w;
+        }
+        if (g == 0)
+            a.lse[(int64_t)head * a.tokens + tok0 + mrow[r]] =
+                (mrun[r] + __log2f(lrun[r])) * 0.69314718055994530942f;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// backward
+// ---------------------------------------------------------------------------
+struct BwdArgs : Common {
+    const uint16_t* out; int64_t ldo;
+    const uint16_t* dout; int64_t lddo;
+    const float* lse;                    // [heads][tokens]
+    float* delta;                        // [heads][tokens]
+    uint16_t* dqkv; int64_t lddq;
+    float* sums;                         // parts > 1: [parts][tokens][kv_heads][2][D]
+    int parts, part_heads;               // divisions of a group's query heads, heads in one
+    float inv_sqrt_d;
+};
+
+// P and dS of one element from the raw score, dO . v, and the row's lse and delta.
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ void grad_of(const Score<CAP, BIAS>& f, float raw, float dist, float l2,
+                                        float dl, bool hidden, float& p, float& ds) {
+    float pv, slope = 1.f;
+    if constexpr (CAP) {
+        const float t = f.tanh_of(raw);
+        slope = __builtin_fmaf(-t, t, 1.f);
+        pv = __builtin_amdgcn_exp2f(f.bias(__builtin_fmaf(f.cap_log2, t, -l2), dist));
+    } else {
+        pv = __builtin_amdgcn_exp2f(f.bias(__builtin_fmaf(raw, f.scale, -l2), dist));
+    }
+    float d = pv * (ds - dl);
+    if constexpr (CAP) d *= slope;
+    p = hidden ? 0.f : pv;
+    ds = hidden ? 0.f : d;
+}
+
+template <int KG, bool CAP, bool BIAS>
+__global__ __launch_bounds__(NTHR * KG, 2 / KG) void docs_dkv_kernel(BwdArgs a) {
+    __shared__ __attribute__((aligned(16))) uint16_t qd[KG][2][2][BM * D];   // [grp][buf][Q|dO]
+    __shared__ float rowv[KG][2][2][BM];                                    // [grp][buf][lse2|delta]
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int grp = wv / NWAVE, wave = wv % NWAVE;
+    const int tid = (int)threadIdx.x % NTHR;   // thread index within the group
+    const int per_slot = a.kv_heads * a.parts;
+    const int which = blockIdx.x % per_slot;
+    const int kvh = which % a.kv_heads, part = which / a.kv_heads;
+    Doc doc;
+    // early keys, which many rows see, first
+    if (!find_tile<6>(a, (int)(blockIdx.x / per_slot), doc)) return;
+    const int kt = doc.tile;
+    const int64_t tok0 = doc.tok0, T = a.tokens;
+    const int64_t hc = (int64_t)kvh * (a.group + 2) * D;
+    const int h0 = kvh * a.group + part * a.part_heads;          // first query head
+    const int nh = min(a.part_heads, a.group - part * a.part_heads);
+
+    const int kabs = kt * BN + wave * 16 + (lane & 15);
+    bf16x8 kf[4], vf[4];
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+        if (kabs < doc.len) {
+            const uint16_t* row = a.qkv + (tok0 + kabs) * a.ldq + hc + (int64_t)a.group * D;
+            kf[ks] = *reinterpret_cast<const bf16x8*>(row + 32 * ks + 8 * g);
+            vf[ks] = *reinterpret_cast<const bf16x8*>(row + D + 32 * ks + 8 * g);
+        } else {
+            kf[ks] = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+            vf[ks] = kf[ks];
+        }
+    }
+    f32x4 dk[8], dv[8];
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) {
+        dk[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        dv[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    auto load_rows = [&](int head, int qt, float& l2, float& dl) {
+        const int t = qt * BM + tid;
+        if (tid < BM && t < doc.len) {
+            l2 = a.lse[(int64_t)head * T + tok0 + t] * kLog2e;
+            dl = a.delta[(int64_t)head * T + tok0 + t];
+        } else {
+            l2 = 0.f;
+            dl = 0.f;
+        }
+    };
+    // the device's first query head is at column hc of a row, head h at hc + (h - kvh group) D
+    const int64_t qshift = hc - (int64_t)kvh * a.group * D;
+    int boff[4], toff[8];
+    offsets(lane, boff, toff);
+    TileDma2<false> cp;
+    cp.init(a.ldq, a.lddo, wave, lane);
+    // every head's query tiles from the first that sees the key tile to the document's
+    // last; the steps of all heads in turn, group 0 the first half, group 1 the rest
+    const int tiles_ = (doc.len + BM - 1) / BM;
+    const int first = kt * BN < doc.prefix ? 0 : kt;
+    const int per = tiles_ - first;
+    const int nsteps = nh * per;
+    const int half = KG > 1 ? (nsteps + 1) / 2 : nsteps;
+    const int begin = grp == 0 ? 0 : half;
+    const int mine = grp == 0 ? half : nsteps - half;   // <= half
+    int head = h0 + begin / per, qt = first + begin % per;
+    uint16_t(*qb)[2][BM * D] = qd[grp];
+    float(*rv)[2][BM] = rowv[grp];
+    float l2r = 0.f, dlr = 0.f;
+    if (mine > 0) {
+        cp.issue(a.qkv + qshift + (int64_t)head * D, a.ldq, a.dout + (int64_t)head * D, a.lddo, tok0,
+                 qt * BM, doc.len, qb[0][0], qb[0][1], wave);
+        load_rows(head, qt, l2r, dlr);
+        if (tid < BM) { rv[0][0][tid] = l2r; rv[0][1][tid] = dlr; }
+    }
+    dma::wait_vmcnt<0>();
+    __syncthreads();
+    for (int i = 0; i < half; ++i) {
+        if (i < mine) {
+            const int buf = i & 1;
+            const uint16_t* qs = qb[buf][0];
+            const uint16_t* ds_ = qb[buf][1];
+            const bool more = i + 1 < mine;
+            const bool wrap = qt + 1 == tiles_;
+            const int head2 = head + (wrap ? 1 : 0), qt2 = wrap ? first : qt + 1;
+            const auto next = cp.rounds(a.qkv + qshift + (int64_t)head2 * D, a.ldq,
+                                        a.dout + (int64_t)head2 * D, a.lddo, tok0, qt2 * BM,
+                                        doc.len, qb[buf ^ 1][0], qb[buf ^ 1][1]);
+            if (more) load_rows(head2, qt2, l2r, dlr);
+            // a tile whose first row sees the whole key tile, and that ends inside the
+            // document, needs no mask
+            const bool masked =
+                (kt + 1) * BN > max(qt * BM + 1, doc.prefix) || (qt + 1) * BM > doc.len;
+            const Score<CAP, BIAS> score(a, head);
+            f32x4 p[4], dsv[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                p[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                dsv[j] = p[j];
+            }
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    p[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        *reinterpret_cast<const bf16x8*>(qs + 16 * j * D + boff[ks]), kf[ks],
+                        p[j], 0, 0, 0);
+                    dsv[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        *reinterpret_cast<const bf16x8*>(ds_ + 16 * j * D + boff[ks]), vf[ks],
+                        dsv[j], 0, 0, 0);
+                    if (j == 3 && more) cp.round(next, ks, wave);
+                }
+            const float ahead = (float)(qt * BM + 4 * g - kabs);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int ql = 16 * j + 4 * g + e;
+                    const int qabs = qt * BM + ql;
+                    const bool hidden =
+                        masked && (kabs >= max(qabs + 1, doc.prefix) || qabs >= doc.len);
+                    float pv, dv_ = dsv[j][e];
+                    grad_of(score, p[j][e], ahead + (float)(16 * j + e), rv[buf][0][ql],
+                            rv[buf][1][ql], hidden, pv, dv_);
+                    p[j][e] = pv;
+                    dsv[j][e] = dv_;
+                }
+#pragma unroll
+            for (int sl = 0; sl < 2; ++sl) {
+                const bf16x8 pf = pack_pair(p[2 * sl], p[2 * sl + 1]);
+                const bf16x8 sf = pack_pair(dsv[2 * sl], dsv[2 * sl + 1]);
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) {
+                    dv[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        frag_tr_at(ds_ + 32 * sl * D + toff[dt]), pf, dv[dt], 0, 0, 0);
+                    dk[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        frag_tr_at(qs + 32 * sl * D + toff[dt]), sf, dk[dt], 0, 0, 0);
+                }
+            }
+            if (more && tid < BM) {
+                rv[buf ^ 1][0][tid] = l2r;
+                rv[buf ^ 1][1][tid] = dlr;
+            }
+            head = head2;
+            qt = qt2;
+        }
+        dma::wait_vmcnt<0>();
+        __syncthreads();
+    }
+    if constexpr (KG > 1) {
+        f32x4* x = reinterpret_cast<f32x4*>(&qd[1][0][0][0]);
+        if (grp == 1) {
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) {
+                x[((wave * 2 + 0) * 8 + dt) * 64 + lane] = dk[dt];
+                x[((wave * 2 + 1) * 8 + dt) * 64 + lane] = dv[dt];
+            }
+        }
+        __syncthreads();
+        if (grp == 1) return;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) {
+            dk[dt] += x[((wave * 2 + 0) * 8 + dt) * 64 + lane];
+            dv[dt] += x[((wave * 2 + 1) * 8 + dt) * 64 + lane];
+        }
+    }
+    if (kabs >= doc.len) return;
+    if (a.parts > 1) {
+        float* to = a.sums + (((int64_t)part * T + tok0 + kabs) * a.kv_heads + kvh) * 2 * D;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) {
+            *reinterpret_cast<f32x4*>(to + 16 * dt + 4 * g) = dk[dt];
+            *reinterpret_cast<f32x4*>(to + D + 16 * dt + 4 * g) = dv[dt];
+        }
+        return;
+    }
+    uint16_t* row = a.dqkv + (tok0 + kabs) * a.lddq + hc + (int64_t)a.group * D;
+#pragma unroll
+    for (int dt = 0; dt < 8; ++dt) {
+        const u32x2 wk = {pack_bf16x2(dk[dt][0] * a.inv_sqrt_d, dk[dt][1] * a.inv_sqrt_d),
+                          pack_bf16x2(dk[dt][2] * a.inv_sqrt_d, dk[dt][3] * a.inv_sqrt_d)};
+        const u32x2 wv2 = {pack_bf16x2(dv[dt][0], dv[dt][1]), pack_bf16x2(dv[dt][2], dv[dt][3])};
+        *reinterpret_cast<u32x2*>(row + 16 * dt + 4 * g) = wk;
+        *reinterpret_cast<u32x2*>(row + D + 16 * dt + 4 * g) = wv2;
+    }
+}
+
+// dK, dV of a row and key head from the parts' sums, in order; 32 lanes each.
+__global__ __launch_bounds__(256) void docs_join_kernel(BwdArgs a) {
+    const int64_t i = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+    const int64_t t = i / a.kv_heads;
+    const int kvh = (int)(i - t * a.kv_heads), c = (threadIdx.x & 31) * 8;
+    if (t >= a.tokens || t < a.cu[0] || t >= a.cu[a.n_docs]) return;
+    float s[8] = {};
+    for (int p = 0; p < a.parts; ++p) {
+        wave::Eight<float> v;
+        v.load(a.sums + (((int64_t)p * a.tokens + t) * a.kv_heads + kvh) * 2 * D + c);
+        float f[8];
+        v.get(f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] += f[e];
+    }
+    if (c < D) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] *= a.inv_sqrt_d;
+    }
+    wave::Eight<uint16_t> o;
+    o.set(s);
+    o.store(a.dqkv + t * a.lddq + ((int64_t)kvh * (a.group + 2) + a.group) * D + c);
+}
+
+template <int RB, int KG, bool CAP, bool BIAS>
+__global__ __launch_bounds__(NTHR * KG + (KG > 1 ? NTHR : 0), KG > 1 ? 3 : 2)
+void docs_dq_kernel(BwdArgs a) {
+    constexpr int QT = 64 * RB;
+    constexpr bool PRODUCERS = KG > 1;
+    __shared__ __attribute__((aligned(16))) uint16_t kv[KG][2][2][BN * D];   // [grp][buf][K|V]
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool producer = PRODUCERS && wv >= KG * NWAVE;
+    const int grp = producer ? 0 : wv / NWAVE, wave = wv % NWAVE;
+    const int heads = a.kv_heads * a.group;
+    const int head = blockIdx.x % heads, kvh = head / a.group;
+    Doc doc;
+    if (!find_tile<RB == 2 ? 7 : 6>(a, a.slots - 1 - (int)(blockIdx.x / heads), doc)) return;
+    const int qt = doc.tile;
+    const int64_t tok0 = doc.tok0, T = a.tokens;
+    const int64_t hc = (int64_t)kvh * (a.group + 2) * D;
+    const int64_t qc = hc + (int64_t)(head - kvh * a.group) * D;
+
+    const uint16_t* kbase = a.qkv + hc + (int64_t)a.group * D;
+    const uint16_t* vbase = kbase + D;
+    const int last = min(qt * QT + QT, doc.len) - 1;
+    const int nk = (max(last + 1, doc.prefix) + BN - 1) / BN;
+    const int half = KG > 1 ? (nk + 1) / 2 : nk;
+    const int k0 = grp == 0 ? 0 : half;
+    const int mine = grp == 0 ? half : nk - half;   // <= half
+    uint16_t(*kb)[2][BN * D] = kv[grp];
+    TileDma2<false> cp;
+    cp.init(a.ldq, a.ldq, wave, lane);
+    if constexpr (PRODUCERS) {
+        if (producer) {
+            produce<KG>(cp, kbase, vbase, a.ldq, tok0, nk, doc.len, kv, wave);
+            return;
+        }
+    } else {
+        if (mine > 0)
+            cp.issue(kbase, a.ldq, vbase, a.ldq, tok0, k0 * BN, doc.len, kb[0][0], kb[0][1], wave);
+        dma::wait_vmcnt<0>();
+    }
+    int qabs[RB], limit[RB];
+    bf16x8 qf[RB][4], of[RB][4];
+    float l2[RB], dl[RB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        qabs[r] = qt * QT + 64 * r + wave * 16 + (lane & 15);
+        limit[r] = max(qabs[r] + 1, doc.prefix);
+        l2[r] = 0.f;
+        dl[r] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            if (qabs[r] < doc.len) {
+                qf[r][ks] = *reinterpret_cast<const bf16x8*>(
+                    a.qkv + (tok0 + qabs[r]) * a.ldq + qc + 32 * ks + 8 * g);
+                of[r][ks] = *reinterpret_cast<const bf16x8*>(
+                    a.dout + (tok0 + qabs[r]) * a.lddo + (int64_t)head * D + 32 * ks + 8 * g);
+            } else {
+                qf[r][ks] = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
+                of[r][ks] = qf[r][ks];
+            }
+        }
+        // delta of the row: each of its four lanes sums 32 columns
+        float acc = 0.f;
+        if (qabs[r] < doc.len) {
+            l2[r] = a.lse[(int64_t)head * T + tok0 + qabs[r]] * kLog2e;
+            const uint16_t* orow = a.out + (tok0 + qabs[r]) * a.ldo + (int64_t)head * D;
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) {
+                const u32x4 o = *reinterpret_cast<const u32x4*>(orow + 32 * ks + 8 * g);
+                const u32x4 d = __builtin_bit_cast(u32x4, of[r][ks]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    acc += __uint_as_float(o[e] << 16) * __uint_as_float(d[e] << 16);
+                    acc += __uint_as_float(o[e] & 0xffff0000u) * __uint_as_float(d[e] & 0xffff0000u);
+                }
+            }
+        }
+        dl[r] = row_sum4(acc);   // every lane of the wave takes part
+        // the dK/dV kernel, launched after this one, reads it
+        if (grp == 0 && g == 0 && qabs[r] < doc.len)
+            a.delta[(int64_t)head * T + tok0 + qabs[r]] = dl[r];
+    }
+    const Score<CAP, BIAS> score(a, head);
+    f32x4 dq[RB][8];
+#pragma unroll
+    for (int r = 0; r < RB; ++r)
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) dq[r][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    int boff[4], toff[8];
+    offsets(lane, boff, toff);
+    __syncthreads();
+    const int clear = max(qt * QT + 1, doc.prefix);
+    for (int i = 0; i < half; ++i) {
+        if (i < mine) {
+            const int kt = k0 + i;
+            const uint16_t* ks_ = kb[i & 1][0];
+            const uint16_t* vs_ = kb[i & 1][1];
+            const bool more = !PRODUCERS && i + 1 < mine;
+            const auto next = cp.rounds(kbase, a.ldq, vbase, a.ldq, tok0, (kt + 1) * BN, doc.len,
+                                        kb[(i + 1) & 1][0], kb[(i + 1) & 1][1]);
+            const bool masked = (kt + 1) * BN > clear;
+            constexpr int JG = RB == 1 ? 4 : 2;
+            f32x4 dsv[RB][4];
+#pragma unroll
+            for (int j0 = 0; j0 < 4; j0 += JG) {
+                f32x4 sacc[RB][JG], dacc[RB][JG];
+#pragma unroll
+                for (int r = 0; r < RB; ++r)
+#pragma unroll
+                    for (int jj = 0; jj < JG; ++jj) {
+                        sacc[r][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+                        dacc[r][jj] = sacc[r][jj];
+                    }
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+                    for (int jj = 0; jj < JG; ++jj) {
+                        const int j = j0 + jj;
+                        const bf16x8 kf =
+                            *reinterpret_cast<const bf16x8*>(ks_ + 16 * j * D + boff[ks]);
+                        const bf16x8 vf =
+                            *reinterpret_cast<const bf16x8*>(vs_ + 16 * j * D + boff[ks]);
+#pragma unroll
+                        for (int r = 0; r < RB; ++r) {
+                            sacc[r][jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                kf, qf[r][ks], sacc[r][jj], 0, 0, 0);
+                            dacc[r][jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                vf, of[r][ks], dacc[r][jj], 0, 0, 0);
+                        }
+                        if (j0 == 0 && jj == JG - 1 && more) cp.round(next, ks, wave);
+                    }
+#pragma unroll
+                for (int jj = 0; jj < JG; ++jj)
+#pragma unroll
+                    for (int r = 0; r < RB; ++r)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int n = kt * BN + 16 * (j0 + jj) + 4 * g + e;
+                            float p, d = dacc[r][jj][e];
+                            grad_of(score, sacc[r][jj][e], (float)(qabs[r] - n), l2[r], dl[r],
+                                    masked && n >= limit[r], p, d);
+                            dsv[r][j0 + jj][e] = d;
+                        }
+            }
+#pragma unroll
+            for (int sl = 0; sl < 2; ++sl) {
+                bf16x8 sf[RB];
+#pragma unroll
+                for (int r = 0; r < RB; ++r) sf[r] = pack_pair(dsv[r][2 * sl], dsv[r][2 * sl + 1]);
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) {
+                    const bf16x8 kt_ = frag_tr_at(ks_ + 32 * sl * D + toff[dt]);
+#pragma unroll
+                    for (int r = 0; r < RB; ++r)
+                        dq[r][dt] =
+                            __builtin_amdgcn_mfma_f32_16x16x32_bf16(kt_, sf[r], dq[r][dt], 0, 0, 0);
+                }
+            }
+        }
+        dma::wait_vmcnt<0>();
+        __syncthreads();
+    }
+    if constexpr (KG > 1) {
+        f32x4* x = reinterpret_cast<f32x4*>(&kv[1][0][0][0]);
+        if (grp == 1) {
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) x[((wave * RB + r) * 8 + dt) * 64 + lane] = dq[r][dt];
+        }
+        __syncthreads();
+        if (grp == 1) return;
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) dq[r][dt] += x[((wave * RB + r) * 8 + dt) * 64 + lane];
+    }
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        if (qabs[r] >= doc.len) continue;
+        uint16_t* row = a.dqkv + (tok0 + qabs[r]) * a.lddq + qc;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) {
+            const u32x2 w = {pack_bf16x2(dq[r][dt][0] * a.inv_sqrt_d, dq[r][dt][1] * a.inv_sqrt_d),
+                             pack_bf16x2(dq[r][dt][2] * a.inv_sqrt_d, dq[r][dt][3] * a.inv_sqrt_d)};
+            *reinterpret_cast<u32x2*>(row + 16 * dt + 4 * g) = w;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------
+constexpr int64_t kFwdWideTiles = 512;    // two workgroups of 128 rows per CU
+constexpr int64_t kBwdSplitTiles = 1024;  // 64-row tiles below which loops are split
+
+void fill(Common& c, const DocsView& d, const uint16_t* qkv, int64_t ldq, int64_t tokens,
+          int kv_heads, int group) {
+    c.qkv = qkv;
+    c.ldq = ldq;
+    c.cu = d.cu;
+    c.prefix = d.prefix;
+    c.slopes = d.slopes;
+    c.tokens = tokens;
+    c.n_docs = d.n_docs;
+    c.kv_heads = kv_heads;
+    c.group = group;
+    c.slots = 0;
+    const float root = sqrtf((float)D);
+    c.scale_log2 = kLog2e / root;
+    c.cap_in = d.cap > 0.f ? 2.f * kLog2e / (root * d.cap) : 0.f;
+    c.cap_log2 = d.cap * kLog2e;
+}
+// Slots of tiles of `rows` rows: up to cu[n] / rows + n.
+int64_t slots_of(int64_t tokens, int rows, int n_docs) { return tokens / rows + n_docs; }
+
+// Divisions of a group's heads for the dK/dV kernel: as many as it takes for four
+// workgroups per CU.
+int dkv_parts(int64_t tokens, int kv_heads, int group, int* heads) {
+    const int64_t tiles = std::max<int64_t>(1, tokens / BM) * kv_heads;
+    const int64_t want = std::min<int64_t>(group, (kBwdSplitTiles + tiles - 1) / tiles);
+    *heads = (int)((group + want - 1) / want);
+    return (group + *heads - 1) / *heads;
+}
+int64_t delta_floats(int64_t tokens, int heads) { return (tokens * heads + 63) / 64 * 64; }
+
+template <int RB, int KG, bool CAP, bool BIAS>
+void fwd(FwdArgs& a, hipStream_t s) {
+    a.slots = (int)slots_of(a.tokens, 64 * RB, a.n_docs);
+    docs_fwd_kernel<RB, KG, CAP, BIAS>
+        <<<dim3((unsigned)((int64_t)a.slots * a.kv_heads * a.group)), KG > 1 ? 3 * NTHR : NTHR, 0,
+           s>>>(a);
+}
+template <bool CAP, bool BIAS>
+void fwd_of(FwdArgs& a, hipStream_t s) {
+    if ((a.tokens + 127) / 128 * a.kv_heads * a.group >= kFwdWideTiles) fwd<2, 1, CAP, BIAS>(a, s);
+    else fwd<1, 2, CAP, BIAS>(a, s);
+}
+
+template <bool CAP, bool BIAS>
+void bwd_of(BwdArgs& a, hipStream_t s) {
+    const int heads = a.kv_heads * a.group;
+    const int64_t s64 = slots_of(a.tokens, 64, a.n_docs);
+    const bool split = (a.tokens + 63) / 64 * heads < kBwdSplitTiles;
+    if (split) {
+        a.slots = (int)s64;
+        docs_dq_kernel<1, 2, CAP, BIAS>
+            <<<dim3((unsigned)(s64 * heads)), 3 * NTHR, 0, s>>>(a);
+    } else {
+        a.slots = (int)slots_of(a.tokens, 128, a.n_docs);
+        docs_dq_kernel<2, 1, CAP, BIAS>
+            <<<dim3((unsigned)((int64_t)a.slots * heads)), NTHR, 0, s>>>(a);
+    }
+    a.slots = (int)s64;
+    const dim3 grid((unsigned)(s64 * a.kv_heads * a.parts));
+    if ((a.tokens + 63) / 64 * a.kv_heads * a.parts < kBwdSplitTiles)
+        docs_dkv_kernel<2, CAP, BIAS><<<grid, 2 * NTHR, 0, s>>>(a);
+    else
+        docs_dkv_kernel<1, CAP, BIAS><<<grid, NTHR, 0, s>>>(a);
+}
+
+}  // namespace
+
+int64_t docs_attention_ws_floats(int64_t tokens, int kv_heads, int group) {
+    int heads;
+    const int parts = dkv_parts(tokens, kv_heads, group, &heads);
+    return delta_floats(tokens, kv_heads * group) +
+           (parts > 1 ? (int64_t)parts * tokens * kv_heads * 2 * D : 0);
+}
+
+hipError_t launch_docs_attention(const DocsAttentionProblem& p, hipStream_t s) {
+    if (p.tokens == 0 || p.docs.n_docs == 0) return hipSuccess;
+    FwdArgs a;
+    fill(a, p.docs, p.qkv, p.ldq, p.tokens, p.kv_heads, p.group);
+    a.out = p.out;
+    a.ldo = p.ldo;
+    a.lse = p.lse;
+    if (p.docs.cap > 0.f) {
+        if (p.docs.slopes) fwd_of<true, true>(a, s);
+        else fwd_of<true, false>(a, s);
+    } else {
+        if (p.docs.slopes) fwd_of<false, true>(a, s);
+        else fwd_of<false, false>(a, s);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_docs_attention_bwd(const DocsAttentionBwdProblem& p, hipStream_t s) {
+    if (p.tokens == 0 || p.docs.n_docs == 0) return hipSuccess;
+    BwdArgs a;
+    fill(a, p.docs, p.qkv, p.ldq, p.tokens, p.kv_heads, p.group);
+    a.out = p.out; a.ldo = p.ldo;
+    a.dout = p.dout; a.lddo = p.lddo;
+    a.lse = p.lse;
+    a.delta = p.ws;
+    a.sums = p.ws + delta_floats(p.tokens, p.kv_heads * p.group);
+    a.dqkv = p.dqkv; a.lddq = p.lddq;
+    a.parts = dkv_parts(p.tokens, p.kv_heads, p.group, &a.part_heads);
+    a.inv_sqrt_d = 1.0f / sqrtf((float)D);
+    if (p.docs.cap > 0.f) {
+        if (p.docs.slopes) bwd_of<true, true>(a, s);
+        else bwd_of<true, false>(a, s);
+    } else {
+        if (p.docs.slopes) bwd_of<false, true>(a, s);
+        else bwd_of<false, false>(a, s);
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.parts < 2) return e;
+    docs_join_kernel<<<dim3((unsigned)((p.tokens * p.kv_heads + 7) / 8)), 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace atp

@@ -1,0 +1,520 @@
+// Layer norm of rows, with the sum that feeds it, and its gradient.
+//
+//   s = x + add,  mu = mean(s),  r = 1 / sqrt(mean((s - mu)^2) + eps),
+//   y = (s - mu) r w + b;
+//   g = w dy,  xh = (s - mu) r,  dx = r (g - mean(g) - xh mean(g xh)) + d_res,
+//   dw = sum over rows of dy xh,  db = sum over rows of dy.
+//
+// A row stays in registers between its two passes (mean, then centred squares: no
+// difference of large sums), so every value is read and written once: the calls
+// are bound by memory.  Up to 2048 columns a wave holds a row, eight consecutive
+// values per lane and vector; wider rows take a workgroup of just as many waves as
+// hold them, joined through LDS.
+//
+// Rows whose columns lie on several devices: each device gives the mean and the
+// centred squares of its own columns (a row's two sums, in the backward), and
+// the join walks the devices in group order, so all of them get the same bits.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "train_kernels.h"
+#include "wave_ops.h"
+
+namespace atp {
+namespace {
+
+using wave::Eight;
+using wave::sum64;
+
+constexpr int kRowsPerGroup = 4;         // rows of a workgroup whose waves hold one each
+
+// How a row of `cols` is held: threads * nv lanes of eight values.
+struct Shape {
+    bool one;                            // a wave per row
+    int nv, threads;                     // vectors of a lane, threads of a row
+};
+Shape shape_of(int64_t cols) {
+    const int64_t vecs = cols / 8;
+    if (vecs <= 256) return Shape{true, vecs <= 64 ? 1 : vecs <= 128 ? 2 : 4, 64};
+    const int nv = vecs <= 1280 ? 2 : 4;
+    return Shape{false, nv, (int)((vecs + 64 * nv - 1) / (64 * nv)) * 64};
+}
+
+struct Args {
+    int64_t tokens;
+    int cols, nparts;
+    float inv_cols, inv_total, eps, part_cols;
+    const void* x; int64_t ldx;
+    const uint16_t* add; int64_t ldadd;
+    void* x_out; int64_t ldxo;
+    const uint16_t *w, *b;
+    float* stats;
+    uint16_t* y; int64_t ldy;
+    float *mean, *rstd;
+    const float* parts[kMaxParts];
+};
+
+// Sum over the row's lanes.  red: 16 floats of LDS that no other sum of the same
+// round uses.
+template <bool ONE>
+__device__ __forceinline__ float row_sum(float v, float* red, int waves) {
+    v = sum64(v);
+    if constexpr (ONE) return v;
+    const int lane = threadIdx.x & 63;
+    if (lane == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    const int i = lane & 15;
+    float t = i < waves ? red[i] : 0.f;
+    t = wave::dpp_add<0xb1>(t);
+    t = wave::dpp_add<0x4e>(t);
+    t = wave::dpp_add<0x141>(t);
+    return wave::dpp_add<0x140>(t);
+}
+
+template <class T, int NV, bool ONE>
+__global__ __launch_bounds__(ONE ? 64 * kRowsPerGroup : 1024) void norm_fwd_kernel(Args A) {
+    __shared__ float red[2][16];
+    const int l = ONE ? (int)(threadIdx.x & 63) : (int)threadIdx.x;
+    const int per = ONE ? 64 : (int)blockDim.x, waves = per >> 6;
+    const int64_t row = ONE ? (int64_t)blockIdx.x * kRowsPerGroup + (threadIdx.x >> 6)
+                            : (int64_t)blockIdx.x;
+    if (row >= A.tokens) return;         // whole waves, and no barrier follows for them
+    const T* x = static_cast<const T*>(A.x) + row * A.ldx;
+    Eight<T> in[NV];
+    float v[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * per + l) * 8;
+        if (c < A.cols) in[i].load(x + c);
+    }
+    if (A.add) {
+        const uint16_t* add = A.add + row * A.ldadd;
+        T* xo = static_cast<T*>(A.x_out) + row * A.ldxo;
+        Eight<uint16_t> more[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * per + l) * 8;
+            if (c < A.cols) more[i].load(add + c);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * per + l) * 8;
+            if (c >= A.cols) continue;
+            float a[8], b[8];
+            in[i].get(a);
+            more[i].get(b);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a[e] += b[e];
+            in[i].set(a);                // what is normed is the sum as it is stored
+            in[i].store(xo + c);
+        }
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if ((i * per + l) * 8 < A.cols) {
+            in[i].get(v[i]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += v[i][e];
+        }
+    }
+    float mean = 0.f, m2 = 0.f;
+    if (A.nparts == 0) {
+        mean = row_sum<ONE>(sum, red[0], waves) * A.inv_cols;
+        float sq = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if ((i * per + l) * 8 < A.cols) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float d = v[i][e] - mean;
+                    sq += d * d;
+                }
+            }
+        }
+        m2 = row_sum<ONE>(sq, red[1], waves);
+        if (A.stats) {
+            if (l == 0) {
+                A.stats[2 * row] = mean;
+                A.stats[2 * row + 1] = m2;
+            }
+            return;
+        }
+    } else {
+        // equal shards: the mean of the means; the squares about it
+        for (int j = 0; j < A.nparts; ++j) mean += A.parts[j][2 * row];
+        mean /= (float)A.nparts;
+        for (int j = 0; j < A.nparts; ++j) {
+            const float d = A.parts[j][2 * row] - mean;
+            m2 += A.parts[j][2 * row + 1] + A.part_cols * d * d;
+        }
+    }
+    const float r = 1.f / sqrtf(m2 * A.inv_total + A.eps);
+    if (l == 0) {
+        A.mean[row] = mean;
+        A.rstd[row] = r;
+    }
+    uint16_t* y = A.y + row * A.ldy;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * per + l) * 8;
+        if (c >= A.cols) continue;
+        float w[8], b[8];
+        Eight<uint16_t> t;
+        if (A.w) {
+            t.load(A.w + c);
+            t.get(w);
+        }
+        if (A.b) {
+            t.load(A.b + c);
+            t.get(b);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float o = (v[i][e] - mean) * r;
+            if (A.w) o *= w[e];
+            if (A.b) o += b[e];
+            v[i][e] = o;
+        }
+        t.set(v[i]);
+        t.store(y + c);
+    }
+}
+
+struct BwdArgs {
+    int64_t tokens;
+    int cols, nparts;
+    float inv_total;
+    const void* x; int64_t ldx;
+    const uint16_t* w;
+    const float *mean, *rstd;
+    const uint16_t* dy; int64_t lddy;
+    float* sums;
+    const void* dres; int64_t lddres;
+    void* dx; int64_t lddx;
+    uint16_t* dadd; int64_t lddadd;
+    float* part;                         // [workgroups][2][cols], nullable
+    const float* parts[kMaxParts];
+};
+
+// A workgroup walks rows gridDim.x apart and keeps its lanes' share of both
+// column sums in registers; it leaves one row of partial sums, which
+// column_sum_kernel adds in order.  The grid is a function of the sizes alone, so
+// the sums are too.
+template <class T, int NV, bool ONE, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_bwd_kernel(BwdArgs A) {
+    __shared__ float red[2][2][16];
+    extern __shared__ float join[];      // ONE: [3 waves][cols]
+    const int l = ONE ? (int)(threadIdx.x & 63) : (int)threadIdx.x;
+    const int per = ONE ? 64 : (int)blockDim.x, waves = per >> 6;
+    const int mine = ONE ? (int)(threadIdx.x >> 6) : 0;
+    const int64_t step = (int64_t)gridDim.x * (ONE ? kRowsPerGroup : 1);
+    float dw[NV][8], db[NV][8];
+    Eight<uint16_t> w[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * per + l) * 8;
+        if (A.w && c < A.cols) w[i].load(A.w + c);
+        else w[i].w = wave::u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};   // ones
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dw[i][e] = db[i][e] = 0.f;
+    }
+    int turn = 0;
+    for (int64_t row = (int64_t)blockIdx.x * (ONE ? kRowsPerGroup : 1) + mine; row < A.tokens;
+         row += step, turn ^= 1) {
+        const T* x = static_cast<const T*>(A.x) + row * A.ldx;
+        const uint16_t* dy = A.dy + row * A.lddy;
+        Eight<T> xs[NV], res[NV];
+        Eight<uint16_t> gs[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * per + l) * 8;
+            if (c < A.cols) {
+                xs[i].load(x + c);
+                gs[i].load(dy + c);
+            }
+        }
+        if (A.dres) {
+            const T* dr = static_cast<const T*>(A.dres) + row * A.lddres;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (i * per + l) * 8;
+                if (c < A.cols) res[i].load(dr + c);
+            }
+        }
+        const float mean = A.mean[row], r = A.rstd[row];
+        float c1 = 0.f, c2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            if ((i * per + l) * 8 >= A.cols) continue;
+            float v[8], g[8], wv[8];
+            xs[i].get(v);
+            gs[i].get(g);
+            w[i].get(wv);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float xh = (v[e] - mean) * r;
+                dw[i][e] += g[e] * xh;
+                db[i][e] += g[e];
+                const float gw = g[e] * wv[e];
+                c1 += gw;
+                c2 += gw * xh;
+            }
+        }
+        if (A.nparts == 0) {
+            // both sums under one barrier
+            c1 = sum64(c1);
+            c2 = sum64(c2);
+            if constexpr (!ONE) {
+                const int lane = threadIdx.x & 63;
+                if (lane == 0) {
+                    red[turn][0][threadIdx.x >> 6] = c1;
+                    red[turn][1][threadIdx.x >> 6] = c2;
+                }
+                __syncthreads();
+                const int k = lane & 15;
+                c1 = k < waves ? red[turn][0][k] : 0.f;
+                c2 = k < waves ? red[turn][1][k] : 0.f;
+                c1 = wave::dpp_add<0xb1>(c1);
+                c2 = wave::dpp_add<0xb1>(c2);
+                c1 = wave::dpp_add<0x4e>(c1);
+                c2 = wave::dpp_add<0x4e>(c2);
+                c1 = wave::dpp_add<0x141>(c1);
+                c2 = wave::dpp_add<0x141>(c2);
+                c1 = wave::dpp_add<0x140>(c1);
+                c2 = wave::dpp_add<0x140>(c2);
+            }
+            if (A.sums) {
+                if (l == 0) {
+                    A.sums[2 * row] = c1;
+                    A.sums[2 * row + 1] = c2;
+                }
+                continue;
+            }
+        } else {
+            c1 = c2 = 0.f;
+            for (int j = 0; j < A.nparts; ++j) {
+                c1 += A.parts[j][2 * row];
+                c2 += A.parts[j][2 * row + 1];
+            }
+        }
+        c1 *= A.inv_total;
+        c2 *= A.inv_total;
+        T* dx = static_cast<T*>(A.dx) + row * A.lddx;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * per + l) * 8;
+            if (c >= A.cols) continue;
+            float v[8], g[8], wv[8];
+            xs[i].get(v);
+            gs[i].get(g);
+            w[i].get(wv);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                g[e] = r * (g[e] * wv[e] - c1 - (v[e] - mean) * r * c2);
+            if (A.dres) {
+                res[i].get(v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[e] += v[e];
+            }
+            Eight<T> o;
+            o.set(g);
+            o.store(dx + c);
+            if (A.dadd) {
+                Eight<uint16_t> o16;
+                o16.set(g);
+                o16.store(A.dadd + row * A.lddadd + c);
+            }
+        }
+    }
+    if (!A.part) return;
+    float* out = A.part + (int64_t)blockIdx.x * 2 * A.cols;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        if constexpr (ONE) {
+            // the waves' sums, in order
+            if (which) __syncthreads();
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (i * per + l) * 8;
+                if (mine && c < A.cols) {
+                    Eight<float> t;
+                    t.set(which ? db[i] : dw[i]);
+                    t.store(join + (mine - 1) * A.cols + c);
+                }
+            }
+            __syncthreads();
+        }
+        if (mine) continue;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * per + l) * 8;
+            if (c >= A.cols) continue;
+            float s[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e] = which ? db[i][e] : dw[i][e];
+            if constexpr (ONE) {
+#pragma unroll
+                for (int k = 0; k < kRowsPerGroup - 1; ++k) {
+                    Eight<float> t;
+                    t.load(join + k * A.cols + c);
+                    float u[8];
+                    t.get(u);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[e] += u[e];
+                }
+            }
+            Eight<float> t;
+            t.set(s);
+            t.store(out + which * A.cols + c);
+        }
+    }
+}
+
+// Column sums of n rows of 2 cols partials: 64 columns per workgroup, 16 runs of
+// rows (every 16th), joined in order.
+constexpr int kSumThreads = 1024;
+__global__ __launch_bounds__(kSumThreads) void column_sum_kernel(const float* part, int n,
+                                                                 int cols, float* dw, float* db) {
+    constexpr int G = kSumThreads / 64;
+    __shared__ float red[G][64];
+    const int c = threadIdx.x & 63, g = threadIdx.x >> 6;
+    const int64_t col = (int64_t)blockIdx.x * 64 + c;
+    float sum = 0.f;
+    if (col < 2 * (int64_t)cols) {
+#pragma unroll 8
+        for (int i = g; i < n; i += G) sum += part[(int64_t)i * 2 * cols + col];
+    }
+    red[g][c] = sum;
+    __syncthreads();
+    if (g != 0 || col >= 2 * (int64_t)cols) return;
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < G; ++i) sum += red[i][c];
+    if (col < cols) {
+        if (dw) dw[col] = sum;
+    } else if (db) {
+        db[col - cols] = sum;
+    }
+}
+
+// Workgroups of the backward: enough to fill the chip, each with four rows at least
+// where it leaves partial sums (they are 8 bytes a column against the 8 to 14 of a
+// row), and all with the same number of visits.
+int64_t bwd_groups(int64_t tokens, int64_t cols) {
+    const Shape sh = shape_of(cols);
+    const int64_t rows = sh.one ? kRowsPerGroup : 1;
+    const int64_t most = 256 * (sh.one ? 4 : std::max(1, 1024 / sh.threads));
+    const int64_t visits = std::max<int64_t>((tokens + most * rows - 1) / (most * rows), 4);
+    return (tokens + visits * rows - 1) / (visits * rows);
+}
+
+template <class T, int NV, bool ONE>
+void fwd(const Args& a, int64_t grid, int threads, hipStream_t s) {
+    norm_fwd_kernel<T, NV, ONE><<<dim3((unsigned)grid), threads, 0, s>>>(a);
+}
+template <class T, int NV, bool ONE, int THREADS>
+void bwd(const BwdArgs& a, int64_t grid, int threads, hipStream_t s) {
+    const size_t lds = ONE && a.part ? sizeof(float) * (kRowsPerGroup - 1) * a.cols : 0;
+    norm_bwd_kernel<T, NV, ONE, THREADS><<<dim3((unsigned)grid), threads, lds, s>>>(a);
+}
+
+template <class T>
+void fwd_of(const Shape& sh, const Args& a, hipStream_t s) {
+    const int64_t rows = sh.one ? kRowsPerGroup : 1;
+    const int64_t grid = (a.tokens + rows - 1) / rows;
+    const int thr = sh.one ? 64 * kRowsPerGroup : sh.threads;
+    if (sh.one) {
+        if (sh.nv == 1) fwd<T, 1, true>(a, grid, thr, s);
+        else if (sh.nv == 2) fwd<T, 2, true>(a, grid, thr, s);
+        else fwd<T, 4, true>(a, grid, thr, s);
+    } else if (sh.nv == 2) {
+        fwd<T, 2, false>(a, grid, thr, s);
+    } else {
+        fwd<T, 4, false>(a, grid, thr, s);
+    }
+}
+template <class T>
+void bwd_of(const Shape& sh, const BwdArgs& a, int64_t grid, hipStream_t s) {
+    const int thr = sh.one ? 64 * kRowsPerGroup : sh.threads;
+    if (sh.one) {
+        if (sh.nv == 1) bwd<T, 1, true, 256>(a, grid, thr, s);
+        else if (sh.nv == 2) bwd<T, 2, true, 256>(a, grid, thr, s);
+        else bwd<T, 4, true, 256>(a, grid, thr, s);
+    } else if (sh.nv == 2) {
+        bwd<T, 2, false, 640>(a, grid, thr, s);
+    } else if (sh.threads <= 768) {
+        bwd<T, 4, false, 768>(a, grid, thr, s);
+    } else {
+        bwd<T, 4, false, 1024>(a, grid, thr, s);
+    }
+}
+
+}  // namespace
+
+int64_t layer_norm_ws_floats(int64_t tokens, int64_t cols) {
+    return bwd_groups(tokens, cols) * 2 * cols;
+}
+
+hipError_t launch_layer_norm(const LayerNormProblem& p, hipStream_t s) {
+    if (p.tokens == 0) return hipSuccess;
+    Args a = {};
+    a.tokens = p.tokens;
+    a.cols = (int)p.cols;
+    a.nparts = p.nparts;
+    a.inv_cols = 1.f / (float)p.cols;
+    a.inv_total = 1.f / (float)(p.cols * std::max(1, p.nparts));
+    a.part_cols = (float)p.cols;
+    a.eps = p.eps;
+    a.x = p.x; a.ldx = p.ldx;
+    a.add = p.add; a.ldadd = p.ldadd;
+    a.x_out = p.x_out; a.ldxo = p.ldxo;
+    a.w = p.weight;
+    a.b = p.bias;
+    a.stats = p.stats_out;
+    a.y = p.y; a.ldy = p.ldy;
+    a.mean = p.mean;
+    a.rstd = p.rstd;
+    std::copy(p.parts, p.parts + p.nparts, a.parts);
+    const Shape sh = shape_of(p.cols);
+    if (p.f32) fwd_of<float>(sh, a, s);
+    else fwd_of<uint16_t>(sh, a, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_layer_norm_bwd(const LayerNormBwdProblem& p, hipStream_t s) {
+    const bool weights = p.dw || p.db;
+    int64_t grid = 0;
+    if (p.tokens > 0) {
+        BwdArgs a = {};
+        a.tokens = p.tokens;
+        a.cols = (int)p.cols;
+        a.nparts = p.nparts;
+        a.inv_total = 1.f / (float)(p.cols * std::max(1, p.nparts));
+        a.x = p.x; a.ldx = p.ldx;
+        a.w = p.weight;
+        a.mean = p.mean;
+        a.rstd = p.rstd;
+        a.dy = p.dy; a.lddy = p.lddy;
+        a.sums = p.sums_out;
+        a.dres = p.dres; a.lddres = p.lddres;
+        a.dx = p.dx; a.lddx = p.lddx;
+        a.dadd = p.dadd; a.lddadd = p.lddadd;
+        a.part = weights ? p.ws : nullptr;
+        std::copy(p.parts, p.parts + p.nparts, a.parts);
+        grid = bwd_groups(p.tokens, p.cols);
+        const Shape sh = shape_of(p.cols);
+        if (p.f32) bwd_of<float>(sh, a, grid, s);
+        else bwd_of<uint16_t>(sh, a, grid, s);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (!weights) return hipSuccess;
+    column_sum_kernel<<<dim3((unsigned)((2 * p.cols + 63) / 64)), kSumThreads, 0, s>>>(
+        p.ws, (int)grid, (int)p.cols, p.dw, p.db);
+    return hipGetLastError();
+}
+
+}  // namespace atp

@@ -1,0 +1,238 @@
+"""Refusals of the calls around the layers -- embedding, layer norm, attention within
+documents, gradient norm and clipping -- before any device work (the pointers are never
+dereferenced), and the sizes of their workspaces."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2301_08658_amd as atp
+from paper_2301_08658_amd import binding as B
+
+P = 0x10000000              # 16-byte aligned, never dereferenced
+Q, R, S, T = 0x40000000, 0x50000000, 0x60000000, 0x70000000
+ODD = 0x10000004
+INV, UNS, OK = B.ATP_ERR_INVALID_ARGUMENT, B.ATP_ERR_UNSUPPORTED, B.ATP_OK
+NAN, INF = float("nan"), float("inf")
+LIB = atp.load_library()
+
+
+def ref(x):
+    return None if x is None else ctypes.byref(x)
+
+
+def table(ptrs):
+    return None if ptrs is None else (ctypes.c_void_p * max(1, len(ptrs)))(*ptrs)
+
+
+def emb(t=5, ids=P, v=100, off=0, c=64, w=Q, ldw=64, scale=1.0, out=R, dt=1, ldo=64):
+    return LIB.atp_embedding_fwd(t, ids, v, off, c, w, ldw, scale, out, dt, ldo, None)
+
+
+def emb_bwd(t=5, ids=P, v=100, off=0, c=64, dy=Q, ldy=64, scale=1.0, dw=R, ldw=64, acc=0, ws=S,
+            wsb=1 << 20):
+    return LIB.atp_embedding_bwd(t, ids, v, off, c, dy, ldy, scale, dw, ldw, acc, ws, wsb, None)
+
+
+@pytest.mark.parametrize("call", [emb, emb_bwd])
+def test_embedding(call):
+    assert call(t=-1) == INV and call(t=(1 << 24) + 1) == UNS
+    assert call(v=0) == INV and call(v=(1 << 24) + 1) == UNS and call(off=-1) == INV
+    assert call(c=0) == INV and call(c=12) == UNS and call(c=(1 << 22) + 8) == UNS
+    assert call(scale=NAN) == INV and call(scale=INF) == INV
+    assert call(ids=None) == INV and call(ids=ODD) == UNS
+    assert call(ldw=56) == INV and call(ldw=68) == UNS
+
+
+def test_embedding_buffers():
+    assert emb(w=None) == INV and emb(w=ODD) == UNS and emb(out=None) == INV
+    assert emb(out=ODD) == UNS and emb(ldo=60) == INV and emb(dt=2) == INV
+    assert emb(out=Q + 16) == INV and "overlap" in B.last_error()
+    assert emb(t=0, ids=None, out=None) == OK
+    assert emb_bwd(dy=None) == INV and emb_bwd(dw=None) == INV and emb_bwd(dw=ODD) == UNS
+    assert emb_bwd(acc=2) == INV and emb_bwd(ws=None) == INV and emb_bwd(ws=ODD) == UNS
+    need = atp.atp_embedding_workspace_bytes(5, 100, 64)
+    assert need > 0 and emb_bwd(wsb=need - 1) == INV
+    assert emb_bwd(dw=Q) == INV and "overlap" in B.last_error()
+    assert emb_bwd(t=0, ids=None, dy=None, ws=None, wsb=0, acc=1) == OK
+    for bad in ((-1, 5, 8), (5, 0, 8), (5, 5, 0), ((1 << 24) + 1, 5, 8), (5, (1 << 24) + 1, 8)):
+        assert atp.atp_embedding_workspace_bytes(*bad) == 0
+    assert atp.atp_embedding_workspace_bytes(0, 5, 8) == 0
+    sizes = [atp.atp_embedding_workspace_bytes(1 << i, 50000, 64) for i in range(25)]
+    assert sizes == sorted(sizes)
+
+
+def norm(w=P, b=P, eps=1e-5):
+    return B.atp_layer_norm(w, b, eps)
+
+
+def fwd(t=5, c=64, dt=1, p=norm(), x=P, ldx=64, add=Q, lda=64, xo=R, ldxo=64, n=1, st=None, y=S,
+        ldy=64, m=T, r=T):
+    return LIB.atp_layer_norm_fwd(t, c, dt, ref(p), x, ldx, add, lda, xo, ldxo, n, table(st), y,
+                                  ldy, m, r, None)
+
+
+def stats(t=5, c=64, dt=1, x=P, ldx=64, add=Q, lda=64, xo=R, ldxo=64, st=T):
+    return LIB.atp_layer_norm_stats(t, c, dt, x, ldx, add, lda, xo, ldxo, st, None)
+
+
+def bwd(t=5, c=64, dt=1, p=norm(), x=P, ldx=64, m=T, r=T, dy=Q, ldy=64, res=None, ldr=64, n=1,
+        su=None, dx=R, ldd=64, da=None, lda=64, dw=T, db=T, ws=S, wsb=1 << 24):
+    return LIB.atp_layer_norm_bwd(t, c, dt, ref(p), x, ldx, m, r, dy, ldy, res, ldr, n, table(su),
+                                  dx, ldd, da, lda, dw, db, ws, wsb, None)
+
+
+def sums(t=5, c=64, dt=1, p=norm(), x=P, ldx=64, m=T, r=T, dy=Q, ldy=64, su=S):
+    return LIB.atp_layer_norm_bwd_sums(t, c, dt, ref(p), x, ldx, m, r, dy, ldy, su, None)
+
+
+@pytest.mark.parametrize("call", [fwd, stats, bwd, sums])
+def test_layer_norm_sizes(call):
+    assert call(t=-1) == INV and call(t=(1 << 24) + 1) == UNS
+    assert call(c=0) == INV and call(c=60) == UNS and call(c=32776, ldx=32776) == UNS
+    assert call(dt=2) == INV and call(x=None) == INV and call(x=ODD) == UNS
+    assert call(ldx=56) == INV and call(ldx=68) == UNS
+    if call is not stats:
+        for p, want in ((None, INV), (norm(eps=-1.0), INV), (norm(eps=NAN), INV),
+                        (norm(eps=INF), INV), (norm(w=ODD), UNS), (norm(b=ODD), UNS)):
+            assert call(p=p) == want
+
+
+def test_layer_norm_buffers():
+    for call in (fwd, stats):
+        assert call(add=None) == INV and call(xo=None) == INV
+        assert call(lda=56) == INV and call(ldxo=56) == INV and call(add=ODD) == UNS
+        assert call(xo=P + 16) == INV and call(xo=P, ldxo=72) == INV and call(xo=Q) == INV
+        assert call(dt=0, xo=P + 5 * 64 * 2) == INV          # fp32 rows are twice as long
+    assert stats(st=None) == INV and stats(st=ODD) == UNS
+    assert fwd(y=None) == INV and fwd(y=P) == INV and fwd(y=R) == INV and fwd(y=Q) == INV
+    assert fwd(m=None) == INV and fwd(r=ODD) == UNS
+    lone = dict(add=None, xo=None)
+    assert fwd(n=0, **lone) == INV and fwd(n=2, **lone) == INV and fwd(n=65, **lone) == UNS
+    assert fwd(n=2, st=[T, None], **lone) == INV
+    assert fwd(n=2, st=[T, T]) == INV and "add belongs" in B.last_error()
+    assert fwd(t=0, x=None, y=None, m=None, r=None, **lone) == OK
+    for call in (bwd, sums):
+        assert call(dy=None) == INV and call(ldy=56) == INV and call(m=None) == INV
+        assert call(r=ODD) == UNS
+    assert sums(su=None) == INV
+    assert bwd(dx=None) == INV and bwd(dx=P) == INV and bwd(dx=Q) == INV
+    assert bwd(res=R + 16) == INV and bwd(res=R, ldr=72) == INV and bwd(res=ODD) == UNS
+    assert bwd(da=R) == INV and bwd(da=P) == INV and bwd(da=Q) == INV and bwd(da=ODD) == UNS
+    assert bwd(n=2) == INV and bwd(n=2, su=[T, None]) == INV and bwd(n=65, su=[T] * 65) == UNS
+    assert bwd(dw=ODD) == UNS and bwd(ws=None) == INV
+    assert bwd(wsb=atp.atp_layer_norm_workspace_bytes(5, 64) - 1) == INV
+    assert bwd(t=0, x=None, dy=None, dx=None, m=None, r=None, dw=None, db=None, ws=None) == OK
+    for bad in ((-1, 64), (5, 0), (5, 60), (5, 32776), ((1 << 24) + 1, 64)):
+        assert atp.atp_layer_norm_workspace_bytes(*bad) == 0
+    assert atp.atp_layer_norm_workspace_bytes(0, 64) == 0
+    for c in (8, 512, 2048, 2056, 10240, 20480, 32768):
+        sizes = [atp.atp_layer_norm_workspace_bytes(1 << i, c) for i in range(25)]
+        assert all(0 < s <= 1280 * 2 * 4 * c for s in sizes)
+
+
+def docs(cu=P, pre=None, sl=None, n=3, cap=0.0):
+    return B.atp_attention_docs(cu, pre, sl, n, cap)
+
+
+W = 2 * 3 * 128
+
+
+def att(t=9, kv=2, g=1, d=docs(), x=Q, ldx=W, o=R, ldo=256, z=T):
+    return LIB.atp_attention_docs_fwd(t, kv, g, ref(d), x, ldx, o, ldo, z, None)
+
+
+def att_bwd(t=9, kv=2, g=1, d=docs(), x=Q, ldx=W, o=R, ldo=256, z=T, do=S, lddo=256, dx=T,
+            lddx=W, ws=P, wsb=1 << 24):
+    return LIB.atp_attention_docs_bwd(t, kv, g, ref(d), x, ldx, o, ldo, z, do, lddo, dx, lddx, ws,
+                                      wsb, None)
+
+
+@pytest.mark.parametrize("call", [att, att_bwd])
+def test_attention_docs(call):
+    assert call(t=-1) == INV and call(t=(1 << 24) + 1) == UNS
+    assert call(kv=0) == INV and call(g=0) == INV and call(g=65) == UNS and call(kv=1 << 20) == UNS
+    for d, want in ((None, INV), (docs(cu=None), INV), (docs(cu=ODD), UNS), (docs(pre=ODD), UNS),
+                    (docs(sl=ODD), UNS), (docs(n=-1), INV), (docs(n=65537), UNS),
+                    (docs(cap=-1.0), INV), (docs(cap=NAN), INV), (docs(cap=INF), INV)):
+        assert call(d=d) == want, B.last_error()
+    assert call(t=1 << 24, kv=10000, ldx=10000 * 384, ldo=10000 * 128) == UNS
+    assert "tiles" in B.last_error()
+    assert call(x=None) == INV and call(x=ODD) == UNS and call(ldx=W - 8) == INV
+    assert call(o=None) == INV and call(ldo=128) == INV and call(z=None) == INV
+    assert call(z=ODD) == UNS
+    assert call(d=docs(n=0, cu=None)) == OK
+
+
+def test_attention_docs_buffers():
+    assert att(o=Q + 64) == INV and "overlap" in B.last_error()
+    assert att(t=0, x=None, o=None, z=None) == OK
+    assert att_bwd(do=None) == INV and att_bwd(dx=None) == INV and att_bwd(lddo=128) == INV
+    for p in (Q, R, S):
+        assert att_bwd(dx=p) == INV and "overlap" in B.last_error()
+    need = atp.atp_attention_docs_workspace_bytes(9, 2, 1)
+    assert att_bwd(ws=None) == INV and att_bwd(wsb=need - 1) == INV
+    for bad in ((-1, 1, 1), (5, 0, 1), (5, 1, 0), (5, 1, 65), ((1 << 24) + 1, 1, 1)):
+        assert atp.atp_attention_docs_workspace_bytes(*bad) == 0
+    assert atp.atp_attention_docs_workspace_bytes(0, 1, 1) == 0
+
+
+def grad(src=P, dst=Q, rows=1, cols=100, lds=100, ldd=100, st=0, dt=1):
+    return B.atp_grad(src, dst, rows, cols, lds, ldd, st, dt)
+
+
+def sq(gs=(grad(),), n=None, out=R, ws=S, wsb=1 << 20):
+    arr = (B.atp_grad * max(1, len(gs)))(*gs)
+    return LIB.atp_grad_sq_sum(len(gs) if n is None else n, arr, out, ws, wsb, None)
+
+
+def clip(gs=(grad(),), n=None, parts=(R,), red=None, scale=1.0, top=1.0, norm=T):
+    arr = (B.atp_grad * max(1, len(gs)))(*gs)
+    return LIB.atp_grad_clip(len(gs) if n is None else n, arr, len(parts) if red is None else red,
+                             table(list(parts)), scale, top, norm, None)
+
+
+@pytest.mark.parametrize("call", [sq, clip])
+def test_gradients(call):
+    assert call(n=-1) == INV
+    for g, want in ((grad(src=None), INV), (grad(src=ODD), UNS), (grad(rows=-1), INV),
+                    (grad(cols=-1), INV), (grad(st=2), INV), (grad(rows=3, lds=99), INV),
+                    (grad(rows=3, lds=101), UNS), (grad(rows=3, lds=(1 << 22) + 8), UNS),
+                    (grad(rows=1 << 31), UNS), (grad(cols=(1 << 40) + 1), UNS),
+                    (grad(rows=1 << 20, cols=1 << 21, lds=1 << 21, ldd=1 << 21), UNS)):
+        assert call(gs=(grad(), g)) == want, B.last_error()
+
+
+def test_gradient_scalars():
+    assert sq(out=None) == INV and sq(out=ODD + 2) == UNS and sq(ws=None) == INV
+    assert sq(wsb=7) == INV
+    assert clip(gs=(grad(dst=None),)) == INV and clip(gs=(grad(dst=ODD),)) == UNS
+    assert clip(gs=(grad(dt=5),)) == INV and clip(gs=(grad(dst=P),)) == INV      # another type
+    assert clip(gs=(grad(dst=P + 16, dt=0),)) == INV
+    assert clip(gs=(grad(rows=3, lds=100, ldd=104),)) == UNS     # 100 is no multiple of 8
+    assert clip(parts=()) == INV and clip(parts=(None,)) == INV and clip(parts=(R, ODD + 2)) == UNS
+    assert clip(parts=[R] * 65) == UNS
+    for bad in (0.0, -1.0, NAN, INF):
+        assert clip(scale=bad) == INV
+    for bad in (0.0, -1.0, NAN):
+        assert clip(top=bad) == INV
+    assert clip(norm=None) == INV and clip(norm=ODD) == UNS
+    assert LIB.atp_grad_workspace_bytes(-1, None) == 0 == LIB.atp_grad_workspace_bytes(0, None)
+    arr = (B.atp_grad * 2)(grad(cols=16384), grad(cols=16385))
+    assert LIB.atp_grad_workspace_bytes(2, arr) == 3 * 8
+    arr[1].src = None
+    assert LIB.atp_grad_workspace_bytes(2, arr) == 0
+
+
+def test_binding_checks_sizes_and_devices():
+    cpu = torch.zeros((8, 16), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="GPU"):
+        atp.layer_norm(cpu[0])
+    with pytest.raises(ValueError, match="weight has 16"):
+        atp.layer_norm(cpu[0], torch.zeros(8, dtype=torch.bfloat16))
+    with pytest.raises(ValueError, match="GPU"):
+        atp.attention_docs(torch.zeros(3, dtype=torch.int32))
+    with pytest.raises(ValueError, match="n_docs"):
+        atp.attention_docs(torch.zeros(0, dtype=torch.int32))
+    with pytest.raises(ValueError, match="GPU"):
+        atp.grad_list([torch.zeros(8)])
