@@ -141,55 +141,49 @@ __device__ __forceinline__ void scan256(uint32_t* v) {
     for (int i = 0; i < 4; ++i) v[4 * lane + i] = a[i] + incl - s;
 }
 
-// All tokens in one workgroup: rows and indices packed into 32 bits, sorted in LDS.
-// `shift` bits hold the index.
-template <int ROUNDS>
-__global__ __launch_bounds__(kSortThreads) void sort_small_kernel(
-    const int32_t* ids, int n, int64_t off, int64_t vocab, int shift, int key_bits, uint32_t* keys,
-    uint32_t* order) {
-    constexpr int N = ROUNDS * kSortThreads;
-    __shared__ uint32_t items[N];
-    __shared__ uint32_t count[kSortWaves][kDigits];
-    __shared__ uint32_t base[kDigits];
+// Few tokens: a token's place is the number of tokens before it in the order of
+// (row, index), counted.  A workgroup places TOK tokens; its waves divide the others,
+// 64 per register, and compare them with one token at a time (one comparison and a
+// count of its bits per 64 pairs).
+constexpr int kCountMax = 16384;
+template <class K, int REGS, int TOK>
+__global__ __launch_bounds__(kSortThreads) void sort_few_kernel(const int32_t* ids, int n,
+                                                                int64_t off, int64_t vocab,
+                                                                int shift, uint32_t* keys,
+                                                                uint32_t* order) {
+    __shared__ uint32_t place[kSortWaves][TOK];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    uint32_t it[ROUNDS], rank[ROUNDS];
+    auto item = [&](int t) -> K {
+        return t < n ? ((K)key_of(ids, t, off, vocab) << shift) | (K)t : ~(K)0;
+    };
+    const int t = blockIdx.x * TOK + lane;           // the tokens placed here, one per lane
+    const K own = item(t);
+    K other[REGS];
 #pragma unroll
-    for (int r = 0; r < ROUNDS; ++r) {
-        const int t = (w * ROUNDS + r) * 64 + lane;
-        it[r] = t < n ? (key_of(ids, t, off, vocab) << shift) | (uint32_t)t : 0xffffffffu;
+    for (int i = 0; i < REGS; ++i) other[i] = item((w * REGS + i) * 64 + lane);
+    uint32_t found = 0;
+#pragma unroll 8
+    for (int k = 0; k < TOK; ++k) {
+        K one;
+        if constexpr (sizeof(K) == 8)
+            one = (K)(uint32_t)__builtin_amdgcn_readlane((int)own, k) |
+                  (K)(uint32_t)__builtin_amdgcn_readlane((int)(own >> 32), k) << 32;
+        else
+            one = (K)__builtin_amdgcn_readlane((int)own, k);
+        uint32_t c = 0;
+#pragma unroll
+        for (int i = 0; i < REGS; ++i)
+            c += __popcll(__builtin_amdgcn_ballot_w64(other[i] < one));
+        found = lane == k ? c : found;
     }
-    for (int done = 0; done < key_bits; done += 8) {
-        ranks<ROUNDS>(it, shift + done, rank, count);
-        if (threadIdx.x < kDigits) {
-            uint32_t s = 0;
+    if (lane < TOK) place[w][lane] = found;
+    __syncthreads();
+    if (w != 0 || lane >= TOK || t >= n) return;
+    uint32_t at = 0;
 #pragma unroll
-            for (int k = 0; k < kSortWaves; ++k) {
-                const uint32_t c = count[k][threadIdx.x];
-                count[k][threadIdx.x] = s;
-                s += c;
-            }
-            base[threadIdx.x] = s;
-        }
-        __syncthreads();
-        if (w == 0) scan256(base);
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < ROUNDS; ++r) {
-            const uint32_t d = digit_of(it[r], shift + done);
-            items[base[d] + count[w][d] + rank[r]] = it[r];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < ROUNDS; ++r) it[r] = items[(w * ROUNDS + r) * 64 + lane];
-    }
-#pragma unroll
-    for (int r = 0; r < ROUNDS; ++r) {
-        const int t = (w * ROUNDS + r) * 64 + lane;
-        if (t >= n) continue;
-        const uint32_t key = it[r] >> shift;
-        keys[t] = key;
-        order[t] = it[r] & ((1u << shift) - 1);
-    }
+    for (int i = 0; i < kSortWaves; ++i) at += place[i][lane];
+    keys[at] = (uint32_t)(own >> shift);
+    order[at] = (uint32_t)t;
 }
 
 // More tokens: tiles of kTile, a pass of eight bits in three launches.
@@ -283,6 +277,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(PassArgs A) {
 struct SumArgs {
     const uint32_t *keys, *order;
     int n, chunk, chunks, col_blocks;
+    int lanes;                           // of a workgroup's 256 that take one chunk
     int64_t vocab;
     int cols;
     const uint16_t* dy; int64_t lddy;
@@ -291,7 +286,7 @@ struct SumArgs {
     float* part;                         // [chunks][2][cols]: a run from the chunk before, one
                                          // that goes on in the next
     int accumulate;
-    int fill_rows;                       // rows of a workgroup that writes zeros (at most 64)
+    int fill_rows;                       // rows of a wave that writes zeros
 };
 
 __device__ __forceinline__ void add_row(float (&s)[8], const float* v) {
@@ -313,39 +308,40 @@ __device__ __forceinline__ void put_row(const SumArgs& A, uint32_t key, int c, f
     o.store(to);
 }
 
-// Zeros for the rows that no token names: lane i of every wave looks row i up.
+// Zeros for the rows that no token names: a wave looks its rows up one by one, 64
+// probes at a time.
 __device__ __forceinline__ void fill(const SumArgs& A, int64_t r0) {
     const int lane = threadIdx.x & 63;
-    const int64_t r = r0 + lane;
-    bool empty = false;
-    if (lane < A.fill_rows && r < A.vocab) {
-        int lo = 0, hi = A.n;
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (A.keys[mid] < (uint32_t)r) lo = mid + 1;
-            else hi = mid;
+    const wave::f32x4 z = {0.f, 0.f, 0.f, 0.f};
+    for (int64_t r = r0; r < r0 + A.fill_rows && r < A.vocab; ++r) {
+        int lo = 0, len = A.n;           // the first key >= r is in [lo, lo + len]
+        while (len > 0) {
+            const int step = (len + 63) >> 6;
+            const int i = lane * step;
+            const bool less = i < len && A.keys[lo + i] < (uint32_t)r;
+            const int c = __popcll(__builtin_amdgcn_ballot_w64(less));
+            if (c == 0) break;
+            const int skip = (c - 1) * step + 1;
+            lo += skip;
+            len = min(step - 1, len - skip);
         }
-        empty = lo == A.n || A.keys[lo] != (uint32_t)r;
-    }
-    uint64_t rows = __builtin_amdgcn_ballot_w64(empty);
-    Eight<float> z;
-    z.a = z.b = wave::f32x4{0.f, 0.f, 0.f, 0.f};
-    while (rows) {
-        const int i = __builtin_ctzll(rows);
-        rows &= rows - 1;
-        float* to = A.dtable + (r0 + i) * A.ldt;
-        for (int c = threadIdx.x * 8; c < A.cols; c += blockDim.x * 8) z.store(to + c);
+        if (lo < A.n && A.keys[lo] == (uint32_t)r) continue;
+        float* to = A.dtable + r * A.ldt;
+#pragma unroll 4
+        for (int c = lane * 4; c < A.cols; c += 256) *reinterpret_cast<wave::f32x4*>(to + c) = z;
     }
 }
 
-__global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs A) {
-    const int64_t work = (int64_t)A.chunks * A.col_blocks;
+__global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs A, int64_t work) {
     if (blockIdx.x >= work) {
-        fill(A, ((int64_t)blockIdx.x - work) * A.fill_rows);
+        fill(A, (((int64_t)blockIdx.x - work) * 4 + threadIdx.x / 64) * A.fill_rows);
         return;
     }
-    const int ch = (int)(blockIdx.x / A.col_blocks);
-    const int c = ((int)(blockIdx.x % A.col_blocks) * (int)blockDim.x + (int)threadIdx.x) * 8;
+    const int ch = __builtin_amdgcn_readfirstlane(
+        (int)(blockIdx.x / A.col_blocks) * (256 / A.lanes) + (int)threadIdx.x / A.lanes);
+    if (ch >= A.chunks) return;
+    const int c =
+        ((int)(blockIdx.x % A.col_blocks) * A.lanes + (int)threadIdx.x % A.lanes) * 8;
     if (c >= A.cols) return;
     const int p0 = ch * A.chunk, p1 = min(p0 + A.chunk, A.n);
     const uint32_t none = (uint32_t)A.vocab;
@@ -403,8 +399,10 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs A) {
 
 // Runs that cross chunks, by the chunk that they begin in.
 __global__ __launch_bounds__(256) void embed_join_kernel(SumArgs A) {
-    const int ch = (int)(blockIdx.x / A.col_blocks);
-    const int c = ((int)(blockIdx.x % A.col_blocks) * (int)blockDim.x + (int)threadIdx.x) * 8;
+    const int ch = __builtin_amdgcn_readfirstlane(
+        (int)(blockIdx.x / A.col_blocks) * (256 / A.lanes) + (int)threadIdx.x / A.lanes);
+    const int c =
+        ((int)(blockIdx.x % A.col_blocks) * A.lanes + (int)threadIdx.x % A.lanes) * 8;
     const int p0 = ch * A.chunk, p1 = p0 + A.chunk;
     if (p1 >= A.n) return;
     const uint32_t k = A.keys[p1 - 1];
@@ -435,7 +433,8 @@ __global__ __launch_bounds__(256) void embed_join_kernel(SumArgs A) {
 
 // ------------------------------------------------------------------ plan
 struct Plan {
-    int key_bits, idx_bits, rounds;      // rounds > 0: one workgroup sorts
+    int key_bits;
+    bool few;                            // places are counted
     int tiles, chunk, chunks;
     int64_t keys, order, keys2, order2, hist, part, bytes;
 };
@@ -444,17 +443,11 @@ int bit_length(uint64_t v) { return v ? 64 - __builtin_clzll(v) : 0; }
 Plan plan_of(int64_t n, int64_t vocab, int64_t cols) {
     Plan p = {};
     p.key_bits = bit_length((uint64_t)vocab);
-    for (int r = 4; r <= 16; r *= 2) {
-        const int bits = bit_length((uint64_t)r * kSortThreads - 1);
-        if (n <= (int64_t)r * kSortThreads && bits + p.key_bits <= 32) {
-            p.rounds = r;
-            p.idx_bits = bits;
-            break;
-        }
-    }
+    p.few = n <= kCountMax;
     p.tiles = (int)((n + kTile - 1) / kTile);
-    // chunks of 32 tokens, longer ones where that makes more than 2048
-    p.chunk = (int)std::max<int64_t>(32, (n / 2048 + 31) / 32 * 32);
+    // chunks of 8 tokens for the smallest calls, which have too few, to 32; longer ones
+    // where that makes more than 2048
+    p.chunk = (int)(n < 1024 ? 8 : n < 4096 ? 16 : std::max<int64_t>(32, (n / 2048 + 31) / 32 * 32));
     p.chunks = (int)((n + p.chunk - 1) / p.chunk);
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
@@ -464,7 +457,7 @@ Plan plan_of(int64_t n, int64_t vocab, int64_t cols) {
     };
     p.keys = take(4 * n);
     p.order = take(4 * n);
-    if (!p.rounds) {
+    if (!p.few) {
         p.keys2 = take(4 * n);
         p.order2 = take(4 * n);
         p.hist = take(4 * (int64_t)kDigits * p.tiles);
@@ -474,12 +467,20 @@ Plan plan_of(int64_t n, int64_t vocab, int64_t cols) {
     return p;
 }
 
-template <int ROUNDS>
-hipError_t sort_small(const EmbeddingBwdProblem& p, const Plan& f, uint32_t* keys, uint32_t* order,
-                      hipStream_t s) {
-    sort_small_kernel<ROUNDS><<<1, kSortThreads, 0, s>>>(p.ids, (int)p.tokens, p.off, p.vocab,
-                                                           f.idx_bits, f.key_bits, keys, order);
-    return hipGetLastError();
+// Tokens of a workgroup: 16, so that 4096 tokens take every CU.
+template <class K, int REGS, int TOK>
+void few(const EmbeddingBwdProblem& p, int shift, uint32_t* keys, uint32_t* order, hipStream_t s) {
+    sort_few_kernel<K, REGS, TOK>
+        <<<dim3((unsigned)((p.tokens + TOK - 1) / TOK)), kSortThreads, 0, s>>>(
+            p.ids, (int)p.tokens, p.off, p.vocab, shift, keys, order);
+}
+template <class K>
+void few_of(const EmbeddingBwdProblem& p, int shift, uint32_t* keys, uint32_t* order,
+            hipStream_t s) {
+    if (p.tokens <= 1024) few<K, 1, 16>(p, shift, keys, order, s);
+    else if (p.tokens <= 4096) few<K, 4, 16>(p, shift, keys, order, s);
+    else if (p.tokens <= 8192) few<K, 8, 32>(p, shift, keys, order, s);
+    else few<K, 16, 64>(p, shift, keys, order, s);
 }
 
 }  // namespace
@@ -512,10 +513,11 @@ hipError_t launch_embedding_bwd(const EmbeddingBwdProblem& p, hipStream_t s) {
     auto u32 = [&](int64_t at) { return reinterpret_cast<uint32_t*>(ws + at); };
     uint32_t *keys = u32(f.keys), *order = u32(f.order);
     hipError_t e = hipSuccess;
-    if (p.tokens > 0 && f.rounds) {
-        e = f.rounds == 4 ? sort_small<4>(p, f, keys, order, s)
-            : f.rounds == 8 ? sort_small<8>(p, f, keys, order, s)
-                             : sort_small<16>(p, f, keys, order, s);
+    if (p.tokens > 0 && f.few) {
+        const int idx = bit_length((uint64_t)p.tokens);      // one more than the last index
+        if (idx + f.key_bits <= 32) few_of<uint32_t>(p, idx, keys, order, s);
+        else few_of<uint64_t>(p, idx, keys, order, s);
+        e = hipGetLastError();
         if (e != hipSuccess) return e;
     } else if (p.tokens > 0) {
         PassArgs a = {};
@@ -554,17 +556,20 @@ hipError_t launch_embedding_bwd(const EmbeddingBwdProblem& p, hipStream_t s) {
     a.dtable = p.dtable; a.ldt = p.ldt;
     a.part = reinterpret_cast<float*>(ws + f.part);
     a.accumulate = p.accumulate;
-    const int vecs = a.cols / 8, thr = std::min(256, (vecs + 63) / 64 * 64);
-    a.col_blocks = (vecs + thr - 1) / thr;
-    // a quarter of a megabyte of zeros per workgroup
-    a.fill_rows = (int)std::min<int64_t>(64, std::max<int64_t>(1, 65536 / p.cols));
-    const int64_t work = (int64_t)f.chunks * a.col_blocks;
-    const int64_t fills = p.accumulate ? 0 : (p.vocab + a.fill_rows - 1) / a.fill_rows;
+    const int vecs = a.cols / 8;
+    a.lanes = vecs <= 64 ? 64 : vecs <= 128 ? 128 : 256;
+    a.col_blocks = (vecs + a.lanes - 1) / a.lanes;
+    // rows of zeros for 16 waves per CU, more than one each where there are more rows
+    a.fill_rows = (int)std::min<int64_t>(16, (p.vocab + 4095) / 4096);
+    const int per = 256 / a.lanes;
+    const int64_t work = (int64_t)(f.chunks + per - 1) / per * a.col_blocks;
+    const int64_t fills =
+        p.accumulate ? 0 : (p.vocab + 4 * a.fill_rows - 1) / (4 * a.fill_rows);
     if (work + fills == 0) return hipSuccess;
-    embed_sum_kernel<<<dim3((unsigned)(work + fills)), thr, 0, s>>>(a);
+    embed_sum_kernel<<<dim3((unsigned)(work + fills)), 256, 0, s>>>(a, work);
     e = hipGetLastError();
     if (e != hipSuccess || f.chunks < 2) return e;
-    embed_join_kernel<<<dim3((unsigned)work), thr, 0, s>>>(a);
+    embed_join_kernel<<<dim3((unsigned)work), 256, 0, s>>>(a);
     return hipGetLastError();
 }
 

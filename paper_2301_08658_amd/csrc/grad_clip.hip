@@ -8,9 +8,10 @@
 // 16384 consecutive values of one tensor and leaves one partial sum; the partial
 // sums are added in a fixed order.  Bound by memory: the gradients are read once
 // for the norm, and once more, with one write, for the clipping, which cannot begin
-// before the norm is known.  The list of tensors travels in the kernels' arguments
-// (a launch takes as many tensors as fit 4 KiB), so a call keeps nothing and can be
-// captured.
+// before the norm is known.  The list of tensors travels in the kernels' arguments,
+// as many per launch as 4 KiB hold (250 for the sum, 160 for the clipping), so a call
+// keeps nothing and can be captured; with one list of 72 entries for all uses 300
+// tensors took 64 us, in 11 launches.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -26,31 +27,77 @@ using wave::Eight;
 
 constexpr int kThreads = 256;
 constexpr int kVecs = 8;                             // vectors of eight values per thread
-constexpr int64_t kSpan = (int64_t)kThreads * kVecs * 8;
+constexpr int kGroupVecs = kThreads * kVecs;         // of a workgroup
+constexpr int64_t kMaxRun = 1 << 30;                 // values of a run; longer ones are cut
 
-// One tensor of a launch: rows of `cols` values, or one run of them.  Bit 0 of the
-// pointers (16-byte aligned) says whether the values are fp32.
-struct Item {
-    uint64_t src, dst;
-    int64_t cols;
-    int32_t ld_src, ld_dst, rows, first;             // first: its first workgroup in the launch
-};
-constexpr int kItems = 72;
-struct Items {
-    Item t[kItems];
-    int n;
+// Tensors of a launch: runs of consecutive values (kRuns without a destination), or
+// matrices with gaps between their rows.  Bit 0 of the pointers (16-byte aligned) says
+// whether the values are fp32.
+enum Kind { kRuns, kRunsTo, kRowsTo };
+template <Kind K, int N>
+struct List {
+    static constexpr Kind kind = K;
+    static constexpr int kMost = N;
+    int32_t n;
+    int32_t first[N];                                // first workgroup of each
+    uint64_t src[N], dst[K == kRuns ? 1 : N];
+    int64_t cols[K == kRowsTo ? N : 1];
+    uint32_t run[K == kRowsTo ? 1 : N];
+    int32_t rows[K == kRowsTo ? N : 1], ld_src[K == kRowsTo ? N : 1], ld_dst[K == kRowsTo ? N : 1];
 };
 
-// Item and span of this workgroup.
-__device__ __forceinline__ int find(const Items& L, int block) {
-    int lo = 0, hi = L.n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (L.t[mid].first <= block) lo = mid;
-        else hi = mid - 1;
+// The tensor of a workgroup, the last one that begins at or before it: 64 entries at a
+// time.
+template <class L>
+__device__ __forceinline__ int find(const L& list, int block) {
+    const int lane = threadIdx.x & 63;
+    int at = -1;
+#pragma unroll
+    for (int i = 0; i < (L::kMost + 63) / 64; ++i) {
+        const int k = i * 64 + lane;
+        at += __popcll(__builtin_amdgcn_ballot_w64(k < list.n && list.first[k] <= block));
     }
-    return lo;
+    return __builtin_amdgcn_readfirstlane(at);
 }
+
+// Where the thread's vectors of eight values lie: vector i in row `row` from value `col`.
+template <Kind K>
+struct Places {
+    int64_t cols, row0;
+    int32_t rows, ld_src, ld_dst;
+    uint32_t rem, per;                               // of the workgroup's first vector, per row
+    template <class L>
+    __device__ __forceinline__ Places(const L& list, int t, int block) {
+        const int64_t vec0 = (int64_t)(block - list.first[t]) * kGroupVecs;
+        if constexpr (K == kRowsTo) {
+            cols = list.cols[t];
+            rows = list.rows[t];
+            ld_src = list.ld_src[t];
+            ld_dst = list.ld_dst[t];
+            per = (uint32_t)((cols + 7) >> 3);       // a row with gaps has at most 2^22 values
+            row0 = vec0 / per;
+            rem = (uint32_t)(vec0 - row0 * per);
+        } else {
+            cols = list.run[t];
+            row0 = vec0 * 8;                         // the first value
+        }
+    }
+    struct At {
+        int64_t row, col;
+        bool in;
+    };
+    __device__ __forceinline__ At at(int i) const {
+        const uint32_t v = i * kThreads + threadIdx.x;
+        if constexpr (K == kRowsTo) {
+            const uint32_t down = (rem + v) / per;
+            const int64_t row = row0 + down;
+            return At{row, (int64_t)(rem + v - down * per) * 8, row < rows};
+        } else {
+            const int64_t col = row0 + (int64_t)v * 8;
+            return At{0, col, col < cols};
+        }
+    }
+};
 
 // Values [c, c + 8) of a row, zeros behind its end.
 template <class T>
@@ -88,21 +135,6 @@ __device__ __forceinline__ void store8(T* row, int64_t c, int64_t cols, const fl
         }
 }
 
-// Row and column of vector i of the workgroup's span `at` (in vectors): a run of
-// vectors for one row, rows one behind the other for several.
-struct Place {
-    int64_t row, col;
-    bool in;
-};
-__device__ __forceinline__ Place place(const Item& it, int64_t vec) {
-    const int64_t per = (it.cols + 7) >> 3;
-    Place p;
-    p.row = it.rows == 1 ? 0 : vec / per;
-    p.col = (vec - p.row * per) * 8;
-    p.in = p.row < it.rows && p.col < it.cols;
-    return p;
-}
-
 __device__ __forceinline__ double block_sum(double v, double* red) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
@@ -114,15 +146,14 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
     return v;
 }
 
-template <class T>
-__device__ __forceinline__ double squares(const Item& it, int64_t vec0) {
-    const T* src = reinterpret_cast<const T*>(it.src & ~(uint64_t)15);
+template <class T, Kind K>
+__device__ __forceinline__ double squares(const T* src, const Places<K>& p) {
     Eight<T> in[kVecs];
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-        const Place p = place(it, vec0 + i * kThreads + threadIdx.x);
+        const auto a = p.at(i);
         float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (p.in) in[i] = load8(src + p.row * it.ld_src, p.col, it.cols);
+        if (a.in) in[i] = load8(K == kRowsTo ? src + a.row * p.ld_src : src, a.col, p.cols);
         else in[i].set(z);
     }
     double s = 0.0;
@@ -136,11 +167,19 @@ __device__ __forceinline__ double squares(const Item& it, int64_t vec0) {
     return s;
 }
 
-__global__ __launch_bounds__(kThreads) void sq_sum_kernel(Items L, double* part) {
+template <class T>
+__device__ __forceinline__ T* pointer(uint64_t p) {
+    return reinterpret_cast<T*>(p & ~(uint64_t)15);
+}
+
+template <class L>
+__global__ __launch_bounds__(kThreads) void sq_sum_kernel(L list, double* part) {
     __shared__ double red[kThreads / 64];
-    const Item& it = L.t[find(L, blockIdx.x)];
-    const int64_t vec0 = (int64_t)((int)blockIdx.x - it.first) * (kThreads * kVecs);
-    double s = it.src & 1 ? squares<float>(it, vec0) : squares<uint16_t>(it, vec0);
+    const int t = find(list, blockIdx.x);
+    const Places<L::kind> p(list, t, blockIdx.x);
+    const uint64_t src = list.src[t];
+    double s = src & 1 ? squares(pointer<const float>(src), p)
+                       : squares(pointer<const uint16_t>(src), p);
     s = block_sum(s, red);
     if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
@@ -156,117 +195,173 @@ __global__ __launch_bounds__(kJoinThreads) void sq_join_kernel(const double* par
     if (threadIdx.x == 0) *sum = s;
 }
 
+template <int N>
 struct Factor {
-    const double* parts[kMaxParts];
+    const double* parts[N];
     int nparts;
     float scale, max_norm;
-};
-struct ClipArgs {
-    Items L;
     float* norm;                                     // in the first launch: norm and factor
 };
-static_assert(sizeof(ClipArgs) + sizeof(Factor) <= 4096, "kernel arguments");
 
-template <class S, class T>
-__device__ __forceinline__ void scaled(const Item& it, int64_t vec0, float f) {
-    const S* src = reinterpret_cast<const S*>(it.src & ~(uint64_t)15);
-    T* dst = reinterpret_cast<T*>(it.dst & ~(uint64_t)15);
+template <class S, class T, Kind K>
+__device__ __forceinline__ void scaled(const S* src, T* dst, const Places<K>& p, float f) {
     Eight<S> in[kVecs];
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-        const Place p = place(it, vec0 + i * kThreads + threadIdx.x);
-        if (p.in) in[i] = load8(src + p.row * it.ld_src, p.col, it.cols);
+        const auto a = p.at(i);
+        if (a.in) in[i] = load8(K == kRowsTo ? src + a.row * p.ld_src : src, a.col, p.cols);
     }
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-        const Place p = place(it, vec0 + i * kThreads + threadIdx.x);
-        if (!p.in) continue;
+        const auto a = p.at(i);
+        if (!a.in) continue;
         float v[8];
         in[i].get(v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= f;
-        store8(dst + p.row * it.ld_dst, p.col, it.cols, v);
+        store8(K == kRowsTo ? dst + a.row * p.ld_dst : dst, a.col, p.cols, v);
     }
 }
 
-__global__ __launch_bounds__(kThreads) void clip_kernel(ClipArgs A, Factor F) {
+template <class L, int N>
+__global__ __launch_bounds__(kThreads) void clip_kernel(L list, Factor<N> F) {
     // every workgroup adds the devices' sums, in group order
     double s = 0.0;
     for (int j = 0; j < F.nparts; ++j) s += *F.parts[j];
     const double norm = (double)F.scale * sqrt(s);
     const float f = (float)((double)F.scale *
                             (norm <= (double)F.max_norm ? 1.0 : (double)F.max_norm / norm));
-    if (A.norm && blockIdx.x == 0 && threadIdx.x == 0) {
-        A.norm[0] = (float)norm;
-        A.norm[1] = f;
+    if (F.norm && blockIdx.x == 0 && threadIdx.x == 0) {
+        F.norm[0] = (float)norm;
+        F.norm[1] = f;
     }
-    if (A.L.n == 0) return;
-    const Item& it = A.L.t[find(A.L, blockIdx.x)];
-    if (f == 1.f && it.src == it.dst && it.ld_src == it.ld_dst) return;    // in place already
-    const int64_t vec0 = (int64_t)((int)blockIdx.x - it.first) * (kThreads * kVecs);
-    if (it.src & 1) {
-        if (it.dst & 1) scaled<float, float>(it, vec0, f);
-        else scaled<float, uint16_t>(it, vec0, f);
+    if (list.n == 0) return;
+    const int t = find(list, blockIdx.x);
+    const Places<L::kind> p(list, t, blockIdx.x);
+    const uint64_t src = list.src[t], dst = list.dst[t];
+    if (f == 1.f && src == dst) return;              // in place already
+    if (src & 1) {
+        const float* from = pointer<const float>(src);
+        if (dst & 1) scaled(from, pointer<float>(dst), p, f);
+        else scaled(from, pointer<uint16_t>(dst), p, f);
     } else {
-        if (it.dst & 1) scaled<uint16_t, float>(it, vec0, f);
-        else scaled<uint16_t, uint16_t>(it, vec0, f);
+        const uint16_t* from = pointer<const uint16_t>(src);
+        if (dst & 1) scaled(from, pointer<float>(dst), p, f);
+        else scaled(from, pointer<uint16_t>(dst), p, f);
     }
 }
 
-// The tensors as items: rows without gaps are one run.
-struct Run {
-    int64_t rows, cols, ld_src, ld_dst;
-};
-Run run_of(const GradView& g, bool with_dst) {
-    const bool flat = g.rows <= 1 || (g.ld_src == g.cols && (!with_dst || g.ld_dst == g.cols));
-    return flat ? Run{g.rows > 0 ? 1 : 0, g.rows * g.cols, 0, 0}
-                : Run{g.rows, g.cols, g.ld_src, g.ld_dst};
+// Rows without gaps are one run.
+bool is_run(const GradView& g, bool with_dst) {
+    return g.rows <= 1 || (g.ld_src == g.cols && (!with_dst || g.ld_dst == g.cols));
 }
-int64_t blocks_of(const Run& r) {
-    if (r.rows == 0 || r.cols == 0) return 0;
-    return (r.rows * ((r.cols + 7) / 8) * 8 + kSpan - 1) / kSpan;
+int64_t row_blocks(int64_t rows, int64_t cols) {
+    return (rows * ((cols + 7) / 8) + kGroupVecs - 1) / kGroupVecs;
 }
-
-// Calls f(items, workgroups) for every launch.
-template <class F>
-hipError_t in_launches(int n, const GradView* g, bool with_dst, F&& f) {
-    Items L;
-    L.n = 0;
+int64_t blocks_of(const GradView& g) {
+    if (g.rows == 0 || g.cols == 0) return 0;
+    if (!is_run(g, false)) return row_blocks(g.rows, g.cols);
     int64_t blocks = 0;
-    for (int i = 0; i < n; ++i) {
-        const Run r = run_of(g[i], with_dst);
-        const int64_t b = blocks_of(r);
-        if (b == 0) continue;
-        if (L.n == kItems || blocks + b > 0x7fffffff) {
-            const hipError_t e = f(L, blocks);
-            if (e != hipSuccess) return e;
-            L.n = 0;
-            blocks = 0;
-        }
-        Item& t = L.t[L.n++];
-        t.src = reinterpret_cast<uint64_t>(g[i].src) | (g[i].src_f32 ? 1 : 0);
-        t.dst = reinterpret_cast<uint64_t>(g[i].dst) | (g[i].dst_f32 ? 1 : 0);
-        t.cols = r.cols;
-        t.ld_src = (int32_t)r.ld_src;
-        t.ld_dst = (int32_t)r.ld_dst;
-        t.rows = (int32_t)r.rows;
-        t.first = (int32_t)blocks;
-        blocks += b;
+    for (int64_t left = g.rows * g.cols; left > 0; left -= kMaxRun)
+        blocks += row_blocks(1, std::min(left, kMaxRun));
+    return blocks;
+}
+
+// Collects entries of one kind and calls f(list, workgroups) for every full one.
+template <class L, class F>
+struct Launches {
+    L list;
+    int64_t blocks = 0;
+    F f;
+    hipError_t e = hipSuccess;
+    explicit Launches(F f_) : f(f_) { list.n = 0; }
+    void flush() {
+        if (list.n && e == hipSuccess) e = f(list, blocks);
+        list.n = 0;
+        blocks = 0;
     }
-    return L.n ? f(L, blocks) : hipSuccess;
+    // the next entry's place; b: its workgroups
+    int next(int64_t b) {
+        if (list.n == L::kMost || blocks + b > 0x7fffffff) flush();
+        list.first[list.n] = (int32_t)blocks;
+        blocks += b;
+        return list.n++;
+    }
+};
+
+template <class Runs, class Rows, class F>
+hipError_t in_launches(int n, const GradView* g, bool with_dst, F f) {
+    Launches<Runs, F> runs(f);
+    Launches<Rows, F> rows(f);
+    for (int i = 0; i < n; ++i) {
+        if (g[i].rows == 0 || g[i].cols == 0) continue;
+        const uint64_t src = reinterpret_cast<uint64_t>(g[i].src);
+        const uint64_t dst = reinterpret_cast<uint64_t>(g[i].dst);
+        if (is_run(g[i], with_dst)) {
+            const int64_t total = g[i].rows * g[i].cols;
+            for (int64_t at = 0; at < total; at += kMaxRun) {
+                const int64_t len = std::min(total - at, kMaxRun);
+                const int t = runs.next(row_blocks(1, len));
+                runs.list.src[t] = (src + at * (g[i].src_f32 ? 4 : 2)) | (g[i].src_f32 ? 1 : 0);
+                if (with_dst)
+                    runs.list.dst[t] = (dst + at * (g[i].dst_f32 ? 4 : 2)) | (g[i].dst_f32 ? 1 : 0);
+                runs.list.run[t] = (uint32_t)len;
+            }
+            continue;
+        }
+        const int t = rows.next(row_blocks(g[i].rows, g[i].cols));
+        rows.list.src[t] = src | (g[i].src_f32 ? 1 : 0);
+        rows.list.dst[t] = dst | (g[i].dst_f32 ? 1 : 0);
+        rows.list.cols[t] = g[i].cols;
+        rows.list.rows[t] = (int32_t)g[i].rows;
+        rows.list.ld_src[t] = (int32_t)g[i].ld_src;
+        rows.list.ld_dst[t] = (int32_t)g[i].ld_dst;
+    }
+    runs.flush();
+    if (runs.e != hipSuccess) return runs.e;
+    rows.flush();
+    return rows.e;
+}
+
+template <int RUNS, int ROWS, int PARTS>
+hipError_t clip(int n, const GradView* g, int nparts, const double* const* parts, float scale,
+                float max_norm, float* norm, hipStream_t s) {
+    Factor<PARTS> F = {};
+    std::copy(parts, parts + nparts, F.parts);
+    F.nparts = nparts;
+    F.scale = scale;
+    F.max_norm = max_norm;
+    F.norm = norm;
+    typedef List<kRunsTo, RUNS> Runs;
+    typedef List<kRowsTo, ROWS> Rows;
+    static_assert(sizeof(Runs) + sizeof(F) <= 4096 && sizeof(Rows) + sizeof(F) <= 4096,
+                  "kernel arguments");
+    const hipError_t e = in_launches<Runs, Rows>(n, g, true, [&](const auto& L, int64_t blocks) {
+        clip_kernel<<<dim3((unsigned)blocks), kThreads, 0, s>>>(L, F);
+        F.norm = nullptr;
+        return hipGetLastError();
+    });
+    if (e != hipSuccess || !F.norm) return e;
+    Runs none;                                       // nothing to scale: the norm alone
+    none.n = 0;
+    clip_kernel<<<1, 64, 0, s>>>(none, F);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 int64_t grad_sum_blocks(int n, const GradView* g) {
     int64_t blocks = 0;
-    for (int i = 0; i < n; ++i) blocks += blocks_of(run_of(g[i], false));
+    for (int i = 0; i < n; ++i) blocks += blocks_of(g[i]);
     return blocks;
 }
 
 hipError_t launch_grad_sq_sum(int n, const GradView* g, double* sum, double* ws, hipStream_t s) {
     int64_t done = 0;
-    const hipError_t e = in_launches(n, g, false, [&](const Items& L, int64_t blocks) {
+    typedef List<kRuns, 250> Runs;
+    typedef List<kRowsTo, 80> Rows;
+    static_assert(sizeof(Runs) + 8 <= 4096 && sizeof(Rows) + 8 <= 4096, "kernel arguments");
+    const hipError_t e = in_launches<Runs, Rows>(n, g, false, [&](const auto& L, int64_t blocks) {
         sq_sum_kernel<<<dim3((unsigned)blocks), kThreads, 0, s>>>(L, ws + done);
         done += blocks;
         return hipGetLastError();
@@ -278,25 +373,8 @@ hipError_t launch_grad_sq_sum(int n, const GradView* g, double* sum, double* ws,
 
 hipError_t launch_grad_clip(int n, const GradView* g, int nparts, const double* const* parts,
                             float scale, float max_norm, float* norm, hipStream_t s) {
-    Factor F = {};
-    std::copy(parts, parts + nparts, F.parts);
-    F.nparts = nparts;
-    F.scale = scale;
-    F.max_norm = max_norm;
-    bool first = true;
-    ClipArgs a;
-    const hipError_t e = in_launches(n, g, true, [&](const Items& L, int64_t blocks) {
-        a.L = L;
-        a.norm = first ? norm : nullptr;
-        first = false;
-        clip_kernel<<<dim3((unsigned)blocks), kThreads, 0, s>>>(a, F);
-        return hipGetLastError();
-    });
-    if (e != hipSuccess || !first) return e;
-    a.L.n = 0;                                       // nothing to scale: the norm alone
-    a.norm = norm;
-    clip_kernel<<<1, 64, 0, s>>>(a, F);
-    return hipGetLastError();
+    if (nparts <= 8) return clip<160, 80, 8>(n, g, nparts, parts, scale, max_norm, norm, s);
+    return clip<140, 80, kMaxParts>(n, g, nparts, parts, scale, max_norm, norm, s);
 }
 
 }  // namespace atp

@@ -19,6 +19,7 @@
 
 #include <algorithm>
 
+#include "lds_dma.h"
 #include "train_kernels.h"
 #include "wave_ops.h"
 
@@ -29,6 +30,7 @@ using wave::Eight;
 using wave::sum64;
 
 constexpr int kRowsPerGroup = 4;         // rows of a workgroup whose waves hold one each
+constexpr size_t kStageBytes = 160 * 1024 - 512;   // LDS beside the row sums
 
 // How a row of `cols` is held: threads * nv lanes of eight values.
 struct Shape {
@@ -183,6 +185,9 @@ __global__ __launch_bounds__(ONE ? 64 * kRowsPerGroup : 1024) void norm_fwd_kern
     }
 }
 
+__device__ __forceinline__ void hold(Eight<uint16_t>& v) { asm volatile("" : "+v"(v.w)); }
+__device__ __forceinline__ void hold(Eight<float>& v) { asm volatile("" : "+v"(v.a), "+v"(v.b)); }
+
 struct BwdArgs {
     int64_t tokens;
     int cols, nparts;
@@ -202,11 +207,19 @@ struct BwdArgs {
 // A workgroup walks rows gridDim.x apart and keeps its lanes' share of both
 // column sums in registers; it leaves one row of partial sums, which
 // column_sum_kernel adds in order.  The grid is a function of the sizes alone, so
-// the sums are too.
-template <class T, int NV, bool ONE, int THREADS>
+// the sums are too.  A row's values come while the row before is worked on: into
+// registers where a wave holds a row, else (STAGED) by copies into LDS, where each
+// wave reads back what it copied itself, because the registers of one or two
+// workgroups per CU do not hold two wide rows beside the column sums.  The copies of
+// x and dy are begun as soon as the row before is in registers and waited for
+// before its results are stored, so that nothing waits for the stores; d_res is
+// read from LDS where it is added, and its next copy begun behind that.
+template <class T, int NV, bool ONE, int THREADS, bool STAGED>
 __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(BwdArgs A) {
+    constexpr bool kAhead = ONE && (sizeof(T) == 2 || NV <= 2);
+    constexpr int kPlanes = sizeof(T) / 2;           // 16-byte pieces of eight values
     __shared__ float red[2][2][16];
-    extern __shared__ float join[];      // ONE: [3 waves][cols]
+    extern __shared__ float join[];      // ONE: [3 waves][cols]; STAGED: planes of the row
     const int l = ONE ? (int)(threadIdx.x & 63) : (int)threadIdx.x;
     const int per = ONE ? 64 : (int)blockDim.x, waves = per >> 6;
     const int mine = ONE ? (int)(threadIdx.x >> 6) : 0;
@@ -221,28 +234,92 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(BwdArgs A) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) dw[i][e] = db[i][e] = 0.f;
     }
-    int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * (ONE ? kRowsPerGroup : 1) + mine; row < A.tokens;
-         row += step, turn ^= 1) {
-        const T* x = static_cast<const T*>(A.x) + row * A.ldx;
-        const uint16_t* dy = A.dy + row * A.lddy;
-        Eight<T> xs[NV], res[NV];
-        Eight<uint16_t> gs[NV];
+    Eight<T> xs[NV], xn[NV], res[NV];
+    Eight<uint16_t> gs[NV], gn[NV];
+    auto load = [&](int64_t row, Eight<T> (&x)[NV], Eight<uint16_t> (&g)[NV]) {
+        const T* xr = static_cast<const T*>(A.x) + row * A.ldx;
+        const uint16_t* gr = A.dy + row * A.lddy;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (i * per + l) * 8;
             if (c < A.cols) {
-                xs[i].load(x + c);
-                gs[i].load(dy + c);
+                x[i].load(xr + c);
+                g[i].load(gr + c);
             }
         }
-        if (A.dres) {
-            const T* dr = static_cast<const T*>(A.dres) + row * A.lddres;
+    };
+    auto load_res = [&](int64_t row) {
+        const T* dr = static_cast<const T*>(A.dres) + row * A.lddres;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * per + l) * 8;
+            if (c < A.cols) res[i].load(dr + c);
+        }
+    };
+    // plane p of vector i: a wave's 64 lanes one behind the other; x, dy, then d_res
+    uint16_t* slots = reinterpret_cast<uint16_t*>(join);
+    const int w0 = __builtin_amdgcn_readfirstlane(l & ~63);
+    auto slot = [&](int p, int i) { return slots + ((p * NV + i) * per + w0) * 8; };
+    auto words = [](const void* base, int64_t bytes) {   // the same in every lane
+        dma::u32x4 r = dma::rsrc_words(base, bytes);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) r[k] = (uint32_t)__builtin_amdgcn_readfirstlane((int)r[k]);
+        return r;
+    };
+    auto stage = [&](int64_t row) {
+        const dma::u32x4 rx =
+            words(static_cast<const T*>(A.x) + row * A.ldx, A.cols * sizeof(T));
+        const dma::u32x4 rg = words(A.dy + row * A.lddy, A.cols * 2);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t at = (uint32_t)(i * per + l) * 16;     // beyond the row: zeros
+#pragma unroll
+            for (int p = 0; p < kPlanes; ++p)
+                dma::lds_dma16(rx, slot(p, i), at * kPlanes + 16 * p, 0u);
+            dma::lds_dma16(rg, slot(kPlanes, i), at, 0u);
+        }
+    };
+    auto stage_res = [&](int64_t row) {
+        const dma::u32x4 rr =
+            words(static_cast<const T*>(A.dres) + row * A.lddres, A.cols * sizeof(T));
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int p = 0; p < kPlanes; ++p)
+                dma::lds_dma16(rr, slot(kPlanes + 1 + p, i),
+                               (uint32_t)(i * per + l) * 16 * kPlanes + 16 * p, 0u);
+    };
+    auto piece = [&](int p, int i) {
+        return *reinterpret_cast<const wave::u32x4*>(slot(p, i) + (l & 63) * 8);
+    };
+    auto staged = [&](int p, int i, Eight<T>& v) {
+        if constexpr (sizeof(T) == 2) {
+            v.w = piece(p, i);
+        } else {
+            v.a = __builtin_bit_cast(wave::f32x4, piece(p, i));
+            v.b = __builtin_bit_cast(wave::f32x4, piece(p + 1, i));
+        }
+    };
+    int64_t row = (int64_t)blockIdx.x * (ONE ? kRowsPerGroup : 1) + mine;
+    if (kAhead && row < A.tokens) load(row, xs, gs);
+    if (STAGED && row < A.tokens) {
+        stage(row);
+        if (A.dres) stage_res(row);
+        dma::wait_vmcnt<0>();
+    }
+    for (int turn = 0; row < A.tokens; row += step, turn ^= 1) {
+        if constexpr (STAGED) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int c = (i * per + l) * 8;
-                if (c < A.cols) res[i].load(dr + c);
+                staged(0, i, xs[i]);
+                gs[i].w = piece(kPlanes, i);
             }
+            // read before the next row's copies may land
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (row + step < A.tokens) stage(row + step);
+        } else {
+            if (!kAhead) load(row, xs, gs);
+            if (A.dres) load_res(row);
         }
         const float mean = A.mean[row], r = A.rstd[row];
         float c1 = 0.f, c2 = 0.f;
@@ -262,6 +339,16 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(BwdArgs A) {
                 c1 += gw;
                 c2 += gw * xh;
             }
+            if constexpr (!ONE) __builtin_amdgcn_sched_barrier(0);   // one vector at a time
+        }
+        if (kAhead && row + step < A.tokens) load(row + step, xn, gn);
+        // the packed values alone live on: what was unpacked above is unpacked again below
+        // (kept, it would take twice the registers)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            hold(xs[i]);
+            hold(gs[i]);
+            hold(w[i]);
         }
         if (A.nparts == 0) {
             // both sums under one barrier
@@ -273,7 +360,8 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(BwdArgs A) {
                     red[turn][0][threadIdx.x >> 6] = c1;
                     red[turn][1][threadIdx.x >> 6] = c2;
                 }
-                __syncthreads();
+                // for LDS alone: the row's loads and copies go on
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
                 const int k = lane & 15;
                 c1 = k < waves ? red[turn][0][k] : 0.f;
                 c2 = k < waves ? red[turn][1][k] : 0.f;
@@ -286,12 +374,9 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(BwdArgs A) {
                 c1 = wave::dpp_add<0x140>(c1);
                 c2 = wave::dpp_add<0x140>(c2);
             }
-            if (A.sums) {
-                if (l == 0) {
-                    A.sums[2 * row] = c1;
-                    A.sums[2 * row + 1] = c2;
-                }
-                continue;
+            if (A.sums && l == 0) {
+                A.sums[2 * row] = c1;
+                A.sums[2 * row + 1] = c2;
             }
         } else {
             c1 = c2 = 0.f;
@@ -302,12 +387,8 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(BwdArgs A) {
         }
         c1 *= A.inv_total;
         c2 *= A.inv_total;
-        T* dx = static_cast<T*>(A.dx) + row * A.lddx;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = (i * per + l) * 8;
-            if (c >= A.cols) continue;
-            float v[8], g[8], wv[8];
+        auto gradient = [&](int i, float* g) {
+            float v[8], wv[8];
             xs[i].get(v);
             gs[i].get(g);
             w[i].get(wv);
@@ -315,17 +396,48 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(BwdArgs A) {
             for (int e = 0; e < 8; ++e)
                 g[e] = r * (g[e] * wv[e] - c1 - (v[e] - mean) * r * c2);
             if (A.dres) {
-                res[i].get(v);
+                if constexpr (STAGED) {
+                    Eight<T> t;
+                    staged(kPlanes + 1, i, t);
+                    t.get(v);
+                } else {
+                    res[i].get(v);
+                }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) g[e] += v[e];
             }
-            Eight<T> o;
-            o.set(g);
-            o.store(dx + c);
-            if (A.dadd) {
-                Eight<uint16_t> o16;
-                o16.set(g);
-                o16.store(A.dadd + row * A.lddadd + c);
+        };
+        if constexpr (STAGED) dma::wait_vmcnt<0>();
+        if (!A.sums) {
+            T* dx = static_cast<T*>(A.dx) + row * A.lddx;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (i * per + l) * 8;
+                if (c >= A.cols) continue;
+                float g[8];
+                gradient(i, g);
+                Eight<T> o;
+                o.set(g);
+                o.store(dx + c);
+                if (A.dadd) {
+                    Eight<uint16_t> o16;
+                    o16.set(g);
+                    o16.store(A.dadd + row * A.lddadd + c);
+                }
+                if constexpr (!ONE) __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if constexpr (STAGED) {
+            if (A.dres && row + step < A.tokens) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                stage_res(row + step);
+            }
+        }
+        if (kAhead) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                xs[i] = xn[i];
+                gs[i] = gn[i];
             }
         }
     }
@@ -400,14 +512,15 @@ __global__ __launch_bounds__(kSumThreads) void column_sum_kernel(const float* pa
     }
 }
 
-// Workgroups of the backward: enough to fill the chip, each with four rows at least
-// where it leaves partial sums (they are 8 bytes a column against the 8 to 14 of a
-// row), and all with the same number of visits.
+// Workgroups of the backward: enough to fill the chip, each with four rows at least (eight
+// where its waves hold one each), since it leaves a row of partial sums, 8 bytes a
+// column against the 8 to 14 of a row, and all with the same number of visits.
 int64_t bwd_groups(int64_t tokens, int64_t cols) {
     const Shape sh = shape_of(cols);
     const int64_t rows = sh.one ? kRowsPerGroup : 1;
     const int64_t most = 256 * (sh.one ? 4 : std::max(1, 1024 / sh.threads));
-    const int64_t visits = std::max<int64_t>((tokens + most * rows - 1) / (most * rows), 4);
+    const int64_t visits =
+        std::max<int64_t>((tokens + most * rows - 1) / (most * rows), sh.one ? 2 : 4);
     return (tokens + visits * rows - 1) / (visits * rows);
 }
 
@@ -417,8 +530,19 @@ void fwd(const Args& a, int64_t grid, int threads, hipStream_t s) {
 }
 template <class T, int NV, bool ONE, int THREADS>
 void bwd(const BwdArgs& a, int64_t grid, int threads, hipStream_t s) {
-    const size_t lds = ONE && a.part ? sizeof(float) * (kRowsPerGroup - 1) * a.cols : 0;
-    norm_bwd_kernel<T, NV, ONE, THREADS><<<dim3((unsigned)grid), threads, lds, s>>>(a);
+    if constexpr (ONE) {
+        const size_t lds = a.part ? sizeof(float) * (kRowsPerGroup - 1) * a.cols : 0;
+        norm_bwd_kernel<T, NV, true, THREADS, false>
+            <<<dim3((unsigned)grid), threads, lds, s>>>(a);
+    } else {
+        const size_t lds = (size_t)threads * NV * (8 * (a.dres ? 2 : 1) * sizeof(T) + 16);
+        if (lds <= kStageBytes)
+            norm_bwd_kernel<T, NV, false, THREADS, true>
+                <<<dim3((unsigned)grid), threads, lds, s>>>(a);
+        else
+            norm_bwd_kernel<T, NV, false, THREADS, false>
+                <<<dim3((unsigned)grid), threads, 0, s>>>(a);
+    }
 }
 
 template <class T>
@@ -445,8 +569,8 @@ void bwd_of(const Shape& sh, const BwdArgs& a, int64_t grid, hipStream_t s) {
         else bwd<T, 4, true, 256>(a, grid, thr, s);
     } else if (sh.nv == 2) {
         bwd<T, 2, false, 640>(a, grid, thr, s);
-    } else if (sh.threads <= 768) {
-        bwd<T, 4, false, 768>(a, grid, thr, s);
+    } else if (sh.threads <= 640) {
+        bwd<T, 4, false, 640>(a, grid, thr, s);
     } else {
         bwd<T, 4, false, 1024>(a, grid, thr, s);
     }
