@@ -12,11 +12,13 @@
 // A row sees an interval of its document from the first key on, so the tiles that
 // need a mask are those that reach past the first row's limit.
 //
-// Documents are found without a list of tiles: document d's tiles of Q rows take the
-// slots from cu[d] / Q + d on.  They do not overlap (floor(a + b) >= floor(a) +
-// floor(b), and a document of n rows has at most floor(n / Q) + 1 tiles), the slots
-// end at cu[n] / Q + n, and a workgroup finds its document by a search over cu alone;
-// slots without a tile end at once.
+// Documents are found without a list of tiles, so that their lengths may change from
+// replay to replay of a graph.  Up to 64 documents: a workgroup finds the tile of its
+// rank in the order of falling work from the lengths alone (ranked_tile).  More:
+// document d's tiles of Q rows take the slots from cu[d] / Q + d on, which do not
+// overlap (floor(a + b) >= floor(a) + floor(b), and a document of n rows has at most
+// floor(n / Q) + 1 tiles) and end at cu[n] / Q + n; a search over cu finds a slot's.
+// Slots without a tile end at once.
 //
 // Backward: P from the saved log-sum-exps, delta_i = dO_i . O_i,
 //   dS = P o (dO V^T - delta) o (1 - tanh^2), dQ = dS K / sqrt(d), dK = dS^T Q / sqrt(d),
@@ -59,10 +61,54 @@ struct Doc {
     int len, tile, prefix;               // rows, this slot's tile, rows that all see
 };
 
-// The document and tile of a slot of 2^SHIFT rows; false for a slot without one.
-// Lists that do not ascend or leave the rows give tiles inside the rows all the same.
+// A document's rows as the lists give them, kept inside the rows whatever they say.
+__device__ __forceinline__ void bounds(const Common& a, int c0, int c1, int prefix, Doc& doc) {
+    const int tokens = (int)a.tokens;
+    const int start = min(max(c0, 0), tokens), end = min(max(c1, start), tokens);
+    doc.tok0 = start;
+    doc.len = end - start;               // both inside [0, tokens]: no overflow
+    doc.prefix = max(0, min(prefix, doc.len));
+}
+
+// The tile at `rank` when all documents' tiles of 2^SHIFT rows are ordered by their
+// index, the highest first (LAST_KEYS: by their index from the document's end):
+// the longest loops lead and the last workgroups are short.  Up to 64 documents, one
+// per lane: a level's first rank is the number of tiles of higher levels.  False for
+// ranks behind the last tile.
+template <int SHIFT, bool LAST_KEYS>
+__device__ __forceinline__ bool ranked_tile(const Common& a, int rank, Doc& doc) {
+    const int lane = threadIdx.x & 63;
+    const bool in = lane < a.n_docs;
+    const int c0 = in ? a.cu[lane] : 0, c1 = in ? a.cu[lane + 1] : 0;
+    const int prefix = in && a.prefix ? a.prefix[lane] : 0;
+    bounds(a, c0, c1, prefix, doc);
+    const int mine = in ? (doc.len + (1 << SHIFT) - 1) >> SHIFT : 0;
+    // tiles of level t and above; below 2^24, exact in fp32
+    auto above = [&](int t) {
+        return __builtin_amdgcn_readfirstlane((int)wave::sum64((float)max(mine - t, 0)));
+    };
+    if (rank >= above(0)) return false;
+    int lo = 0, hi = (int)((a.tokens + (1 << SHIFT) - 1) >> SHIFT);   // above(lo) > rank >= above(hi)
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (above(mid) > rank) lo = mid;
+        else hi = mid;
+    }
+    const uint64_t level = __builtin_amdgcn_ballot_w64(mine > lo);
+    const int place = rank - above(lo + 1);
+    const bool here = mine > lo && __popcll(level & ((1ull << lane) - 1)) == place;
+    const int d = __builtin_ctzll(__builtin_amdgcn_ballot_w64(here));
+    doc.tok0 = __builtin_amdgcn_readlane((int)doc.tok0, d);
+    doc.len = __builtin_amdgcn_readlane(doc.len, d);
+    doc.prefix = __builtin_amdgcn_readlane(doc.prefix, d);
+    doc.tile = LAST_KEYS ? ((doc.len + (1 << SHIFT) - 1) >> SHIFT) - 1 - lo : lo;
+    return true;
+}
+
+// The document and tile of a slot of 2^SHIFT rows, for more documents; false for a slot
+// without one.
 template <int SHIFT>
-__device__ __forceinline__ bool find_tile(const Common& a, int slot, Doc& doc) {
+__device__ __forceinline__ bool slot_tile(const Common& a, int slot, Doc& doc) {
     const int lane = threadIdx.x & 63;
     int lo = 0, span = a.n_docs;         // the document is in [lo, lo + span)
     for (;;) {
@@ -77,16 +123,25 @@ __device__ __forceinline__ bool find_tile(const Common& a, int slot, Doc& doc) {
         if (step == 1) break;
     }
     lo = __builtin_amdgcn_readfirstlane(lo);
-    const int64_t c0 = a.cu[lo];
-    const int64_t start = c0 < 0 ? 0 : (c0 > a.tokens ? a.tokens : c0);
-    int64_t end = a.cu[lo + 1];
-    end = end > a.tokens ? a.tokens : end;
-    doc.tok0 = start;
-    doc.len = end > start ? (int)(end - start) : 0;
-    doc.tile = slot - (int)(c0 >> SHIFT) - lo;
-    doc.prefix = 0;
-    if (a.prefix) doc.prefix = max(0, min(a.prefix[lo], doc.len));
+    const int c0 = __builtin_amdgcn_readfirstlane(a.cu[lo]);
+    bounds(a, c0, __builtin_amdgcn_readfirstlane(a.cu[lo + 1]),
+           a.prefix ? __builtin_amdgcn_readfirstlane(a.prefix[lo]) : 0, doc);
+    doc.tile = slot - (c0 >> SHIFT) - lo;
     return doc.tile >= 0 && ((int64_t)doc.tile << SHIFT) < doc.len;
+}
+
+// Tile number i of the launch, the longest loops first where that is known.
+template <int SHIFT, bool LAST_KEYS>
+__device__ __forceinline__ bool find_tile(const Common& a, int i, Doc& doc) {
+    const bool ok = a.n_docs <= 64
+                        ? ranked_tile<SHIFT, LAST_KEYS>(a, i, doc)
+                        : slot_tile<SHIFT>(a, LAST_KEYS ? i : a.slots - 1 - i, doc);
+    // the same in every lane: scalars, for the copies' addresses
+    doc.tok0 = __builtin_amdgcn_readfirstlane((int)doc.tok0);
+    doc.len = __builtin_amdgcn_readfirstlane(doc.len);
+    doc.tile = __builtin_amdgcn_readfirstlane(doc.tile);
+    doc.prefix = __builtin_amdgcn_readfirstlane(doc.prefix);
+    return __builtin_amdgcn_readfirstlane(ok);
 }
 
 // Scores in base 2 from raw products.  Without cap and bias they stay raw and are
@@ -128,13 +183,18 @@ __device__ __forceinline__ uint32_t odd_bits(uint32_t w) {
     return (w & 0x7f807f80u) + 0x00800080u;
 }
 
+__device__ __forceinline__ uint32_t without_odd(uint32_t w) {
+    return w & ~(((odd_bits(w) & 0x80008000u) >> 15) * 0xffffu);
+}
+
 // Values of a masked tile may be infinite or NaN where no row of the tile, or only
 // some, see them, and 0 times such a value is NaN.  These values are left out of the
 // products and added to the rows that see them (as their sum with anything is what
 // the weighted sum gives too).
 template <int RB>
-__device__ void odd_values(const uint16_t* vs, int n_first, const int (&limit)[RB], int g,
+__device__ __forceinline__ void odd_values(const uint16_t* vs, int n_first, const int (&limit)[RB], int g,
                            f32x4 (&o)[RB][8]) {
+#pragma unroll 1
     for (int n = 0; n < BN; ++n) {
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) {
@@ -164,11 +224,10 @@ void docs_fwd_kernel(FwdArgs a) {
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const bool producer = PRODUCERS && wv >= KG * NWAVE;
     const int grp = producer ? 0 : wv / NWAVE, wave = wv % NWAVE;
-    // the last slots first: a document's long rows lead
     const int heads = a.kv_heads * a.group;
     const int head = blockIdx.x % heads, kvh = head / a.group;
-    Doc doc;
-    if (!find_tile<RB == 2 ? 7 : 6>(a, a.slots - 1 - (int)(blockIdx.x / heads), doc)) return;
+    Doc doc = {};
+    if (!find_tile<RB == 2 ? 7 : 6, false>(a, (int)(blockIdx.x / heads), doc)) return;
     const int qt = doc.tile;
     const int64_t tok0 = doc.tok0;
     const int64_t hc = (int64_t)kvh * (a.group + 2) * D;
@@ -230,123 +289,175 @@ void docs_fwd_kernel(FwdArgs a) {
     for (int ks = 0; ks < 4; ++ks) koff[ks] = l16 * D + kpos(l16, 4 * ks + g) * 8;
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) voff[dt] = tr_offset(lane, dt);
-    const int clear = max(qt * QT + 1, doc.prefix);   // keys that every row sees
-    for (int i = 0; i < half; ++i) {
-        if (i < mine) {
-            const int kt = kt0 + i;
-            const uint16_t* ks_ = buf[i & 1][0];
-            const uint16_t* vs_ = buf[i & 1][1];
-            const bool more = !PRODUCERS && i + 1 < mine;
-            const auto next = cp.rounds(kbase, a.ldq, vbase, a.ldq, tok0, (kt + 1) * BN, doc.len,
-                                        buf[(i + 1) & 1][0], buf[(i + 1) & 1][1]);
-            f32x4 s[RB][4];
+    // keys that all rows of the tile see; keys that any row of a block sees
+    const int clear = max(qt * QT + 1, doc.prefix);
+    int reach[RB];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+    for (int r = 0; r < RB; ++r) {
+        const int top = qt * QT + 64 * r;
+        reach[r] = top < doc.len ? max(min(top + 64, doc.len), doc.prefix) : 0;
+    }
+    // One key tile for the row blocks [R0, R1), those that see some of it.
+    auto step = [&](int i, auto r0, auto r1, auto mask) {
+        constexpr int R0 = decltype(r0)::value, R1 = decltype(r1)::value;
+        constexpr bool MASKED = decltype(mask)::value;
+        const int kt = kt0 + i;
+        const uint16_t* ks_ = buf[i & 1][0];
+        const uint16_t* vs_ = buf[i & 1][1];
+        const bool more = !PRODUCERS && i + 1 < mine;
+        const auto next = cp.rounds(kbase, a.ldq, vbase, a.ldq, tok0, (kt + 1) * BN, doc.len,
+                                    buf[(i + 1) & 1][0], buf[(i + 1) & 1][1]);
+        f32x4 s[RB][4];
 #pragma unroll
-                for (int r = 0; r < RB; ++r) s[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
+            for (int r = R0; r < R1; ++r) s[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const bf16x8 kf =
-                        *reinterpret_cast<const bf16x8*>(ks_ + 16 * j * D + koff[ks]);
+        for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
-                    for (int r = 0; r < RB; ++r)
-                        s[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][ks], s[r][j],
-                                                                          0, 0, 0);
-                    if (j == 3 && more) cp.round(next, ks, wave);
-                }
-            if constexpr (!Score<CAP, BIAS>::kRaw) {
+            for (int j = 0; j < 4; ++j) {
+                const bf16x8 kf = *reinterpret_cast<const bf16x8*>(ks_ + 16 * j * D + koff[ks]);
 #pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    const float ahead = (float)(mrow[r] - kt * BN - 4 * g);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            s[r][j][e] = score(s[r][j][e], ahead - (float)(16 * j + e));
-                }
+                for (int r = R0; r < R1; ++r)
+                    s[r][j] =
+                        __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][ks], s[r][j], 0, 0, 0);
+                if (j == 3 && more) cp.round(next, ks, wave);
             }
-            // keys past the document are past every limit of its rows
-            const bool masked = (kt + 1) * BN > clear;
-            bool odd = false;
-            if (masked) {
+        if constexpr (!Score<CAP, BIAS>::kRaw) {
 #pragma unroll
-                for (int r = 0; r < RB; ++r)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (kt * BN + 16 * j + 4 * g + e >= limit[r]) s[r][j][e] = -INFINITY;
-                uint32_t seen = 0;
-#pragma unroll
-                for (int c = 0; c < BN * D / 512; ++c) {
-                    const u32x4 w = *reinterpret_cast<const u32x4*>(vs_ + (c * 64 + lane) * 8);
-                    seen |= odd_bits(w[0]) | odd_bits(w[1]) | odd_bits(w[2]) | odd_bits(w[3]);
-                }
-                odd = __builtin_amdgcn_ballot_w64((seen & 0x80008000u) != 0) != 0;
-            }
-#pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                float mx = max16(s[r]);
-                mx = row_max4(mx);
-                const float mnew = fmaxf(mrun[r], mx * factor);
-                if (__builtin_amdgcn_ballot_w64(mnew > mrun[r] + kSlack) != 0) {
-                    const float alpha =
-                        __builtin_amdgcn_exp2f(mrun[r] - (mnew == -INFINITY ? 0.f : mnew));
-                    lrun[r] *= alpha;
-#pragma unroll
-                    for (int dt = 0; dt < 8; ++dt) o[r][dt] *= alpha;
-                    mrun[r] = mnew;
-                }
-                const float msub = mrun[r] == -INFINITY ? 0.f : mrun[r];
-                float rs = 0.f;
+            for (int r = R0; r < R1; ++r) {
+                const float ahead = (float)(mrow[r] - kt * BN - 4 * g);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float p =
-                            __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][j][e], factor, -msub));
-                        s[r][j][e] = p;
-                        rs += p;
-                    }
-                lrun[r] += row_sum4(rs);
-            }
-
-            // O += P V over two 32-key slices
-            auto add_values = [&](auto clean) {
-#pragma unroll
-                for (int sl = 0; sl < 2; ++sl) {
-                    bf16x8 pf[RB];
-#pragma unroll
-                    for (int r = 0; r < RB; ++r) pf[r] = pack_pair(s[r][2 * sl], s[r][2 * sl + 1]);
-#pragma unroll
-                    for (int dt = 0; dt < 8; ++dt) {
-                        bf16x8 vf = frag_tr_at(vs_ + 32 * sl * D + voff[dt]);
-                        if constexpr (decltype(clean)::value) {
-                            u32x4 w = __builtin_bit_cast(u32x4, vf);
-#pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                w[k] &= ~(((odd_bits(w[k]) & 0x80008000u) >> 15) * 0xffffu);
-                            vf = __builtin_bit_cast(bf16x8, w);
-                        }
-#pragma unroll
-                        for (int r = 0; r < RB; ++r)
-                            o[r][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r], o[r][dt],
-                                                                               0, 0, 0);
-                    }
-                }
-            };
-            if (odd) {
-                add_values(std::true_type{});
-                odd_values<RB>(vs_, kt * BN, limit, g, o);
-            } else {
-                add_values(std::false_type{});
+                    for (int e = 0; e < 4; ++e)
+                        s[r][j][e] = score(s[r][j][e], ahead - (float)(16 * j + e));
             }
         }
+        // keys past the document are past every limit of its rows
+        bool odd = false;
+        if constexpr (MASKED) {
+#pragma unroll
+            for (int r = R0; r < R1; ++r)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (kt * BN + 16 * j + 4 * g + e >= limit[r]) s[r][j][e] = -INFINITY;
+            uint32_t seen = 0;
+#pragma unroll 2
+            for (int c = 0; c < BN * D / 512; ++c) {
+                const u32x4 w = *reinterpret_cast<const u32x4*>(vs_ + (c * 64 + lane) * 8);
+                seen |= odd_bits(w[0]) | odd_bits(w[1]) | odd_bits(w[2]) | odd_bits(w[3]);
+            }
+            odd = __builtin_amdgcn_ballot_w64((seen & 0x80008000u) != 0) != 0;
+        }
+#pragma unroll
+        for (int r = R0; r < R1; ++r) {
+            float mx = max16(s[r]);
+            mx = row_max4(mx);
+            const float mnew = fmaxf(mrun[r], mx * factor);
+            if (__builtin_amdgcn_ballot_w64(mnew > mrun[r] + kSlack) != 0) {
+                const float alpha =
+                    __builtin_amdgcn_exp2f(mrun[r] - (mnew == -INFINITY ? 0.f : mnew));
+                lrun[r] *= alpha;
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) o[r][dt] *= alpha;
+                mrun[r] = mnew;
+            }
+            const float msub = mrun[r] == -INFINITY ? 0.f : mrun[r];
+            float rs = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p =
+                        __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][j][e], factor, -msub));
+                    s[r][j][e] = p;
+                    rs += p;
+                }
+            lrun[r] += rs;               // the lane's share: a row's four lanes join at the end
+        }
+
+        // O += P V over two 32-key slices
+        auto add_values = [&](auto clean) {
+#pragma unroll
+            for (int sl = 0; sl < 2; ++sl) {
+                bf16x8 pf[RB];
+#pragma unroll
+                for (int r = R0; r < R1; ++r) pf[r] = pack_pair(s[r][2 * sl], s[r][2 * sl + 1]);
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) {
+                    bf16x8 vf = frag_tr_at(vs_ + 32 * sl * D + voff[dt]);
+                    if constexpr (decltype(clean)::value) {
+                        u32x4 w = __builtin_bit_cast(u32x4, vf);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) w[k] = without_odd(w[k]);
+                        vf = __builtin_bit_cast(bf16x8, w);
+                    }
+#pragma unroll
+                    for (int r = R0; r < R1; ++r)
+                        o[r][dt] =
+                            __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r], o[r][dt], 0, 0, 0);
+                }
+            }
+        };
+        if constexpr (KG > 1) {          // the groups' tiles differ: fragments are cleaned
+            if (odd) {
+                odd_values<RB>(vs_, kt * BN, limit, g, o);
+                add_values(std::true_type{});
+                return;
+            }
+        } else if (odd) {                // by all waves: the tile is cleaned
+            odd_values<RB>(vs_, kt * BN, limit, g, o);
+            __syncthreads();
+            u32x4* own = reinterpret_cast<u32x4*>(buf[i & 1][1]) + wave * 64 + lane;
+#pragma unroll 1
+            for (int c = 0; c < BN * D / 8; c += NTHR) {
+                u32x4 w = own[c];
+                for (int k = 0; k < 4; ++k) w[k] = without_odd(w[k]);
+                own[c] = w;
+            }
+            __syncthreads();
+        }
+        add_values(std::false_type{});
+    };
+    const std::integral_constant<int, 0> b0;
+    const std::integral_constant<int, 1> b1;
+    const std::integral_constant<int, RB> bn;
+    auto end_step = [&] {
+        // this wave's copies of its next step have landed; after the barrier
+        // every wave's have, and no wave reads the buffers of this step
         dma::wait_vmcnt<0>();
         __syncthreads();
+    };
+    // tiles that every row sees whole, then those with masks, then (two row blocks) those
+    // behind all keys of the first
+    const int whole = max(0, min(clear / BN - kt0, mine));
+    int i = 0;
+    if (RB == 1 || reach[RB - 1] > 0) {
+        for (; i < whole; ++i) {
+            step(i, b0, bn, std::false_type{});
+            end_step();
+        }
+        for (; i < mine && (RB == 1 || (kt0 + i) * BN < reach[0]); ++i) {
+            step(i, b0, bn, std::true_type{});
+            end_step();
+        }
+        if constexpr (RB > 1)
+            for (; i < mine; ++i) {
+                step(i, b1, bn, std::true_type{});
+                end_step();
+            }
+    } else {                             // the second block lies past the document
+        for (; i < mine; ++i) {
+            step(i, b0, b1, std::true_type{});
+            end_step();
+        }
     }
+    for (; i < half; ++i) end_step();    // a group with fewer tiles idles
+#pragma unroll
+    for (int r = 0; r < RB; ++r) lrun[r] = row_sum4(lrun[r]);
 
     if constexpr (KG > 1) {
         f32x4* ox = reinterpret_cast<f32x4*>(&kv[1][0][0][0]);
@@ -436,9 +547,8 @@ __global__ __launch_bounds__(NTHR * KG, 2 / KG) void docs_dkv_kernel(BwdArgs a) 
     const int per_slot = a.kv_heads * a.parts;
     const int which = blockIdx.x % per_slot;
     const int kvh = which % a.kv_heads, part = which / a.kv_heads;
-    Doc doc;
-    // early keys, which many rows see, first
-    if (!find_tile<6>(a, (int)(blockIdx.x / per_slot), doc)) return;
+    Doc doc = {};
+    if (!find_tile<6, true>(a, (int)(blockIdx.x / per_slot), doc)) return;
     const int kt = doc.tile;
     const int64_t tok0 = doc.tok0, T = a.tokens;
     const int64_t hc = (int64_t)kvh * (a.group + 2) * D;
@@ -648,8 +758,8 @@ void docs_dq_kernel(BwdArgs a) {
     const int grp = producer ? 0 : wv / NWAVE, wave = wv % NWAVE;
     const int heads = a.kv_heads * a.group;
     const int head = blockIdx.x % heads, kvh = head / a.group;
-    Doc doc;
-    if (!find_tile<RB == 2 ? 7 : 6>(a, a.slots - 1 - (int)(blockIdx.x / heads), doc)) return;
+    Doc doc = {};
+    if (!find_tile<RB == 2 ? 7 : 6, false>(a, (int)(blockIdx.x / heads), doc)) return;
     const int qt = doc.tile;
     const int64_t tok0 = doc.tok0, T = a.tokens;
     const int64_t hc = (int64_t)kvh * (a.group + 2) * D;
@@ -728,76 +838,108 @@ void docs_dq_kernel(BwdArgs a) {
     offsets(lane, boff, toff);
     __syncthreads();
     const int clear = max(qt * QT + 1, doc.prefix);
-    for (int i = 0; i < half; ++i) {
-        if (i < mine) {
-            const int kt = k0 + i;
-            const uint16_t* ks_ = kb[i & 1][0];
-            const uint16_t* vs_ = kb[i & 1][1];
-            const bool more = !PRODUCERS && i + 1 < mine;
-            const auto next = cp.rounds(kbase, a.ldq, vbase, a.ldq, tok0, (kt + 1) * BN, doc.len,
-                                        kb[(i + 1) & 1][0], kb[(i + 1) & 1][1]);
-            const bool masked = (kt + 1) * BN > clear;
-            constexpr int JG = RB == 1 ? 4 : 2;
-            f32x4 dsv[RB][4];
+    int reach[RB];                       // keys that any row of a block sees
 #pragma unroll
-            for (int j0 = 0; j0 < 4; j0 += JG) {
-                f32x4 sacc[RB][JG], dacc[RB][JG];
+    for (int r = 0; r < RB; ++r) {
+        const int top = qt * QT + 64 * r;
+        reach[r] = top < doc.len ? max(min(top + 64, doc.len), doc.prefix) : 0;
+    }
+    auto step = [&](int i, auto r0, auto r1, auto mask) {
+        constexpr int R0 = decltype(r0)::value, R1 = decltype(r1)::value;
+        constexpr bool MASKED = decltype(mask)::value;
+        const int kt = k0 + i;
+        const uint16_t* ks_ = kb[i & 1][0];
+        const uint16_t* vs_ = kb[i & 1][1];
+        const bool more = !PRODUCERS && i + 1 < mine;
+        const auto next = cp.rounds(kbase, a.ldq, vbase, a.ldq, tok0, (kt + 1) * BN, doc.len,
+                                    kb[(i + 1) & 1][0], kb[(i + 1) & 1][1]);
+        constexpr int JG = RB == 1 ? 4 : 2;
+        f32x4 dsv[RB][4];
 #pragma unroll
-                for (int r = 0; r < RB; ++r)
+        for (int j0 = 0; j0 < 4; j0 += JG) {
+            f32x4 sacc[RB][JG], dacc[RB][JG];
 #pragma unroll
-                    for (int jj = 0; jj < JG; ++jj) {
-                        sacc[r][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
-                        dacc[r][jj] = sacc[r][jj];
-                    }
+            for (int r = R0; r < R1; ++r)
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-                    for (int jj = 0; jj < JG; ++jj) {
-                        const int j = j0 + jj;
-                        const bf16x8 kf =
-                            *reinterpret_cast<const bf16x8*>(ks_ + 16 * j * D + boff[ks]);
-                        const bf16x8 vf =
-                            *reinterpret_cast<const bf16x8*>(vs_ + 16 * j * D + boff[ks]);
-#pragma unroll
-                        for (int r = 0; r < RB; ++r) {
-                            sacc[r][jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                                kf, qf[r][ks], sacc[r][jj], 0, 0, 0);
-                            dacc[r][jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                                vf, of[r][ks], dacc[r][jj], 0, 0, 0);
-                        }
-                        if (j0 == 0 && jj == JG - 1 && more) cp.round(next, ks, wave);
-                    }
-#pragma unroll
-                for (int jj = 0; jj < JG; ++jj)
-#pragma unroll
-                    for (int r = 0; r < RB; ++r)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int n = kt * BN + 16 * (j0 + jj) + 4 * g + e;
-                            float p, d = dacc[r][jj][e];
-                            grad_of(score, sacc[r][jj][e], (float)(qabs[r] - n), l2[r], dl[r],
-                                    masked && n >= limit[r], p, d);
-                            dsv[r][j0 + jj][e] = d;
-                        }
-            }
-#pragma unroll
-            for (int sl = 0; sl < 2; ++sl) {
-                bf16x8 sf[RB];
-#pragma unroll
-                for (int r = 0; r < RB; ++r) sf[r] = pack_pair(dsv[r][2 * sl], dsv[r][2 * sl + 1]);
-#pragma unroll
-                for (int dt = 0; dt < 8; ++dt) {
-                    const bf16x8 kt_ = frag_tr_at(ks_ + 32 * sl * D + toff[dt]);
-#pragma unroll
-                    for (int r = 0; r < RB; ++r)
-                        dq[r][dt] =
-                            __builtin_amdgcn_mfma_f32_16x16x32_bf16(kt_, sf[r], dq[r][dt], 0, 0, 0);
+                for (int jj = 0; jj < JG; ++jj) {
+                    sacc[r][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    dacc[r][jj] = sacc[r][jj];
                 }
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+                for (int jj = 0; jj < JG; ++jj) {
+                    const int j = j0 + jj;
+                    const bf16x8 kf = *reinterpret_cast<const bf16x8*>(ks_ + 16 * j * D + boff[ks]);
+                    const bf16x8 vf = *reinterpret_cast<const bf16x8*>(vs_ + 16 * j * D + boff[ks]);
+#pragma unroll
+                    for (int r = R0; r < R1; ++r) {
+                        sacc[r][jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][ks],
+                                                                              sacc[r][jj], 0, 0, 0);
+                        dacc[r][jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, of[r][ks],
+                                                                              dacc[r][jj], 0, 0, 0);
+                    }
+                    if (j0 == 0 && jj == JG - 1 && more) cp.round(next, ks, wave);
+                }
+#pragma unroll
+            for (int jj = 0; jj < JG; ++jj)
+#pragma unroll
+                for (int r = R0; r < R1; ++r)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int n = kt * BN + 16 * (j0 + jj) + 4 * g + e;
+                        float p, d = dacc[r][jj][e];
+                        grad_of(score, sacc[r][jj][e], (float)(qabs[r] - n), l2[r], dl[r],
+                                MASKED && n >= limit[r], p, d);
+                        dsv[r][j0 + jj][e] = d;
+                    }
+        }
+#pragma unroll
+        for (int sl = 0; sl < 2; ++sl) {
+            bf16x8 sf[RB];
+#pragma unroll
+            for (int r = R0; r < R1; ++r) sf[r] = pack_pair(dsv[r][2 * sl], dsv[r][2 * sl + 1]);
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) {
+                const bf16x8 kt_ = frag_tr_at(ks_ + 32 * sl * D + toff[dt]);
+#pragma unroll
+                for (int r = R0; r < R1; ++r)
+                    dq[r][dt] =
+                        __builtin_amdgcn_mfma_f32_16x16x32_bf16(kt_, sf[r], dq[r][dt], 0, 0, 0);
             }
         }
+    };
+    const std::integral_constant<int, 0> b0;
+    const std::integral_constant<int, 1> b1;
+    const std::integral_constant<int, RB> bn;
+    auto end_step = [&] {
         dma::wait_vmcnt<0>();
         __syncthreads();
+    };
+    // as in the forward
+    const int whole = max(0, min(clear / BN - k0, mine));
+    int i = 0;
+    if (RB == 1 || reach[RB - 1] > 0) {
+        for (; i < whole; ++i) {
+            step(i, b0, bn, std::false_type{});
+            end_step();
+        }
+        for (; i < mine && (RB == 1 || (k0 + i) * BN < reach[0]); ++i) {
+            step(i, b0, bn, std::true_type{});
+            end_step();
+        }
+        if constexpr (RB > 1)
+            for (; i < mine; ++i) {
+                step(i, b1, bn, std::true_type{});
+                end_step();
+            }
+    } else {
+        for (; i < mine; ++i) {
+            step(i, b0, b1, std::true_type{});
+            end_step();
+        }
     }
+    for (; i < half; ++i) end_step();
     if constexpr (KG > 1) {
         f32x4* x = reinterpret_cast<f32x4*>(&kv[1][0][0][0]);
         if (grp == 1) {

@@ -54,6 +54,7 @@ __device__ __forceinline__ int find(const L& list, int block) {
     int at = -1;
 #pragma unroll
     for (int i = 0; i < (L::kMost + 63) / 64; ++i) {
+        if (i * 64 >= list.n) break;
         const int k = i * 64 + lane;
         at += __popcll(__builtin_amdgcn_ballot_w64(k < list.n && list.first[k] <= block));
     }
@@ -203,14 +204,31 @@ struct Factor {
     float* norm;                                     // in the first launch: norm and factor
 };
 
-template <class S, class T, Kind K>
-__device__ __forceinline__ void scaled(const S* src, T* dst, const Places<K>& p, float f) {
+// The devices' sums, in group order, as norm and factor (by every workgroup).
+template <int N>
+__device__ __forceinline__ float factor_of(const Factor<N>& F) {
+    double s = 0.0;
+    for (int j = 0; j < F.nparts; ++j) s += *F.parts[j];
+    const double norm = (double)F.scale * sqrt(s);
+    const float f = (float)((double)F.scale *
+                            (norm <= (double)F.max_norm ? 1.0 : (double)F.max_norm / norm));
+    if (F.norm && blockIdx.x == 0 && threadIdx.x == 0) {
+        F.norm[0] = (float)norm;
+        F.norm[1] = f;
+    }
+    return f;
+}
+
+template <class S, class T, Kind K, int N>
+__device__ __forceinline__ void scaled(const S* src, T* dst, const Places<K>& p,
+                                       const Factor<N>& F) {
     Eight<S> in[kVecs];
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
         const auto a = p.at(i);
         if (a.in) in[i] = load8(K == kRowsTo ? src + a.row * p.ld_src : src, a.col, p.cols);
     }
+    const float f = factor_of(F);                    // while the values come
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
         const auto a = p.at(i);
@@ -223,31 +241,27 @@ __device__ __forceinline__ void scaled(const S* src, T* dst, const Places<K>& p,
     }
 }
 
+// The last spans first: the sum, which ran before, read them last, so that some of
+// their values may still be cached.
 template <class L, int N>
 __global__ __launch_bounds__(kThreads) void clip_kernel(L list, Factor<N> F) {
-    // every workgroup adds the devices' sums, in group order
-    double s = 0.0;
-    for (int j = 0; j < F.nparts; ++j) s += *F.parts[j];
-    const double norm = (double)F.scale * sqrt(s);
-    const float f = (float)((double)F.scale *
-                            (norm <= (double)F.max_norm ? 1.0 : (double)F.max_norm / norm));
-    if (F.norm && blockIdx.x == 0 && threadIdx.x == 0) {
-        F.norm[0] = (float)norm;
-        F.norm[1] = f;
+    if (list.n == 0) {
+        factor_of(F);
+        return;
     }
-    if (list.n == 0) return;
-    const int t = find(list, blockIdx.x);
-    const Places<L::kind> p(list, t, blockIdx.x);
+    const int block = (int)blockIdx.x;
+    const int t = find(list, block);
+    const Places<L::kind> p(list, t, block);
     const uint64_t src = list.src[t], dst = list.dst[t];
-    if (f == 1.f && src == dst) return;              // in place already
+    if (src == dst && factor_of(F) == 1.f) return;   // in place already
     if (src & 1) {
         const float* from = pointer<const float>(src);
-        if (dst & 1) scaled(from, pointer<float>(dst), p, f);
-        else scaled(from, pointer<uint16_t>(dst), p, f);
+        if (dst & 1) scaled(from, pointer<float>(dst), p, F);
+        else scaled(from, pointer<uint16_t>(dst), p, F);
     } else {
         const uint16_t* from = pointer<const uint16_t>(src);
-        if (dst & 1) scaled(from, pointer<float>(dst), p, f);
-        else scaled(from, pointer<uint16_t>(dst), p, f);
+        if (dst & 1) scaled(from, pointer<float>(dst), p, F);
+        else scaled(from, pointer<uint16_t>(dst), p, F);
     }
 }
 

@@ -75,6 +75,24 @@ __device__ __forceinline__ float row_sum(float v, float* red, int waves) {
     return wave::dpp_add<0x140>(t);
 }
 
+// A row's entry of every device's table: lane j holds device j's.
+struct Pair {
+    float a, b;
+};
+__device__ __forceinline__ Pair part_of(const float* const* parts, int n, int64_t row) {
+    Pair p = {0.f, 0.f};
+    const int j = threadIdx.x & 63;
+    if (j < n) {
+        const wave::f32x2 v = *reinterpret_cast<const wave::f32x2*>(parts[j] + 2 * row);
+        p.a = v[0];
+        p.b = v[1];
+    }
+    return p;
+}
+__device__ __forceinline__ float of_lane(float v, int j) {
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), j));
+}
+
 template <class T, int NV, bool ONE>
 __global__ __launch_bounds__(ONE ? 64 * kRowsPerGroup : 1024) void norm_fwd_kernel(Args A) {
     __shared__ float red[2][16];
@@ -84,6 +102,7 @@ __global__ __launch_bounds__(ONE ? 64 * kRowsPerGroup : 1024) void norm_fwd_kern
                             : (int64_t)blockIdx.x;
     if (row >= A.tokens) return;         // whole waves, and no barrier follows for them
     const T* x = static_cast<const T*>(A.x) + row * A.ldx;
+    const Pair part = part_of(A.parts, A.nparts, row);
     Eight<T> in[NV];
     float v[NV][8];
 #pragma unroll
@@ -146,11 +165,11 @@ __global__ __launch_bounds__(ONE ? 64 * kRowsPerGroup : 1024) void norm_fwd_kern
         }
     } else {
         // equal shards: the mean of the means; the squares about it
-        for (int j = 0; j < A.nparts; ++j) mean += A.parts[j][2 * row];
+        for (int j = 0; j < A.nparts; ++j) mean += of_lane(part.a, j);
         mean /= (float)A.nparts;
         for (int j = 0; j < A.nparts; ++j) {
-            const float d = A.parts[j][2 * row] - mean;
-            m2 += A.parts[j][2 * row + 1] + A.part_cols * d * d;
+            const float d = of_lane(part.a, j) - mean;
+            m2 += of_lane(part.b, j) + A.part_cols * d * d;
         }
     }
     const float r = 1.f / sqrtf(m2 * A.inv_total + A.eps);
@@ -322,6 +341,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(BwdArgs A) {
             if (A.dres) load_res(row);
         }
         const float mean = A.mean[row], r = A.rstd[row];
+        const Pair part = part_of(A.parts, A.nparts, row);
         float c1 = 0.f, c2 = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -381,8 +401,8 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(BwdArgs A) {
         } else {
             c1 = c2 = 0.f;
             for (int j = 0; j < A.nparts; ++j) {
-                c1 += A.parts[j][2 * row];
-                c2 += A.parts[j][2 * row + 1];
+                c1 += of_lane(part.a, j);
+                c2 += of_lane(part.b, j);
             }
         }
         c1 *= A.inv_total;
@@ -485,15 +505,17 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(BwdArgs A) {
     }
 }
 
-// Column sums of n rows of 2 cols partials: 64 columns per workgroup, 16 runs of
-// rows (every 16th), joined in order.
+// Column sums of n rows of 2 cols partials: C columns per workgroup, 1024 / C runs of
+// rows (every 1024 / C-th), joined in order.  16 columns where 64 would leave CUs idle:
+// 626 rows of 2048 columns 3.9 us, 5.3 with 64.
 constexpr int kSumThreads = 1024;
+template <int C>
 __global__ __launch_bounds__(kSumThreads) void column_sum_kernel(const float* part, int n,
                                                                  int cols, float* dw, float* db) {
-    constexpr int G = kSumThreads / 64;
-    __shared__ float red[G][64];
-    const int c = threadIdx.x & 63, g = threadIdx.x >> 6;
-    const int64_t col = (int64_t)blockIdx.x * 64 + c;
+    constexpr int G = kSumThreads / C;
+    __shared__ float red[G][C + 1];
+    const int c = threadIdx.x % C, g = threadIdx.x / C;
+    const int64_t col = (int64_t)blockIdx.x * C + c;
     float sum = 0.f;
     if (col < 2 * (int64_t)cols) {
 #pragma unroll 8
@@ -636,8 +658,13 @@ hipError_t launch_layer_norm_bwd(const LayerNormBwdProblem& p, hipStream_t s) {
         if (e != hipSuccess) return e;
     }
     if (!weights) return hipSuccess;
-    column_sum_kernel<<<dim3((unsigned)((2 * p.cols + 63) / 64)), kSumThreads, 0, s>>>(
-        p.ws, (int)grid, (int)p.cols, p.dw, p.db);
+    const int cols = (int)p.cols;
+    if (2 * cols < 64 * 256)
+        column_sum_kernel<16><<<dim3((unsigned)((2 * cols + 15) / 16)), kSumThreads, 0, s>>>(
+            p.ws, (int)grid, cols, p.dw, p.db);
+    else
+        column_sum_kernel<64><<<dim3((unsigned)((2 * cols + 63) / 64)), kSumThreads, 0, s>>>(
+            p.ws, (int)grid, cols, p.dw, p.db);
     return hipGetLastError();
 }
 
