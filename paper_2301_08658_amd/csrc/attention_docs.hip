@@ -54,6 +54,7 @@ struct Common {
     int n_docs, kv_heads, group, slots;
     float scale_log2;                    // log2(e) / sqrt(D)
     float cap_in, cap_log2;              // 2 log2(e) / (sqrt(D) cap), cap log2(e)
+    float root_d;                        // sqrt(D)
 };
 
 struct Doc {
@@ -144,30 +145,51 @@ __device__ __forceinline__ bool find_tile(const Common& a, int i, Doc& doc) {
     return __builtin_amdgcn_readfirstlane(ok);
 }
 
-// Scores in base 2 from raw products.  Without cap and bias they stay raw and are
-// scaled in the exponential's argument.
+// What is done to raw products q . k.  A bias alone is what the products are added to
+// (in their units), a cap alone keeps their order, so that both keep the raw maximum; cap
+// and bias together are formed for every score before it.
 template <bool CAP, bool BIAS>
 struct Score {
-    static constexpr bool kRaw = !CAP && !BIAS;
-    float scale, cap_in, cap_log2, slope;
+    static constexpr bool kFormed = CAP && BIAS;
+    float scale, cap_in, cap_log2, slope, slope_raw;
     __device__ __forceinline__ Score(const Common& a, int head)
-        : scale(a.scale_log2), cap_in(a.cap_in), cap_log2(a.cap_log2), slope(0.f) {
-        if constexpr (BIAS) slope = a.slopes[head] * kLog2e;
+        : scale(a.scale_log2), cap_in(a.cap_in), cap_log2(a.cap_log2), slope(0.f), slope_raw(0.f) {
+        if constexpr (BIAS) {
+            slope = a.slopes[head] * kLog2e;
+            slope_raw = a.slopes[head] * a.root_d;
+        }
     }
-    // tanh(y) = 1 - 2 / (1 + e^(2 y)): off by 2^-23 of 1 at most, which moves a score of
-    // cap 50 by 6e-6
-    __device__ __forceinline__ float tanh_of(float raw) const {
-        return 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(raw * cap_in));
+    // the products' first summand
+    __device__ __forceinline__ float start(float dist) const {
+        if constexpr (BIAS && !CAP) return -slope_raw * __builtin_fabsf(dist);
+        return 0.f;
+    }
+    // tanh(y) = 1 - 2 r, r = 1 / (1 + e^(2 y)): off by 2^-23 of 1 at most, which moves a
+    // score of cap 50 by 6e-6
+    __device__ __forceinline__ float rest_of(float raw) const {
+        return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(raw * cap_in));
+    }
+    __device__ __forceinline__ float capped(float raw) const {
+        return __builtin_fmaf(rest_of(raw), -2.f * cap_log2, cap_log2);
     }
     __device__ __forceinline__ float bias(float x, float dist) const {
-        if constexpr (BIAS) return __builtin_fmaf(-slope, __builtin_fabsf(dist), x);
+        if constexpr (kFormed) return __builtin_fmaf(-slope, __builtin_fabsf(dist), x);
         return x;
     }
-    __device__ __forceinline__ float operator()(float raw, float dist) const {
-        if constexpr (kRaw) return raw;
-        return bias(CAP ? cap_log2 * tanh_of(raw) : raw * scale, dist);
+    // base-2 score of a row's largest raw (or formed) value; -inf stays
+    __device__ __forceinline__ float top(float mx) const {
+        if constexpr (kFormed) return mx;
+        if constexpr (CAP) return mx == -INFINITY ? mx : capped(mx);
+        return mx * scale;
     }
-    __device__ __forceinline__ float factor() const { return kRaw ? scale : 1.f; }
+    // 2^(score - m) of a raw (or formed) value
+    __device__ __forceinline__ float weight(float v, float m) const {
+        if constexpr (kFormed) return __builtin_amdgcn_exp2f(v - m);
+        if constexpr (CAP)
+            return __builtin_amdgcn_exp2f(
+                __builtin_fmaf(rest_of(v), -2.f * cap_log2, cap_log2 - m));
+        return __builtin_amdgcn_exp2f(__builtin_fmaf(v, scale, -m));
+    }
 };
 
 // ---------------------------------------------------------------------------
@@ -270,7 +292,6 @@ void docs_fwd_kernel(FwdArgs a) {
         }
     }
     const Score<CAP, BIAS> score(a, head);
-    const float factor = score.factor();
 
     f32x4 o[RB][8];
     float mrun[RB], lrun[RB];
@@ -309,9 +330,13 @@ void docs_fwd_kernel(FwdArgs a) {
                                     buf[(i + 1) & 1][0], buf[(i + 1) & 1][1]);
         f32x4 s[RB][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int r = R0; r < R1; ++r) {
+            const float ahead = (float)(mrow[r] - kt * BN - 4 * g);
 #pragma unroll
-            for (int r = R0; r < R1; ++r) s[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[r][j][e] = score.start(ahead - (float)(16 * j + e));
+        }
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
@@ -323,7 +348,7 @@ void docs_fwd_kernel(FwdArgs a) {
                         __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][ks], s[r][j], 0, 0, 0);
                 if (j == 3 && more) cp.round(next, ks, wave);
             }
-        if constexpr (!Score<CAP, BIAS>::kRaw) {
+        if constexpr (Score<CAP, BIAS>::kFormed) {
 #pragma unroll
             for (int r = R0; r < R1; ++r) {
                 const float ahead = (float)(mrow[r] - kt * BN - 4 * g);
@@ -331,7 +356,8 @@ void docs_fwd_kernel(FwdArgs a) {
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        s[r][j][e] = score(s[r][j][e], ahead - (float)(16 * j + e));
+                        s[r][j][e] =
+                            score.bias(score.capped(s[r][j][e]), ahead - (float)(16 * j + e));
             }
         }
         // keys past the document are past every limit of its rows
@@ -356,7 +382,7 @@ void docs_fwd_kernel(FwdArgs a) {
         for (int r = R0; r < R1; ++r) {
             float mx = max16(s[r]);
             mx = row_max4(mx);
-            const float mnew = fmaxf(mrun[r], mx * factor);
+            const float mnew = fmaxf(mrun[r], score.top(mx));
             if (__builtin_amdgcn_ballot_w64(mnew > mrun[r] + kSlack) != 0) {
                 const float alpha =
                     __builtin_amdgcn_exp2f(mrun[r] - (mnew == -INFINITY ? 0.f : mnew));
@@ -371,8 +397,10 @@ void docs_fwd_kernel(FwdArgs a) {
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float p =
-                        __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][j][e], factor, -msub));
+                    float p = score.weight(s[r][j][e], msub);
+                    // a cap makes a finite score of a masked one's -inf
+                    if constexpr (MASKED && CAP && !BIAS)
+                        if (kt * BN + 16 * j + 4 * g + e >= limit[r]) p = 0.f;
                     s[r][j][e] = p;
                     rs += p;
                 }
@@ -522,24 +550,29 @@ struct BwdArgs : Common {
 template <bool CAP, bool BIAS>
 __device__ __forceinline__ void grad_of(const Score<CAP, BIAS>& f, float raw, float dist, float l2,
                                         float dl, bool hidden, float& p, float& ds) {
-    float pv, slope = 1.f;
+    float pv, d;
     if constexpr (CAP) {
-        const float t = f.tanh_of(raw);
-        slope = __builtin_fmaf(-t, t, 1.f);
-        pv = __builtin_amdgcn_exp2f(f.bias(__builtin_fmaf(f.cap_log2, t, -l2), dist));
+        const float r = f.rest_of(raw), r4 = 4.f * r;
+        pv = __builtin_amdgcn_exp2f(
+            f.bias(__builtin_fmaf(r, -2.f * f.cap_log2, f.cap_log2 - l2), dist));
+        d = pv * (ds - dl) * __builtin_fmaf(-r4, r, r4);     // 1 - tanh^2 = 4 r (1 - r)
     } else {
-        pv = __builtin_amdgcn_exp2f(f.bias(__builtin_fmaf(raw, f.scale, -l2), dist));
+        pv = __builtin_amdgcn_exp2f(__builtin_fmaf(raw, f.scale, -l2));
+        d = pv * (ds - dl);
     }
-    float d = pv * (ds - dl);
-    if constexpr (CAP) d *= slope;
     p = hidden ? 0.f : pv;
     ds = hidden ? 0.f : d;
 }
 
+// dK and dV of a 64-key tile, 16 keys per wave, 32 queries at a time (so that scores and
+// dP take 16 registers each).  KG groups of four waves split the steps (group 0 the
+// first half, group 1 the rest, added through LDS at the end).  32 keys per wave would
+// halve the fragments' reads but leave one wave per SIMD: 20 heads of two documents of
+// 4096 rows took 100 us more.
 template <int KG, bool CAP, bool BIAS>
 __global__ __launch_bounds__(NTHR * KG, 2 / KG) void docs_dkv_kernel(BwdArgs a) {
     __shared__ __attribute__((aligned(16))) uint16_t qd[KG][2][2][BM * D];   // [grp][buf][Q|dO]
-    __shared__ float rowv[KG][2][2][BM];                                    // [grp][buf][lse2|delta]
+    __shared__ __attribute__((aligned(16))) float rowv[KG][2][2][BM];       // [grp][buf][lse2|delta]
     const int lane = threadIdx.x & 63, g = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int grp = wv / NWAVE, wave = wv % NWAVE;
@@ -557,6 +590,7 @@ __global__ __launch_bounds__(NTHR * KG, 2 / KG) void docs_dkv_kernel(BwdArgs a) 
 
     const int kabs = kt * BN + wave * 16 + (lane & 15);
     bf16x8 kf[4], vf[4];
+    f32x4 dk[8], dv[8];
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
         if (kabs < doc.len) {
@@ -568,7 +602,6 @@ __global__ __launch_bounds__(NTHR * KG, 2 / KG) void docs_dkv_kernel(BwdArgs a) 
             vf[ks] = kf[ks];
         }
     }
-    f32x4 dk[8], dv[8];
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) {
         dk[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -624,55 +657,68 @@ __global__ __launch_bounds__(NTHR * KG, 2 / KG) void docs_dkv_kernel(BwdArgs a) 
                                         a.dout + (int64_t)head2 * D, a.lddo, tok0, qt2 * BM,
                                         doc.len, qb[buf ^ 1][0], qb[buf ^ 1][1]);
             if (more) load_rows(head2, qt2, l2r, dlr);
-            // a tile whose first row sees the whole key tile, and that ends inside the
-            // document, needs no mask
-            const bool masked =
-                (kt + 1) * BN > max(qt * BM + 1, doc.prefix) || (qt + 1) * BM > doc.len;
             const Score<CAP, BIAS> score(a, head);
-            f32x4 p[4], dsv[4];
+            // 32 queries: their scores and dP (lane: key kabs, query 16 j + 4 g + e), then
+            // their share of dV and dK
+            auto slice = [&](auto sl_, auto mask) {
+                constexpr int sl = decltype(sl_)::value;
+                constexpr bool MASKED = decltype(mask)::value;
+                const float ahead = (float)(qt * BM + 32 * sl + 4 * g - kabs);
+                f32x4 p[2], d[2];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                p[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-                dsv[j] = p[j];
-            }
+                for (int jj = 0; jj < 2; ++jj)
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
+                    for (int e = 0; e < 4; ++e) {
+                        p[jj][e] = score.start(ahead + (float)(16 * jj + e));
+                        d[jj][e] = 0.f;
+                    }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    p[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        *reinterpret_cast<const bf16x8*>(qs + 16 * j * D + boff[ks]), kf[ks],
-                        p[j], 0, 0, 0);
-                    dsv[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        *reinterpret_cast<const bf16x8*>(ds_ + 16 * j * D + boff[ks]), vf[ks],
-                        dsv[j], 0, 0, 0);
-                    if (j == 3 && more) cp.round(next, ks, wave);
-                }
-            const float ahead = (float)(qt * BM + 4 * g - kabs);
+                for (int ks = 0; ks < 4; ++ks) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int ql = 16 * j + 4 * g + e;
-                    const int qabs = qt * BM + ql;
-                    const bool hidden =
-                        masked && (kabs >= max(qabs + 1, doc.prefix) || qabs >= doc.len);
-                    float pv, dv_ = dsv[j][e];
-                    grad_of(score, p[j][e], ahead + (float)(16 * j + e), rv[buf][0][ql],
-                            rv[buf][1][ql], hidden, pv, dv_);
-                    p[j][e] = pv;
-                    dsv[j][e] = dv_;
+                    for (int jj = 0; jj < 2; ++jj) {
+                        const int j = 2 * sl + jj;
+                        const bf16x8 qf =
+                            *reinterpret_cast<const bf16x8*>(qs + 16 * j * D + boff[ks]);
+                        const bf16x8 of =
+                            *reinterpret_cast<const bf16x8*>(ds_ + 16 * j * D + boff[ks]);
+                        p[jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf, kf[ks], p[jj], 0, 0, 0);
+                        d[jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(of, vf[ks], d[jj], 0, 0, 0);
+                    }
+                    if (sl == 0 && more) cp.round(next, ks, wave);
                 }
 #pragma unroll
-            for (int sl = 0; sl < 2; ++sl) {
-                const bf16x8 pf = pack_pair(p[2 * sl], p[2 * sl + 1]);
-                const bf16x8 sf = pack_pair(dsv[2 * sl], dsv[2 * sl + 1]);
+                for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int ql = 16 * (2 * sl + jj) + 4 * g + e;
+                        const int qabs = qt * BM + ql;
+                        const bool hidden =
+                            MASKED && (kabs >= max(qabs + 1, doc.prefix) || qabs >= doc.len);
+                        float pv, dsv = d[jj][e];
+                        grad_of(score, p[jj][e], ahead + (float)(16 * jj + e), rv[buf][0][ql],
+                                rv[buf][1][ql], hidden, pv, dsv);
+                        p[jj][e] = pv;
+                        d[jj][e] = dsv;
+                    }
+                const bf16x8 pf = pack_pair(p[0], p[1]), sf = pack_pair(d[0], d[1]);
 #pragma unroll
                 for (int dt = 0; dt < 8; ++dt) {
-                    dv[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        frag_tr_at(ds_ + 32 * sl * D + toff[dt]), pf, dv[dt], 0, 0, 0);
-                    dk[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        frag_tr_at(qs + 32 * sl * D + toff[dt]), sf, dk[dt], 0, 0, 0);
+                    const bf16x8 of = frag_tr_at(ds_ + 32 * sl * D + toff[dt]);
+                    const bf16x8 qf = frag_tr_at(qs + 32 * sl * D + toff[dt]);
+                    dv[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(of, pf, dv[dt], 0, 0, 0);
+                    dk[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf, sf, dk[dt], 0, 0, 0);
                 }
+            };
+            const std::integral_constant<int, 0> s0;
+            const std::integral_constant<int, 1> s1;
+            // a tile whose first row sees the whole key tile, and that ends inside the
+            // document, needs no mask
+            if ((kt + 1) * BN <= max(qt * BM + 1, doc.prefix) && (qt + 1) * BM <= doc.len) {
+                slice(s0, std::false_type{});
+                slice(s1, std::false_type{});
+            } else {
+                slice(s0, std::true_type{});
+                if (qt * BM + 32 < doc.len) slice(s1, std::true_type{});
             }
             if (more && tid < BM) {
                 rv[buf ^ 1][0][tid] = l2r;
@@ -714,11 +760,11 @@ __global__ __launch_bounds__(NTHR * KG, 2 / KG) void docs_dkv_kernel(BwdArgs a) 
     uint16_t* row = a.dqkv + (tok0 + kabs) * a.lddq + hc + (int64_t)a.group * D;
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) {
-        const u32x2 wk = {pack_bf16x2(dk[dt][0] * a.inv_sqrt_d, dk[dt][1] * a.inv_sqrt_d),
-                          pack_bf16x2(dk[dt][2] * a.inv_sqrt_d, dk[dt][3] * a.inv_sqrt_d)};
-        const u32x2 wv2 = {pack_bf16x2(dv[dt][0], dv[dt][1]), pack_bf16x2(dv[dt][2], dv[dt][3])};
-        *reinterpret_cast<u32x2*>(row + 16 * dt + 4 * g) = wk;
-        *reinterpret_cast<u32x2*>(row + D + 16 * dt + 4 * g) = wv2;
+        const f32x4 k = dk[dt] * a.inv_sqrt_d, v = dv[dt];
+        *reinterpret_cast<u32x2*>(row + 16 * dt + 4 * g) =
+            u32x2{pack_bf16x2(k[0], k[1]), pack_bf16x2(k[2], k[3])};
+        *reinterpret_cast<u32x2*>(row + D + 16 * dt + 4 * g) =
+            u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
     }
 }
 
@@ -861,10 +907,13 @@ void docs_dq_kernel(BwdArgs a) {
 #pragma unroll
             for (int r = R0; r < R1; ++r)
 #pragma unroll
-                for (int jj = 0; jj < JG; ++jj) {
-                    sacc[r][jj] = f32x4{0.f, 0.f, 0.f, 0.f};
-                    dacc[r][jj] = sacc[r][jj];
-                }
+                for (int jj = 0; jj < JG; ++jj)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int n = kt * BN + 16 * (j0 + jj) + 4 * g + e;
+                        sacc[r][jj][e] = score.start((float)(qabs[r] - n));
+                        dacc[r][jj][e] = 0.f;
+                    }
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
@@ -988,6 +1037,7 @@ void fill(Common& c, const DocsView& d, const uint16_t* qkv, int64_t ldq, int64_
     c.slots = 0;
     const float root = sqrtf((float)D);
     c.scale_log2 = kLog2e / root;
+    c.root_d = root;
     c.cap_in = d.cap > 0.f ? 2.f * kLog2e / (root * d.cap) : 0.f;
     c.cap_log2 = d.cap * kLog2e;
 }
@@ -1031,12 +1081,13 @@ void bwd_of(BwdArgs& a, hipStream_t s) {
         docs_dq_kernel<2, 1, CAP, BIAS>
             <<<dim3((unsigned)((int64_t)a.slots * heads)), NTHR, 0, s>>>(a);
     }
+    const int per_slot = a.kv_heads * a.parts;
     a.slots = (int)s64;
-    const dim3 grid((unsigned)(s64 * a.kv_heads * a.parts));
-    if ((a.tokens + 63) / 64 * a.kv_heads * a.parts < kBwdSplitTiles)
-        docs_dkv_kernel<2, CAP, BIAS><<<grid, 2 * NTHR, 0, s>>>(a);
-    else
-        docs_dkv_kernel<1, CAP, BIAS><<<grid, NTHR, 0, s>>>(a);
+    if ((a.tokens + 63) / 64 * per_slot < kBwdSplitTiles) {
+        docs_dkv_kernel<2, CAP, BIAS><<<dim3((unsigned)(s64 * per_slot)), 2 * NTHR, 0, s>>>(a);
+    } else {
+        docs_dkv_kernel<1, CAP, BIAS><<<dim3((unsigned)(s64 * per_slot)), NTHR, 0, s>>>(a);
+    }
 }
 
 }  // namespace
