@@ -807,14 +807,16 @@ def atp_attention_bwd_noalloc(m: atp_mesh, block_mode: int, batch: int, seq: int
 
 # The calls below are made token by token, so their arguments are looked at once and
 # quickly; what does not fit goes to _mat / _vec, which say what is wrong.
-def _rows(t, rows: int, cols: int, name: str, dev: int):
-    """(pointer, ld) of a bf16 matrix on device dev."""
-    if t is not None and t.dtype is torch.bfloat16 and t.get_device() == dev and t.dim() == 2:
+def _rows(t, rows: int, cols: int, name: str, dev: int, dtype=torch.bfloat16):
+    """(pointer, ld) of a matrix on device dev (None stays NULL)."""
+    if t is None:
+        return None, 0
+    if t.dtype is dtype and t.get_device() == dev and t.dim() == 2:
         r, c = t.shape
         s0, s1 = t.stride()
         if r >= rows and c >= cols and (s1 == 1 or c <= 1):
             return t.data_ptr(), (s0 if r > 1 else max(c, cols))
-    return _mat(t, rows, cols, torch.bfloat16, name)
+    return _mat(t, rows, cols, dtype, name)
 
 
 def _list(t, n: int, name: str, dev: int, dtype=torch.int32):
@@ -1046,17 +1048,21 @@ def atp_attention_cache_fwd(cache: kv_cache, batch: kv_batch, tokens: int, group
 
 
 # ------------------------------------------------ around the layers, for training
-def _stream_mat(t, rows: int, cols: int, dtype, name: str, dev: int):
-    """(pointer, ld) of a matrix of the residual stream's type."""
-    if dtype is torch.bfloat16:
-        return _rows(t, rows, cols, name, dev)
-    return _mat(t, rows, cols, dtype, name)
+_FLOATS = {torch.float32: ATP_F32, torch.bfloat16: ATP_BF16}
 
 
-def _float_dtype(t, name: str):
-    if t.dtype not in (torch.float32, torch.bfloat16):
+def _float_code(t, name: str) -> int:
+    code = _FLOATS.get(t.dtype)
+    if code is None:
         raise TypeError(f"{name}: expected torch.float32 or torch.bfloat16, got {t.dtype}")
-    return t.dtype, (ATP_F32 if t.dtype is torch.float32 else ATP_BF16)
+    return code
+
+
+def _width(t, name: str) -> int:
+    """Columns of a matrix that gives a call its row width."""
+    if t.dim() != 2:
+        raise ValueError(f"{name}: needs a 2-D row-major tensor")
+    return t.shape[1]
 
 
 def atp_embedding_fwd(tokens: int, ids, table, out, scale: float = 1.0, vocab_off: int = 0,
@@ -1065,12 +1071,10 @@ def atp_embedding_fwd(tokens: int, ids, table, out, scale: float = 1.0, vocab_of
     devices.  ids: int32 [tokens]; table: bf16 [vocab_loc, cols]; out: float32 or
     bf16 [tokens, cols]."""
     dev = torch.cuda.current_device()
-    if table.dim() != 2:
-        raise ValueError("table: needs a 2-D row-major tensor")
-    vocab, cols = table.shape
-    odt, code = _float_dtype(out, "out")
+    cols, vocab = _width(table, "table"), table.shape[0]
     tp, ldt = _rows(table, vocab, cols, "table", dev)
-    op, ldo = _stream_mat(out, tokens, cols, odt, "out", dev)
+    code = _float_code(out, "out")
+    op, ldo = _rows(out, tokens, cols, "out", dev, out.dtype)
     _check(load_library().atp_embedding_fwd(
         int(tokens), _list(ids, tokens, "ids", dev), vocab, int(vocab_off), cols, tp, ldt,
         float(scale), op, code, ldo, _stream(stream, dev)))
@@ -1086,11 +1090,9 @@ def atp_embedding_bwd(tokens: int, ids, dy, dtable, workspace, scale: float = 1.
     sum of dy (bf16 [tokens, cols]) over the tokens with that id; workspace:
     atp_embedding_workspace_bytes(tokens, vocab_loc, cols) bytes."""
     dev = torch.cuda.current_device()
-    if dtable.dim() != 2:
-        raise ValueError("dtable: needs a 2-D row-major tensor")
-    vocab, cols = dtable.shape
+    cols, vocab = _width(dtable, "dtable"), dtable.shape[0]
     yp, ldy = _rows(dy, tokens, cols, "dy", dev)
-    tp, ldt = _mat(dtable, vocab, cols, torch.float32, "dtable")
+    tp, ldt = _rows(dtable, vocab, cols, "dtable", dev, torch.float32)
     wsp, wsb = _bytes(workspace, dev)
     _check(load_library().atp_embedding_bwd(
         int(tokens), _list(ids, tokens, "ids", dev), vocab, int(vocab_off), cols, yp, ldy,
@@ -1132,15 +1134,12 @@ def _row_tables(ts, tokens: int, name: str, dev: int):
 
 def _summed(tokens: int, x, add, x_out, dev: int):
     """Sizes and arguments of the sum that a norm is of."""
-    if x.dim() != 2:
-        raise ValueError("x: needs a 2-D row-major tensor")
-    cols = x.size(1)
-    dt, code = _float_dtype(x, "x")
-    xp, ldx = _stream_mat(x, tokens, cols, dt, "x", dev)
-    ap, lda = _rows(add, tokens, cols, "add", dev) if add is not None else (None, 0)
-    op, ldo = (_stream_mat(x_out, tokens, cols, dt, "x_out", dev) if x_out is not None
-               else (None, 0))
-    return cols, code, (xp, ldx, ap, lda, op, ldo)
+    cols, code = _width(x, "x"), _float_code(x, "x")
+    xp, ldx = _rows(x, tokens, cols, "x", dev, x.dtype)
+    if add is None and x_out is None:
+        return cols, code, (xp, ldx, None, 0, None, 0)
+    return cols, code, (xp, ldx, *_rows(add, tokens, cols, "add", dev),
+                        *_rows(x_out, tokens, cols, "x_out", dev, x.dtype))
 
 
 def atp_layer_norm_stats(tokens: int, x, stats, add=None, x_out=None, stream=None):
@@ -1169,23 +1168,20 @@ def atp_layer_norm_fwd(tokens: int, norm: layer_norm, x, y, mean, rstd, add=None
 
 
 def _normed(tokens: int, norm, x, mean, rstd, dy, dev: int):
-    """Sizes and the arguments that both calls of the backward share."""
-    if x.dim() != 2:
-        raise ValueError("x: needs a 2-D row-major tensor")
-    cols = x.size(1)
-    dt, code = _float_dtype(x, "x")
-    xp, ldx = _stream_mat(x, tokens, cols, dt, "x", dev)
-    gp, ldg = _rows(dy, tokens, cols, "dy", dev)
-    return cols, dt, (int(tokens), cols, code, norm.of(cols, dev), xp, ldx,
-                      _list(mean, tokens, "mean", dev, torch.float32),
-                      _list(rstd, tokens, "rstd", dev, torch.float32), gp, ldg)
+    """Row width and the arguments that both calls of the backward share."""
+    cols, code = _width(x, "x"), _float_code(x, "x")
+    return cols, (int(tokens), cols, code, norm.of(cols, dev),
+                  *_rows(x, tokens, cols, "x", dev, x.dtype),
+                  _list(mean, tokens, "mean", dev, torch.float32),
+                  _list(rstd, tokens, "rstd", dev, torch.float32),
+                  *_rows(dy, tokens, cols, "dy", dev))
 
 
 def atp_layer_norm_bwd_sums(tokens: int, norm: layer_norm, x, mean, rstd, dy, sums, stream=None):
     """The row sums of this device's columns that the others need, into sums
     (float32 [tokens, 2])."""
     dev = torch.cuda.current_device()
-    _, _, args = _normed(tokens, norm, x, mean, rstd, dy, dev)
+    _, args = _normed(tokens, norm, x, mean, rstd, dy, dev)
     _check(load_library().atp_layer_norm_bwd_sums(
         *args, _list(sums, 2 * tokens, "sums", dev, torch.float32), _stream(stream, dev)))
 
@@ -1202,12 +1198,11 @@ def atp_layer_norm_bwd(tokens: int, norm: layer_norm, x, mean, rstd, dy, dx, d_r
     need a workspace of atp_layer_norm_workspace_bytes(tokens, cols) bytes).  x: the
     normed values; sums: the group's row sums, as stats in the forward."""
     dev = torch.cuda.current_device()
-    cols, dt, args = _normed(tokens, norm, x, mean, rstd, dy, dev)
-    rp, ldr = (_stream_mat(d_res, tokens, cols, dt, "d_res", dev) if d_res is not None
-               else (None, 0))
+    cols, args = _normed(tokens, norm, x, mean, rstd, dy, dev)
+    rp, ldr = _rows(d_res, tokens, cols, "d_res", dev, x.dtype)
     n, tab = _row_tables(sums, tokens, "sums", dev)
-    dp_, ldd = _stream_mat(dx, tokens, cols, dt, "dx", dev)
-    ap, lda = _rows(d_add, tokens, cols, "d_add", dev) if d_add is not None else (None, 0)
+    dp_, ldd = _rows(dx, tokens, cols, "dx", dev, x.dtype)
+    ap, lda = _rows(d_add, tokens, cols, "d_add", dev)
     wsp, wsb = _bytes(workspace, dev)
     _check(load_library().atp_layer_norm_bwd(
         *args, rp, ldr, n, tab, dp_, ldd, ap, lda,
@@ -1302,7 +1297,7 @@ class grad_list:
                 setattr(g, side, t.data_ptr())
                 gaps = t.dim() == 2 and rows == t.size(0) and rows > 1
                 setattr(g, "ld_" + side, t.stride(0) if gaps else cols)
-                setattr(g, side + "_dtype", _float_dtype(t, f"{side}[{i}]")[1])
+                setattr(g, side + "_dtype", _float_code(t, f"{side}[{i}]"))
                 if t.numel():
                     end = (rows - 1) * getattr(g, "ld_" + side) + cols
                     spans.append((t.data_ptr(), t.data_ptr() + end * t.element_size(), i, side))

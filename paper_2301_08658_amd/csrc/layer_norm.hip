@@ -237,6 +237,8 @@ template <class T, int NV, bool ONE, int THREADS, bool STAGED>
 __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(BwdArgs A) {
     constexpr bool kAhead = ONE && (sizeof(T) == 2 || NV <= 2);
     constexpr int kPlanes = sizeof(T) / 2;           // 16-byte pieces of eight values
+    // the weights stay in registers where there are some for them, else come from L2
+    constexpr bool kHoldW = NV <= 2 || ONE || (sizeof(T) == 2 && THREADS <= 640);
     __shared__ float red[2][2][16];
     extern __shared__ float join[];      // ONE: [3 waves][cols]; STAGED: planes of the row
     const int l = ONE ? (int)(threadIdx.x & 63) : (int)threadIdx.x;
@@ -248,11 +250,22 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(BwdArgs A) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = (i * per + l) * 8;
-        if (A.w && c < A.cols) w[i].load(A.w + c);
+        if (kHoldW && A.w && c < A.cols) w[i].load(A.w + c);
         else w[i].w = wave::u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};   // ones
 #pragma unroll
         for (int e = 0; e < 8; ++e) dw[i][e] = db[i][e] = 0.f;
     }
+    auto weight = [&](int i, float* v) {
+        if constexpr (!kHoldW) {
+            if (A.w) {
+                Eight<uint16_t> t;
+                t.load(A.w + (i * per + l) * 8);
+                t.get(v);
+                return;
+            }
+        }
+        w[i].get(v);
+    };
     Eight<T> xs[NV], xn[NV], res[NV];
     Eight<uint16_t> gs[NV], gn[NV];
     auto load = [&](int64_t row, Eight<T> (&x)[NV], Eight<uint16_t> (&g)[NV]) {
@@ -349,7 +362,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(BwdArgs A) {
             float v[8], g[8], wv[8];
             xs[i].get(v);
             gs[i].get(g);
-            w[i].get(wv);
+            weight(i, wv);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float xh = (v[e] - mean) * r;
@@ -368,7 +381,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(BwdArgs A) {
         for (int i = 0; i < NV; ++i) {
             hold(xs[i]);
             hold(gs[i]);
-            hold(w[i]);
+            if constexpr (kHoldW) hold(w[i]);
         }
         if (A.nparts == 0) {
             // both sums under one barrier
@@ -411,7 +424,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(BwdArgs A) {
             float v[8], wv[8];
             xs[i].get(v);
             gs[i].get(g);
-            w[i].get(wv);
+            weight(i, wv);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 g[e] = r * (g[e] * wv[e] - c1 - (v[e] - mean) * r * c2);
