@@ -44,6 +44,10 @@ namespace {
 using namespace tiles;
 
 constexpr float kLog2e = 1.44269504088896340736f;
+// forward: a lane's sum of weights (16 keys of a row) that moves the row's reference.  Far
+// below fp32's largest number, so that values up to 2^90 do not overflow; 2^20 and 2^30
+// measured the same.
+constexpr float kMostSum = 4096.f;
 
 struct Common {
     const uint16_t* qkv; int64_t ldq;
@@ -260,6 +264,12 @@ void docs_fwd_kernel(FwdArgs a) {
     const int half = KG > 1 ? (nkt + 1) / 2 : nkt;
     const int kt0 = grp == 0 ? 0 : half;
     const int mine = grp == 0 ? half : nkt - half;   // <= half
+    // With a bias the last tile, with the diagonal, comes first, so that near keys, which it
+    // favours, do not move the weights' reference at every tile (20 heads of two documents
+    // of 4096 rows: 270 us in ascending order, 226 so; of nine documents of up to 1500 rows,
+    // half of each a prefix, 55 and 60).
+    constexpr bool BACK = KG == 1 && BIAS;
+    auto tile_of = [&](int i) { return BACK ? nkt - 1 - i : kt0 + i; };
     uint16_t(*buf)[2][BN * D] = kv[grp];
     TileDma2<true> cp;
     cp.init(a.ldq, a.ldq, wave, lane);
@@ -272,8 +282,8 @@ void docs_fwd_kernel(FwdArgs a) {
         }
     } else {
         if (mine > 0)
-            cp.issue(kbase, a.ldq, vbase, a.ldq, tok0, kt0 * BN, doc.len, buf[0][0], buf[0][1],
-                     wave);
+            cp.issue(kbase, a.ldq, vbase, a.ldq, tok0, tile_of(0) * BN, doc.len, buf[0][0],
+                     buf[0][1], wave);
         dma::wait_vmcnt<0>();
     }
     int mrow[RB], limit[RB];             // rows in the document, keys that they see
@@ -319,14 +329,17 @@ void docs_fwd_kernel(FwdArgs a) {
         reach[r] = top < doc.len ? max(min(top + 64, doc.len), doc.prefix) : 0;
     }
     // One key tile for the row blocks [R0, R1), those that see some of it.
+    // Without masks there is a next tile, whose copies then stand between the products without
+    // a branch, so that a slice's fragments are read while the slice before is multiplied.
     auto step = [&](int i, auto r0, auto r1, auto mask) {
         constexpr int R0 = decltype(r0)::value, R1 = decltype(r1)::value;
         constexpr bool MASKED = decltype(mask)::value;
-        const int kt = kt0 + i;
+        const int kt = tile_of(i);
         const uint16_t* ks_ = buf[i & 1][0];
         const uint16_t* vs_ = buf[i & 1][1];
-        const bool more = !PRODUCERS && i + 1 < mine;
-        const auto next = cp.rounds(kbase, a.ldq, vbase, a.ldq, tok0, (kt + 1) * BN, doc.len,
+        const bool more = !PRODUCERS && (!MASKED || i + 1 < mine);
+        const auto next = cp.rounds(kbase, a.ldq, vbase, a.ldq, tok0,
+                                    tile_of(i + 1) * BN, doc.len,
                                     buf[(i + 1) & 1][0], buf[(i + 1) & 1][1]);
         f32x4 s[RB][4];
 #pragma unroll
@@ -335,19 +348,30 @@ void docs_fwd_kernel(FwdArgs a) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[r][j][e] = score.start(ahead - (float)(16 * j + e));
+                for (int e = 0; e < 4; ++e)
+                    s[r][j][e] = score.start(ahead - (float)(16 * j + e));
         }
+        bf16x8 kf[4], kn[4];
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
+        for (int j = 0; j < 4; ++j)
+            kf[j] = *reinterpret_cast<const bf16x8*>(ks_ + 16 * j * D + koff[0]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bf16x8 kf = *reinterpret_cast<const bf16x8*>(ks_ + 16 * j * D + koff[ks]);
+        for (int ks = 0; ks < 4; ++ks) {
+            if (ks < 3) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    kn[j] = *reinterpret_cast<const bf16x8*>(ks_ + 16 * j * D + koff[ks + 1]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int r = R0; r < R1; ++r)
-                    s[r][j] =
-                        __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][ks], s[r][j], 0, 0, 0);
-                if (j == 3 && more) cp.round(next, ks, wave);
-            }
+                    s[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[j], qf[r][ks], s[r][j], 0,
+                                                                      0, 0);
+            if (more) cp.round(next, ks, wave);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) kf[j] = kn[j];
+        }
         if constexpr (Score<CAP, BIAS>::kFormed) {
 #pragma unroll
             for (int r = R0; r < R1; ++r) {
@@ -378,32 +402,52 @@ void docs_fwd_kernel(FwdArgs a) {
             }
             odd = __builtin_amdgcn_ballot_w64((seen & 0x80008000u) != 0) != 0;
         }
+        // The weights 2^(x - m) take the reference m of earlier tiles; it moves, to the row's
+        // maximum, when a lane's sum of weights passes kMostSum.  O / l and m + log2 l do not
+        // depend on m, so the results differ from a maximum at every step by rounding only,
+        // and the maxima, a third of the vector instructions, are spared.
+        bf16x8 pf[RB][2];
 #pragma unroll
         for (int r = R0; r < R1; ++r) {
-            float mx = max16(s[r]);
-            mx = row_max4(mx);
-            const float mnew = fmaxf(mrun[r], score.top(mx));
-            if (__builtin_amdgcn_ballot_w64(mnew > mrun[r] + kSlack) != 0) {
-                const float alpha =
-                    __builtin_amdgcn_exp2f(mrun[r] - (mnew == -INFINITY ? 0.f : mnew));
+            auto weights = [&](float m) {
+                float sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; j += 2) {
+                    f32x4 p[2];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            p[k][e] = score.weight(s[r][j + k][e], m);
+                            // a cap makes a finite score of a masked one's -inf
+                            if constexpr (MASKED && CAP && !BIAS)
+                                if (kt * BN + 16 * (j + k) + 4 * g + e >= limit[r]) p[k][e] = 0.f;
+                            sum += p[k][e];
+                        }
+                    pf[r][j / 2] = pack_pair(p[0], p[1]);
+                }
+                return sum;
+            };
+            // The first tile sets the reference.  From the back a row may see nothing in it:
+            // m stays -inf, and the next sums are infinite or NaN.
+            const bool first = KG > 1 || (!BACK && i == 0);
+            float rs = 0.f;
+            if (!first) rs = weights(mrun[r]);
+            const bool over = BACK ? !(rs <= kMostSum) : rs > kMostSum;
+            if (first || __builtin_amdgcn_ballot_w64(over) != 0) {
+                // row by row, so that no row's bits depend on its neighbours
+                const bool move = first || row_max4(over ? 1.f : 0.f) > 0.f;
+                const float mnew =
+                    move ? fmaxf(mrun[r], score.top(row_max4(max16(s[r])))) : mrun[r];
+                // a row that has seen no key keeps -inf: subtract 0
+                const float msub = mnew == -INFINITY ? 0.f : mnew;
+                const float alpha = __builtin_amdgcn_exp2f(mrun[r] - msub);
                 lrun[r] *= alpha;
 #pragma unroll
                 for (int dt = 0; dt < 8; ++dt) o[r][dt] *= alpha;
                 mrun[r] = mnew;
+                rs = weights(msub);
             }
-            const float msub = mrun[r] == -INFINITY ? 0.f : mrun[r];
-            float rs = 0.f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float p = score.weight(s[r][j][e], msub);
-                    // a cap makes a finite score of a masked one's -inf
-                    if constexpr (MASKED && CAP && !BIAS)
-                        if (kt * BN + 16 * j + 4 * g + e >= limit[r]) p = 0.f;
-                    s[r][j][e] = p;
-                    rs += p;
-                }
             lrun[r] += rs;               // the lane's share: a row's four lanes join at the end
         }
 
@@ -411,9 +455,6 @@ void docs_fwd_kernel(FwdArgs a) {
         auto add_values = [&](auto clean) {
 #pragma unroll
             for (int sl = 0; sl < 2; ++sl) {
-                bf16x8 pf[RB];
-#pragma unroll
-                for (int r = R0; r < R1; ++r) pf[r] = pack_pair(s[r][2 * sl], s[r][2 * sl + 1]);
 #pragma unroll
                 for (int dt = 0; dt < 8; ++dt) {
                     bf16x8 vf = frag_tr_at(vs_ + 32 * sl * D + voff[dt]);
@@ -425,8 +466,8 @@ void docs_fwd_kernel(FwdArgs a) {
                     }
 #pragma unroll
                     for (int r = R0; r < R1; ++r)
-                        o[r][dt] =
-                            __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r], o[r][dt], 0, 0, 0);
+                        o[r][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r][sl], o[r][dt],
+                                                                           0, 0, 0);
                 }
             }
         };
@@ -453,33 +494,59 @@ void docs_fwd_kernel(FwdArgs a) {
     const std::integral_constant<int, 0> b0;
     const std::integral_constant<int, 1> b1;
     const std::integral_constant<int, RB> bn;
+    const std::true_type yes;
+    const std::false_type no;
     auto end_step = [&] {
         // this wave's copies of its next step have landed; after the barrier
         // every wave's have, and no wave reads the buffers of this step
         dma::wait_vmcnt<0>();
         __syncthreads();
     };
-    // tiles that every row sees whole, then those with masks, then (two row blocks) those
-    // behind all keys of the first
+    // tiles that every row sees whole
     const int whole = max(0, min(clear / BN - kt0, mine));
     int i = 0;
-    if (RB == 1 || reach[RB - 1] > 0) {
-        for (; i < whole; ++i) {
-            step(i, b0, bn, std::false_type{});
+    if constexpr (BACK) {
+        if (reach[RB - 1] > 0) {
+            if constexpr (RB > 1)        // behind all keys of the first block
+                for (; tile_of(i) * BN >= reach[0]; ++i) {
+                    step(i, b1, bn, yes);
+                    end_step();
+                }
+            for (; i < nkt - whole; ++i) {
+                step(i, b0, bn, yes);
+                end_step();
+            }
+            for (; i < nkt - 1; ++i) {
+                step(i, b0, bn, no);
+                end_step();
+            }
+            if (i < nkt) {
+                step(i, b0, bn, yes);
+                end_step();
+            }
+        } else {                         // the second block lies past the document
+            for (; i < nkt; ++i) {
+                step(i, b0, b1, yes);
+                end_step();
+            }
+        }
+    } else if (RB == 1 || reach[RB - 1] > 0) {
+        for (; i < min(whole, mine - 1); ++i) {
+            step(i, b0, bn, no);
             end_step();
         }
         for (; i < mine && (RB == 1 || (kt0 + i) * BN < reach[0]); ++i) {
-            step(i, b0, bn, std::true_type{});
+            step(i, b0, bn, yes);
             end_step();
         }
         if constexpr (RB > 1)
             for (; i < mine; ++i) {
-                step(i, b1, bn, std::true_type{});
+                step(i, b1, bn, yes);
                 end_step();
             }
-    } else {                             // the second block lies past the document
+    } else {
         for (; i < mine; ++i) {
-            step(i, b0, b1, std::true_type{});
+            step(i, b0, b1, yes);
             end_step();
         }
     }
