@@ -5,8 +5,8 @@
 //
 // Squares and sums are formed in 64 bits: squares of 32-bit values neither overflow
 // nor vanish there, and a sum of 10^9 of them keeps its digits.  A workgroup takes
-// 16384 consecutive values of one tensor and leaves one partial sum; the partial
-// sums are added in a fixed order.  Bound by memory: the gradients are read once
+// consecutive values of one tensor and leaves one partial sum; the partial sums are
+// added in a fixed order.  Bound by memory: the gradients are read once
 // for the norm, and once more, with one write, for the clipping, which cannot begin
 // before the norm is known.  The list of tensors travels in the kernels' arguments,
 // as many per launch as 4 KiB hold (250 for the sum, 160 for the clipping), so a call
@@ -23,12 +23,16 @@
 namespace atp {
 namespace {
 
-using wave::Eight;
-
 constexpr int kThreads = 256;
-constexpr int kVecs = 8;                             // vectors of eight values per thread
-constexpr int kGroupVecs = kThreads * kVecs;         // of a workgroup
+// Values of a workgroup, of the sum and of the clipping (629 M fp32 values: sums of 4096
+// 381 us, of 16384 380, of bf16 values 394 and 381; clipping of 4096 857 us, of 8192 940,
+// of 16384 990).
+constexpr int kSumValues = 16384, kClipValues = 4096;
 constexpr int64_t kMaxRun = 1 << 30;                 // values of a run; longer ones are cut
+// Gradients of more bytes go past the caches, which hold no value from the sum to the
+// clipping then.  Sum and clipping into other memory, cached and past the caches: of
+// 128 MiB 65 and 71 us, of 256 MiB 154 and 134, of 1 GiB 572 and 526.
+constexpr int64_t kCachedBytes = 128 << 20;
 
 // Tensors of a launch: runs of consecutive values (kRuns without a destination), or
 // matrices with gaps between their rows.  Bit 0 of the pointers (16-byte aligned) says
@@ -61,26 +65,27 @@ __device__ __forceinline__ int find(const L& list, int block) {
     return __builtin_amdgcn_readfirstlane(at);
 }
 
-// Where the thread's vectors of eight values lie: vector i in row `row` from value `col`.
-template <Kind K>
+// Where the thread's vectors of W values lie, in workgroups of G values: vector i in row
+// `row` from value `col`.
+template <Kind K, int W, int G>
 struct Places {
     int64_t cols, row0;
     int32_t rows, ld_src, ld_dst;
     uint32_t rem, per;                               // of the workgroup's first vector, per row
     template <class L>
     __device__ __forceinline__ Places(const L& list, int t, int block) {
-        const int64_t vec0 = (int64_t)(block - list.first[t]) * kGroupVecs;
+        const int64_t vec0 = (int64_t)(block - list.first[t]) * (G / W);
         if constexpr (K == kRowsTo) {
             cols = list.cols[t];
             rows = list.rows[t];
             ld_src = list.ld_src[t];
             ld_dst = list.ld_dst[t];
-            per = (uint32_t)((cols + 7) >> 3);       // a row with gaps has at most 2^22 values
+            per = (uint32_t)((cols + 7) >> 3) * (8 / W);   // a row with gaps has at most 2^22 values
             row0 = vec0 / per;
             rem = (uint32_t)(vec0 - row0 * per);
         } else {
             cols = list.run[t];
-            row0 = vec0 * 8;                         // the first value
+            row0 = vec0 * W;                         // the first value
         }
     }
     struct At {
@@ -92,49 +97,58 @@ struct Places {
         if constexpr (K == kRowsTo) {
             const uint32_t down = (rem + v) / per;
             const int64_t row = row0 + down;
-            return At{row, (int64_t)(rem + v - down * per) * 8, row < rows};
+            return At{row, (int64_t)(rem + v - down * per) * W, row < rows};
         } else {
-            const int64_t col = row0 + (int64_t)v * 8;
+            const int64_t col = row0 + (int64_t)v * W;
             return At{0, col, col < cols};
         }
     }
 };
 
-// Values [c, c + 8) of a row, zeros behind its end.
-template <class T>
-__device__ __forceinline__ Eight<T> load8(const T* row, int64_t c, int64_t cols) {
-    Eight<T> v;
-    if (c + 8 <= cols) {
-        v.load(row + c);
-    } else {
-        float f[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            f[e] = 0.f;
-            if (c + e < cols) {
-                if constexpr (sizeof(T) == 4) f[e] = row[c + e];
-                else f[e] = __uint_as_float((uint32_t)row[c + e] << 16);
-            }
+// W values of a tensor, in the tensor's type.  fp32 values go four at a time, so that a
+// wave's 16-byte accesses lie side by side.  PAST: past the caches.
+template <class T, int W, bool PAST>
+struct Values {
+    typedef T Vec __attribute__((ext_vector_type(W)));
+    Vec w;
+    // values [c, c + W) of a row, zeros behind its end
+    __device__ __forceinline__ void load(const T* row, int64_t c, int64_t cols) {
+        if (c + W <= cols) {
+            const Vec* from = reinterpret_cast<const Vec*>(row + c);
+            if constexpr (PAST) w = __builtin_nontemporal_load(from);
+            else w = *from;
+            return;
         }
-        v.set(f);
-    }
-    return v;
-}
-template <class T>
-__device__ __forceinline__ void store8(T* row, int64_t c, int64_t cols, const float* f) {
-    Eight<T> v;
-    v.set(f);
-    if (c + 8 <= cols) {
-        v.store(row + c);
-        return;
-    }
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (c + e < cols) {
-            if constexpr (sizeof(T) == 4) row[c + e] = f[e];
-            else row[c + e] = (uint16_t)(wave::pack2(f[e], 0.f) & 0xffffu);
+        for (int e = 0; e < W; ++e) w[e] = c + e < cols ? row[c + e] : T(0);
+    }
+    __device__ __forceinline__ void store(T* row, int64_t c, int64_t cols) const {
+        if (c + W <= cols) {
+            Vec* to = reinterpret_cast<Vec*>(row + c);
+            if constexpr (PAST) __builtin_nontemporal_store(w, to);
+            else *to = w;
+            return;
         }
-}
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            if (c + e < cols) row[c + e] = w[e];
+    }
+    __device__ __forceinline__ float get(int e) const {
+        if constexpr (sizeof(T) == 4) return w[e];
+        else return __uint_as_float((uint32_t)w[e] << 16);
+    }
+    __device__ __forceinline__ void set(const float (&v)[W]) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int e = 0; e < W; ++e) w[e] = v[e];
+        } else {
+            uint32_t two[W / 2];
+#pragma unroll
+            for (int e = 0; e < W / 2; ++e) two[e] = wave::pack2(v[2 * e], v[2 * e + 1]);
+            w = __builtin_bit_cast(Vec, two);
+        }
+    }
+};
 
 __device__ __forceinline__ double block_sum(double v, double* red) {
 #pragma unroll
@@ -147,23 +161,23 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
     return v;
 }
 
-template <class T, Kind K>
-__device__ __forceinline__ double squares(const T* src, const Places<K>& p) {
-    Eight<T> in[kVecs];
+template <bool PAST, class T, class L>
+__device__ __forceinline__ double squares(const T* src, const L& list, int t) {
+    constexpr int W = sizeof(T) == 4 ? 4 : 8, N = kSumValues / kThreads / W;
+    constexpr Kind K = L::kind;
+    const Places<K, W, kSumValues> p(list, t, blockIdx.x);
+    Values<T, W, PAST> in[N];
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
+    for (int i = 0; i < N; ++i) {
         const auto a = p.at(i);
-        float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (a.in) in[i] = load8(K == kRowsTo ? src + a.row * p.ld_src : src, a.col, p.cols);
-        else in[i].set(z);
+        if (a.in) in[i].load(K == kRowsTo ? src + a.row * p.ld_src : src, a.col, p.cols);
+        else in[i].w = {};
     }
     double s = 0.0;
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        float f[8];
-        in[i].get(f);
+    for (int i = 0; i < N; ++i) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s += (double)f[e] * (double)f[e];
+        for (int e = 0; e < W; ++e) s += (double)in[i].get(e) * (double)in[i].get(e);
     }
     return s;
 }
@@ -173,14 +187,13 @@ __device__ __forceinline__ T* pointer(uint64_t p) {
     return reinterpret_cast<T*>(p & ~(uint64_t)15);
 }
 
-template <class L>
+template <bool PAST, class L>
 __global__ __launch_bounds__(kThreads) void sq_sum_kernel(L list, double* part) {
     __shared__ double red[kThreads / 64];
     const int t = find(list, blockIdx.x);
-    const Places<L::kind> p(list, t, blockIdx.x);
     const uint64_t src = list.src[t];
-    double s = src & 1 ? squares(pointer<const float>(src), p)
-                       : squares(pointer<const uint16_t>(src), p);
+    double s = src & 1 ? squares<PAST>(pointer<const float>(src), list, t)
+                       : squares<PAST>(pointer<const uint16_t>(src), list, t);
     s = block_sum(s, red);
     if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
@@ -219,49 +232,49 @@ __device__ __forceinline__ float factor_of(const Factor<N>& F) {
     return f;
 }
 
-template <class S, class T, Kind K, int N>
-__device__ __forceinline__ void scaled(const S* src, T* dst, const Places<K>& p,
-                                       const Factor<N>& F) {
-    Eight<S> in[kVecs];
+template <bool PAST, class S, class T, class L, int PARTS>
+__device__ __forceinline__ void scaled(const S* src, T* dst, const L& list, int t,
+                                       const Factor<PARTS>& F) {
+    constexpr int W = sizeof(S) == 4 || sizeof(T) == 4 ? 4 : 8, N = kClipValues / kThreads / W;
+    constexpr Kind K = L::kind;
+    const Places<K, W, kClipValues> p(list, t, blockIdx.x);
+    Values<S, W, PAST> in[N];
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
+    for (int i = 0; i < N; ++i) {
         const auto a = p.at(i);
-        if (a.in) in[i] = load8(K == kRowsTo ? src + a.row * p.ld_src : src, a.col, p.cols);
+        if (a.in) in[i].load(K == kRowsTo ? src + a.row * p.ld_src : src, a.col, p.cols);
     }
     const float f = factor_of(F);                    // while the values come
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
+    for (int i = 0; i < N; ++i) {
         const auto a = p.at(i);
         if (!a.in) continue;
-        float v[8];
-        in[i].get(v);
+        float v[W];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= f;
-        store8(K == kRowsTo ? dst + a.row * p.ld_dst : dst, a.col, p.cols, v);
+        for (int e = 0; e < W; ++e) v[e] = f * in[i].get(e);
+        Values<T, W, PAST> out;
+        out.set(v);
+        out.store(K == kRowsTo ? dst + a.row * p.ld_dst : dst, a.col, p.cols);
     }
 }
 
-// The last spans first: the sum, which ran before, read them last, so that some of
-// their values may still be cached.
-template <class L, int N>
+template <bool PAST, class L, int N>
 __global__ __launch_bounds__(kThreads) void clip_kernel(L list, Factor<N> F) {
     if (list.n == 0) {
         factor_of(F);
         return;
     }
-    const int block = (int)blockIdx.x;
-    const int t = find(list, block);
-    const Places<L::kind> p(list, t, block);
+    const int t = find(list, blockIdx.x);
     const uint64_t src = list.src[t], dst = list.dst[t];
     if (src == dst && factor_of(F) == 1.f) return;   // in place already
     if (src & 1) {
         const float* from = pointer<const float>(src);
-        if (dst & 1) scaled(from, pointer<float>(dst), p, F);
-        else scaled(from, pointer<uint16_t>(dst), p, F);
+        if (dst & 1) scaled<PAST>(from, pointer<float>(dst), list, t, F);
+        else scaled<PAST>(from, pointer<uint16_t>(dst), list, t, F);
     } else {
         const uint16_t* from = pointer<const uint16_t>(src);
-        if (dst & 1) scaled(from, pointer<float>(dst), p, F);
-        else scaled(from, pointer<uint16_t>(dst), p, F);
+        if (dst & 1) scaled<PAST>(from, pointer<float>(dst), list, t, F);
+        else scaled<PAST>(from, pointer<uint16_t>(dst), list, t, F);
     }
 }
 
@@ -269,16 +282,22 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(L list, Factor<N> F) {
 bool is_run(const GradView& g, bool with_dst) {
     return g.rows <= 1 || (g.ld_src == g.cols && (!with_dst || g.ld_dst == g.cols));
 }
-int64_t row_blocks(int64_t rows, int64_t cols) {
-    return (rows * ((cols + 7) / 8) + kGroupVecs - 1) / kGroupVecs;
+int64_t row_blocks(int64_t rows, int64_t cols, int group) {
+    return (rows * ((cols + 7) / 8) + group / 8 - 1) / (group / 8);
 }
 int64_t blocks_of(const GradView& g) {
     if (g.rows == 0 || g.cols == 0) return 0;
-    if (!is_run(g, false)) return row_blocks(g.rows, g.cols);
+    if (!is_run(g, false)) return row_blocks(g.rows, g.cols, kSumValues);
     int64_t blocks = 0;
     for (int64_t left = g.rows * g.cols; left > 0; left -= kMaxRun)
-        blocks += row_blocks(1, std::min(left, kMaxRun));
+        blocks += row_blocks(1, std::min(left, kMaxRun), kSumValues);
     return blocks;
+}
+
+bool past_caches(int n, const GradView* g) {
+    int64_t bytes = 0;
+    for (int i = 0; i < n; ++i) bytes += g[i].rows * g[i].cols * (g[i].src_f32 ? 4 : 2);
+    return bytes > kCachedBytes;
 }
 
 // Collects entries of one kind and calls f(list, workgroups) for every full one.
@@ -307,6 +326,7 @@ template <class Runs, class Rows, class F>
 hipError_t in_launches(int n, const GradView* g, bool with_dst, F f) {
     Launches<Runs, F> runs(f);
     Launches<Rows, F> rows(f);
+    const int group = with_dst ? kClipValues : kSumValues;
     for (int i = 0; i < n; ++i) {
         if (g[i].rows == 0 || g[i].cols == 0) continue;
         const uint64_t src = reinterpret_cast<uint64_t>(g[i].src);
@@ -315,7 +335,7 @@ hipError_t in_launches(int n, const GradView* g, bool with_dst, F f) {
             const int64_t total = g[i].rows * g[i].cols;
             for (int64_t at = 0; at < total; at += kMaxRun) {
                 const int64_t len = std::min(total - at, kMaxRun);
-                const int t = runs.next(row_blocks(1, len));
+                const int t = runs.next(row_blocks(1, len, group));
                 runs.list.src[t] = (src + at * (g[i].src_f32 ? 4 : 2)) | (g[i].src_f32 ? 1 : 0);
                 if (with_dst)
                     runs.list.dst[t] = (dst + at * (g[i].dst_f32 ? 4 : 2)) | (g[i].dst_f32 ? 1 : 0);
@@ -323,7 +343,7 @@ hipError_t in_launches(int n, const GradView* g, bool with_dst, F f) {
             }
             continue;
         }
-        const int t = rows.next(row_blocks(g[i].rows, g[i].cols));
+        const int t = rows.next(row_blocks(g[i].rows, g[i].cols, group));
         rows.list.src[t] = src | (g[i].src_f32 ? 1 : 0);
         rows.list.dst[t] = dst | (g[i].dst_f32 ? 1 : 0);
         rows.list.cols[t] = g[i].cols;
@@ -350,15 +370,18 @@ hipError_t clip(int n, const GradView* g, int nparts, const double* const* parts
     typedef List<kRowsTo, ROWS> Rows;
     static_assert(sizeof(Runs) + sizeof(F) <= 4096 && sizeof(Rows) + sizeof(F) <= 4096,
                   "kernel arguments");
+    const bool past = past_caches(n, g);
     const hipError_t e = in_launches<Runs, Rows>(n, g, true, [&](const auto& L, int64_t blocks) {
-        clip_kernel<<<dim3((unsigned)blocks), kThreads, 0, s>>>(L, F);
+        const dim3 grid((unsigned)blocks);
+        if (past) clip_kernel<true><<<grid, kThreads, 0, s>>>(L, F);
+        else clip_kernel<false><<<grid, kThreads, 0, s>>>(L, F);
         F.norm = nullptr;
         return hipGetLastError();
     });
     if (e != hipSuccess || !F.norm) return e;
     Runs none;                                       // nothing to scale: the norm alone
     none.n = 0;
-    clip_kernel<<<1, 64, 0, s>>>(none, F);
+    clip_kernel<false><<<1, 64, 0, s>>>(none, F);
     return hipGetLastError();
 }
 
@@ -375,8 +398,11 @@ hipError_t launch_grad_sq_sum(int n, const GradView* g, double* sum, double* ws,
     typedef List<kRuns, 250> Runs;
     typedef List<kRowsTo, 80> Rows;
     static_assert(sizeof(Runs) + 8 <= 4096 && sizeof(Rows) + 8 <= 4096, "kernel arguments");
+    const bool past = past_caches(n, g);
     const hipError_t e = in_launches<Runs, Rows>(n, g, false, [&](const auto& L, int64_t blocks) {
-        sq_sum_kernel<<<dim3((unsigned)blocks), kThreads, 0, s>>>(L, ws + done);
+        const dim3 grid((unsigned)blocks);
+        if (past) sq_sum_kernel<true><<<grid, kThreads, 0, s>>>(L, ws + done);
+        else sq_sum_kernel<false><<<grid, kThreads, 0, s>>>(L, ws + done);
         done += blocks;
         return hipGetLastError();
     });

@@ -162,3 +162,24 @@ def test_list_refuses_overlaps_and_shapes():
         atp.atp_grad_sq_sum(atp.grad_list([x[1:9]]), torch.empty(1, dtype=torch.float64,
                                                                  device=DEV),
                             torch.empty(64, dtype=torch.uint8, device=DEV))
+
+
+@pytest.mark.parametrize("st,dt", [(F32, F32), (F32, BF), (BF, F32), (BF, BF)])
+def test_more_than_the_caches_hold(st, dt):
+    # above 128 MiB values go past the caches: runs, rows with gaps and ragged ends in one
+    # list, apart and in place
+    g = torch.Generator(device=DEV).manual_seed(9)
+    shapes = [(7001, 5003), (1, 34000003), (3, 5)]
+    wide = [torch.randn((r, c + 8 - c % 8), device=DEV, generator=g).to(st) for r, c in shapes]
+    src = [w[:, :c] for w, (_, c) in zip(wide, shapes)]
+    assert sum(s.numel() * s.element_size() for s in src) > 128 << 20
+    dst = [torch.full((r, c + 16 - c % 8), float("nan"), dtype=dt, device=DEV) for r, c in shapes]
+    views = [d[:, :c] for d, (_, c) in zip(dst, shapes)]
+    check_clip(src, views, src, 0.5, 1.0, extra=(7.0,))
+    for d, (_, c) in zip(dst, shapes):
+        assert torch.isnan(d[:, c:]).all()
+    if st == dt:
+        gaps = [w[:, c:].clone() for w, (_, c) in zip(wide, shapes)]
+        before = [s.clone() for s in src]
+        check_clip(src, None, before, 0.5, 1.0)
+        assert all(torch.equal(w[:, c:], k) for w, k, (_, c) in zip(wide, gaps, shapes))
