@@ -428,25 +428,36 @@ void docs_fwd_kernel(FwdArgs a) {
                 }
                 return sum;
             };
-            // The first tile sets the reference.  From the back a row may see nothing in it:
-            // m stays -inf, and the next sums are infinite or NaN.
-            const bool first = KG > 1 || (!BACK && i == 0);
-            float rs = 0.f;
-            if (!first) rs = weights(mrun[r]);
-            const bool over = BACK ? !(rs <= kMostSum) : rs > kMostSum;
-            if (first || __builtin_amdgcn_ballot_w64(over) != 0) {
-                // row by row, so that no row's bits depend on its neighbours
-                const bool move = first || row_max4(over ? 1.f : 0.f) > 0.f;
+            // Where the reference moves it does so row by row, so that no row's bits depend on
+            // its neighbours.
+            auto moved = [&](bool move) {
                 const float mnew =
                     move ? fmaxf(mrun[r], score.top(row_max4(max16(s[r])))) : mrun[r];
                 // a row that has seen no key keeps -inf: subtract 0
-                const float msub = mnew == -INFINITY ? 0.f : mnew;
-                const float alpha = __builtin_amdgcn_exp2f(mrun[r] - msub);
+                const float alpha =
+                    __builtin_amdgcn_exp2f(mrun[r] - (mnew == -INFINITY ? 0.f : mnew));
                 lrun[r] *= alpha;
 #pragma unroll
                 for (int dt = 0; dt < 8; ++dt) o[r][dt] *= alpha;
                 mrun[r] = mnew;
-                rs = weights(msub);
+            };
+            float rs = 0.f;
+            if constexpr (KG > 1) {
+                // a group's few tiles: by the maximum of each, when it is 2^8 above
+                const float top = score.top(row_max4(max16(s[r])));
+                const bool move = top > mrun[r] + kSlack;
+                if (__builtin_amdgcn_ballot_w64(move) != 0) moved(move);
+                rs = weights(mrun[r] == -INFINITY ? 0.f : mrun[r]);
+            } else {
+                // The first tile sets the reference.  From the back a row may see nothing in
+                // it: m stays -inf, and the next sums are infinite or NaN.
+                const bool first = !BACK && i == 0;
+                if (!first) rs = weights(mrun[r]);
+                const bool over = BACK ? !(rs <= kMostSum) : rs > kMostSum;
+                if (first || __builtin_amdgcn_ballot_w64(over) != 0) {
+                    moved(first || row_max4(over ? 1.f : 0.f) > 0.f);
+                    rs = weights(mrun[r] == -INFINITY ? 0.f : mrun[r]);
+                }
             }
             lrun[r] += rs;               // the lane's share: a row's four lanes join at the end
         }
@@ -531,7 +542,7 @@ void docs_fwd_kernel(FwdArgs a) {
             }
         }
     } else if (RB == 1 || reach[RB - 1] > 0) {
-        for (; i < min(whole, mine - 1); ++i) {
+        for (; i < (PRODUCERS ? whole : min(whole, mine - 1)); ++i) {
             step(i, b0, bn, no);
             end_step();
         }

@@ -80,7 +80,8 @@ struct Places {
             rows = list.rows[t];
             ld_src = list.ld_src[t];
             ld_dst = list.ld_dst[t];
-            per = (uint32_t)((cols + 7) >> 3) * (8 / W);   // a row with gaps has at most 2^22 values
+            // a row with gaps has at most 2^22 values
+            per = (uint32_t)((cols + 7) >> 3) * (8 / W);
             row0 = vec0 / per;
             rem = (uint32_t)(vec0 - row0 * per);
         } else {
