@@ -26,7 +26,11 @@
 // heads of its key head; where that leaves too few workgroups the heads are divided
 // over several, which leave fp32 sums that are added in order.
 //
-// Bound by the matrix cores and the exponentials together, as the causal core is.
+// Bound by the matrix cores and the vector instructions together, as the causal core is: 20
+// heads of two documents of 4096 rows forward 186 us, 927 TFLOP/s of the visible pairs'
+// products (matrix cores busy 43% of the cycles), backward 680 us, 632 TFLOP/s (dQ 260 us,
+// 48%, dK and dV 450 us, 35%, the waves waiting for LDS 39% of their time); one of 16384
+// rows and 8 heads 508 us and 1903, 1080 and 722 TFLOP/s.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -93,7 +97,8 @@ __device__ __forceinline__ bool ranked_tile(const Common& a, int rank, Doc& doc)
         return __builtin_amdgcn_readfirstlane((int)wave::sum64((float)max(mine - t, 0)));
     };
     if (rank >= above(0)) return false;
-    int lo = 0, hi = (int)((a.tokens + (1 << SHIFT) - 1) >> SHIFT);   // above(lo) > rank >= above(hi)
+    // above(lo) > rank >= above(hi)
+    int lo = 0, hi = (int)((a.tokens + (1 << SHIFT) - 1) >> SHIFT);
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (above(mid) > rank) lo = mid;
@@ -218,7 +223,8 @@ __device__ __forceinline__ uint32_t without_odd(uint32_t w) {
 // products and added to the rows that see them (as their sum with anything is what
 // the weighted sum gives too).
 template <int RB>
-__device__ __forceinline__ void odd_values(const uint16_t* vs, int n_first, const int (&limit)[RB], int g,
+__device__ __forceinline__ void odd_values(const uint16_t* vs, int n_first,
+                                           const int (&limit)[RB], int g,
                            f32x4 (&o)[RB][8]) {
 #pragma unroll 1
     for (int n = 0; n < BN; ++n) {
@@ -571,7 +577,8 @@ void docs_fwd_kernel(FwdArgs a) {
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
 #pragma unroll
-                for (int dt = 0; dt < 8; ++dt) ox[((wave * RB + r) * 8 + dt) * 64 + lane] = o[r][dt];
+                for (int dt = 0; dt < 8; ++dt)
+                    ox[((wave * RB + r) * 8 + dt) * 64 + lane] = o[r][dt];
                 mls[((wave * RB + r) * 2 + 0) * 64 + lane] = mrun[r];
                 mls[((wave * RB + r) * 2 + 1) * 64 + lane] = lrun[r];
             }
@@ -644,13 +651,14 @@ __device__ __forceinline__ void grad_of(const Score<CAP, BIAS>& f, float raw, fl
 
 // dK and dV of a 64-key tile, 16 keys per wave, 32 queries at a time (so that scores and
 // dP take 16 registers each).  KG groups of four waves split the steps (group 0 the
-// first half, group 1 the rest, added through LDS at the end).  32 keys per wave would
-// halve the fragments' reads but leave one wave per SIMD: 20 heads of two documents of
-// 4096 rows took 100 us more.
+// first half, group 1 the rest, added through LDS at the end).  20 heads of two documents
+// of 4096 rows took 100 us more with 32 keys per wave, which halve the fragments' reads
+// but leave one wave per SIMD; 25 us more with the products at a raised wave priority; and
+// 230 us more with the first transposed fragments read ahead of the weights (spills).
 template <int KG, bool CAP, bool BIAS>
 __global__ __launch_bounds__(NTHR * KG, 2 / KG) void docs_dkv_kernel(BwdArgs a) {
     __shared__ __attribute__((aligned(16))) uint16_t qd[KG][2][2][BM * D];   // [grp][buf][Q|dO]
-    __shared__ __attribute__((aligned(16))) float rowv[KG][2][2][BM];       // [grp][buf][lse2|delta]
+    __shared__ __attribute__((aligned(16))) float rowv[KG][2][2][BM];   // [grp][buf][lse2|delta]
     const int lane = threadIdx.x & 63, g = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int grp = wv / NWAVE, wave = wv % NWAVE;
@@ -716,8 +724,8 @@ __global__ __launch_bounds__(NTHR * KG, 2 / KG) void docs_dkv_kernel(BwdArgs a) 
     float(*rv)[2][BM] = rowv[grp];
     float l2r = 0.f, dlr = 0.f;
     if (mine > 0) {
-        cp.issue(a.qkv + qshift + (int64_t)head * D, a.ldq, a.dout + (int64_t)head * D, a.lddo, tok0,
-                 qt * BM, doc.len, qb[0][0], qb[0][1], wave);
+        cp.issue(a.qkv + qshift + (int64_t)head * D, a.ldq, a.dout + (int64_t)head * D, a.lddo,
+                 tok0, qt * BM, doc.len, qb[0][0], qb[0][1], wave);
         load_rows(head, qt, l2r, dlr);
         if (tid < BM) { rv[0][0][tid] = l2r; rv[0][1][tid] = dlr; }
     }
@@ -942,7 +950,8 @@ void docs_dq_kernel(BwdArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     acc += __uint_as_float(o[e] << 16) * __uint_as_float(d[e] << 16);
-                    acc += __uint_as_float(o[e] & 0xffff0000u) * __uint_as_float(d[e] & 0xffff0000u);
+                    acc +=
+                        __uint_as_float(o[e] & 0xffff0000u) * __uint_as_float(d[e] & 0xffff0000u);
                 }
             }
         }
@@ -1073,7 +1082,8 @@ void docs_dq_kernel(BwdArgs a) {
 #pragma unroll
             for (int r = 0; r < RB; ++r)
 #pragma unroll
-                for (int dt = 0; dt < 8; ++dt) x[((wave * RB + r) * 8 + dt) * 64 + lane] = dq[r][dt];
+                for (int dt = 0; dt < 8; ++dt)
+                    x[((wave * RB + r) * 8 + dt) * 64 + lane] = dq[r][dt];
         }
         __syncthreads();
         if (grp == 1) return;
@@ -1098,8 +1108,13 @@ void docs_dq_kernel(BwdArgs a) {
 // ---------------------------------------------------------------------------
 // launches
 // ---------------------------------------------------------------------------
-constexpr int64_t kFwdWideTiles = 512;    // two workgroups of 128 rows per CU
-constexpr int64_t kBwdSplitTiles = 1024;  // 64-row tiles below which loops are split
+// Forward: from two workgroups of 128 rows per CU on; below that 64 rows and two groups of
+// waves for each half of the keys.  8 heads, wide and split: one document of 4096 rows (256
+// tiles) 82 and 52 us, of 4096 and 2048 (384) 85 and 69, two of 4096 (512) 96 and 103.
+constexpr int64_t kFwdWideTiles = 512;
+// Backward: 64-row tiles below which the loops are split.  The same documents, whole and
+// split: 254 and 197 us, 258 and 235, 310 and 350.
+constexpr int64_t kBwdSplitTiles = 1024;
 
 void fill(Common& c, const DocsView& d, const uint16_t* qkv, int64_t ldq, int64_t tokens,
           int kv_heads, int group) {
@@ -1123,7 +1138,8 @@ void fill(Common& c, const DocsView& d, const uint16_t* qkv, int64_t ldq, int64_
 int64_t slots_of(int64_t tokens, int rows, int n_docs) { return tokens / rows + n_docs; }
 
 // Divisions of a group's heads for the dK/dV kernel: as many as it takes for four
-// workgroups per CU.
+// workgroups per CU (16 heads of two key heads, one document of 4096 rows: 317 us; for two
+// workgroups 391, for eight 349).
 int dkv_parts(int64_t tokens, int kv_heads, int group, int* heads) {
     const int64_t tiles = std::max<int64_t>(1, tokens / BM) * kv_heads;
     const int64_t want = std::min<int64_t>(group, (kBwdSplitTiles + tiles - 1) / tiles);

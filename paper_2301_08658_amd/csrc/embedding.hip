@@ -10,7 +10,9 @@
 // some columns in registers, and runs that cross a chunk's end are joined in order.  A row
 // that occurs thousands of times is so shared by many workgroups, nothing is added by
 // atomics, and the result depends on the sizes and tokens alone.  Bound by memory: dy
-// is read once, every row of dW written once (zeros where no token is).
+// is read once, every row of dW written once (zeros where no token is); 8192 rows of
+// 4096 values to fp32 40 us, 4.9 TB/s, the gradient of 4096 rows of 20480 values in 6250
+// rows 155 us, 4.4 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -445,9 +447,13 @@ Plan plan_of(int64_t n, int64_t vocab, int64_t cols) {
     p.key_bits = bit_length((uint64_t)vocab);
     p.few = n <= kCountMax;
     p.tiles = (int)((n + kTile - 1) / kTile);
-    // chunks of 8 tokens for the smallest calls, which have too few, to 32; longer ones
-    // where that makes more than 2048
-    p.chunk = (int)(n < 1024 ? 8 : n < 4096 ? 16 : std::max<int64_t>(32, (n / 2048 + 31) / 32 * 32));
+    // Short chunks fill the chip, long ones leave fewer runs that cross an end.  Gradients
+    // with chunks of 8, 16, 32 and 64 tokens, us: 1024 x 2048 values 20, 24, 32, 50; 4096 x
+    // 4096 33, 32, 37, 54; 4096 x 20480 172, 174, 164, 185; 65536 x 2048 242, 184, 183, 168.
+    // No more than 2048 chunks, which one run may cross.
+    const int64_t values = n * cols;
+    const int64_t chunk = values < 1 << 22 ? 8 : values < 1 << 25 ? 16 : values < 1 << 27 ? 32 : 64;
+    p.chunk = (int)std::max(chunk, ((n + 2047) / 2048 + 7) / 8 * 8);
     p.chunks = (int)((n + p.chunk - 1) / p.chunk);
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
@@ -467,7 +473,9 @@ Plan plan_of(int64_t n, int64_t vocab, int64_t cols) {
     return p;
 }
 
-// Tokens of a workgroup: 16, so that 4096 tokens take every CU.
+// Tokens of a workgroup: 16, so that 4096 tokens take every CU (their places 5.2 us; the
+// whole gradient of 4096 tokens of 20480 values by counted places 164 us, by the passes
+// over digits 212, of 16384 of 4096 73 and 112).
 template <class K, int REGS, int TOK>
 void few(const EmbeddingBwdProblem& p, int shift, uint32_t* keys, uint32_t* order, hipStream_t s) {
     sort_few_kernel<K, REGS, TOK>

@@ -498,7 +498,8 @@ atp_status atp_attention_docs_fwd(int64_t tokens, int32_t kv_heads, int32_t grou
                                   const atp_attention_docs* docs, const void* qkv, int64_t ld_qkv,
                                   void* out, int64_t ld_out, float* lse, void* stream) {
     ATP_CHECK(check_docs(docs, tokens, kv_heads, group));
-    const int64_t cols = (int64_t)kv_heads * (group + 2) * 128, ocols = (int64_t)kv_heads * group * 128;
+    const int64_t cols = (int64_t)kv_heads * (group + 2) * 128;
+    const int64_t ocols = (int64_t)kv_heads * group * 128;
     ATP_CHECK(check_matrix(qkv, tokens, ld_qkv, cols, "qkv"));
     ATP_CHECK(check_matrix(out, tokens, ld_out, ocols, "out"));
     if (tokens == 0 || docs->n_docs == 0) return ATP_OK;
@@ -532,7 +533,8 @@ atp_status atp_attention_docs_bwd(int64_t tokens, int32_t kv_heads, int32_t grou
                                   const void* d_out, int64_t ld_dout, void* d_qkv, int64_t ld_dqkv,
                                   void* workspace, size_t ws_bytes, void* stream) {
     ATP_CHECK(check_docs(docs, tokens, kv_heads, group));
-    const int64_t cols = (int64_t)kv_heads * (group + 2) * 128, ocols = (int64_t)kv_heads * group * 128;
+    const int64_t cols = (int64_t)kv_heads * (group + 2) * 128;
+    const int64_t ocols = (int64_t)kv_heads * group * 128;
     ATP_CHECK(check_matrix(qkv, tokens, ld_qkv, cols, "qkv"));
     ATP_CHECK(check_matrix(out, tokens, ld_out, ocols, "out"));
     ATP_CHECK(check_matrix(d_out, tokens, ld_dout, ocols, "d_out"));
