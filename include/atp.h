@@ -817,7 +817,7 @@ atp_status atp_embedding_fwd(int64_t tokens, const int32_t* ids, int64_t vocab_l
 
 /* Gradient of the table (Sec. 4.2, dW = X^T dY):
  *   dtable[v, :] = scale * sum over t with ids[t] = vocab_off + v of dy[t, :],
- * the sum in fp32 over ascending t, in pieces that depend on `tokens` and the ids
+ * the sum in fp32 over ascending t, in pieces that depend on the sizes and the ids
  * alone.  dy: bf16 [tokens, cols].  dtable: fp32 [vocab_loc, cols]; accumulate 0:
  * every row is written (zeros for rows without tokens); 1: the sums are added to
  * it and rows without tokens are not touched (a table that is the output
