@@ -927,8 +927,9 @@ atp_status atp_attention_docs_fwd(int64_t tokens, int32_t kv_heads, int32_t grou
 /* Gradient of atp_attention_docs_fwd: out and lse are the forward's, d_out (bf16) the
  * gradient of out, d_qkv (bf16) receives dq, dk, dv of the documents' rows in qkv's
  * layout and must not overlap qkv, out or d_out.  dk and dv are summed in fp32 over the
- * group's query heads.  An infinity or NaN in a document may reach all gradients of that
- * document, and no other.  workspace: atp_attention_docs_workspace_bytes() bytes,
+ * group's query heads.  The weights are formed again from lse, whose last bit moves
+ * them by |lse| 2^-23 of themselves; scores of 2^30 and more have no defined gradient.
+ * An infinity or NaN in a document may reach all gradients of that document, and no other.  workspace: atp_attention_docs_workspace_bytes() bytes,
  * scratch.  Errors as atp_attention_docs_fwd; INVALID_ARGUMENT for a short
  * workspace. */
 atp_status atp_attention_docs_bwd(int64_t tokens, int32_t kv_heads, int32_t group,

@@ -199,6 +199,15 @@ struct Score {
                 __builtin_fmaf(rest_of(v), -2.f * cap_log2, cap_log2 - m));
         return __builtin_amdgcn_exp2f(__builtin_fmaf(v, scale, -m));
     }
+    // The same with the product rounded as m's was: 1 at the maximum however large the
+    // scores are, where the product's own last bits, kept by a fused step, pass 2^7 from
+    // scores of 2^31 on.
+    __device__ __forceinline__ float weight_at_top(float v, float m) const {
+#pragma clang fp contract(off)
+        if constexpr (CAP) return weight(v, m);
+        const float x = v * scale;
+        return __builtin_amdgcn_exp2f(x - m);
+    }
 };
 
 // ---------------------------------------------------------------------------
@@ -335,6 +344,8 @@ void docs_fwd_kernel(FwdArgs a) {
         reach[r] = top < doc.len ? max(min(top + 64, doc.len), doc.prefix) : 0;
     }
     // One key tile for the row blocks [R0, R1), those that see some of it.
+    const std::integral_constant<int, 0> b0;
+    const std::integral_constant<int, 1> b1;
     // Without masks there is a next tile, whose copies then stand between the products without
     // a branch, so that a slice's fragments are read while the slice before is multiplied.
     auto step = [&](int i, auto r0, auto r1, auto mask) {
@@ -415,7 +426,7 @@ void docs_fwd_kernel(FwdArgs a) {
         bf16x8 pf[RB][2];
 #pragma unroll
         for (int r = R0; r < R1; ++r) {
-            auto weights = [&](float m) {
+            auto weights = [&](auto form, float m, bool moved) {
                 float sum = 0.f;
 #pragma unroll
                 for (int j = 0; j < 4; j += 2) {
@@ -424,7 +435,13 @@ void docs_fwd_kernel(FwdArgs a) {
                     for (int k = 0; k < 2; ++k)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            p[k][e] = score.weight(s[r][j + k][e], m);
+                            const float x = s[r][j + k][e];
+                            if constexpr (decltype(form)::value == 0)
+                                p[k][e] = score.weight(x, m);
+                            else if constexpr (KG > 1)
+                                p[k][e] = score.weight_at_top(x, m);
+                            else
+                                p[k][e] = moved ? score.weight_at_top(x, m) : score.weight(x, m);
                             // a cap makes a finite score of a masked one's -inf
                             if constexpr (MASKED && CAP && !BIAS)
                                 if (kt * BN + 16 * (j + k) + 4 * g + e >= limit[r]) p[k][e] = 0.f;
@@ -436,7 +453,7 @@ void docs_fwd_kernel(FwdArgs a) {
             };
             // Where the reference moves it does so row by row, so that no row's bits depend on
             // its neighbours.
-            auto moved = [&](bool move) {
+            auto move_to_top = [&](bool move) {
                 const float mnew =
                     move ? fmaxf(mrun[r], score.top(row_max4(max16(s[r])))) : mrun[r];
                 // a row that has seen no key keeps -inf: subtract 0
@@ -452,17 +469,19 @@ void docs_fwd_kernel(FwdArgs a) {
                 // a group's few tiles: by the maximum of each, when it is 2^8 above
                 const float top = score.top(row_max4(max16(s[r])));
                 const bool move = top > mrun[r] + kSlack;
-                if (__builtin_amdgcn_ballot_w64(move) != 0) moved(move);
-                rs = weights(mrun[r] == -INFINITY ? 0.f : mrun[r]);
+                if (__builtin_amdgcn_ballot_w64(move) != 0) move_to_top(move);
+                rs = weights(b1, mrun[r] == -INFINITY ? 0.f : mrun[r], true);
             } else {
-                // The first tile sets the reference.  From the back a row may see nothing in
-                // it: m stays -inf, and the next sums are infinite or NaN.
+                // The first tile sets the reference.  Where a row sees nothing in it (from the
+                // back) or scores of -inf alone, m stays -inf, and the next sums are infinite
+                // or NaN.
                 const bool first = !BACK && i == 0;
-                if (!first) rs = weights(mrun[r]);
-                const bool over = BACK ? !(rs <= kMostSum) : rs > kMostSum;
+                if (!first) rs = weights(b0, mrun[r], false);
+                const bool over = !(rs <= kMostSum);
                 if (first || __builtin_amdgcn_ballot_w64(over) != 0) {
-                    moved(first || row_max4(over ? 1.f : 0.f) > 0.f);
-                    rs = weights(mrun[r] == -INFINITY ? 0.f : mrun[r]);
+                    const bool move = first || row_max4(over ? 1.f : 0.f) > 0.f;
+                    move_to_top(move);
+                    rs = weights(b1, mrun[r] == -INFINITY ? 0.f : mrun[r], move);
                 }
             }
             lrun[r] += rs;               // the lane's share: a row's four lanes join at the end
@@ -508,8 +527,6 @@ void docs_fwd_kernel(FwdArgs a) {
         }
         add_values(std::false_type{});
     };
-    const std::integral_constant<int, 0> b0;
-    const std::integral_constant<int, 1> b1;
     const std::integral_constant<int, RB> bn;
     const std::true_type yes;
     const std::false_type no;

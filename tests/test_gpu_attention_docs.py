@@ -256,3 +256,24 @@ def test_nothing():
     empty = atp.attention_docs(ints([0, 0, 0]))
     atp.atp_attention_docs_fwd(r.t, 1, 1, empty, r.qkv, out[:r.t, :D], lse)
     assert torch.isnan(out).all() and torch.isnan(lse).all()
+
+
+@pytest.mark.parametrize("kv,n,slopes", [(2, 300, False), (2, 300, True), (16, 4096, False),
+                                         (16, 4096, True)])
+def test_seen_scores_of_minus_infinity_weigh_nothing(kv, n, slopes):
+    # a first tile of such scores, and some among others: what scores of -1e30 give, whose
+    # weights are exactly zero beside any other (rows that see nothing else are NaN)
+    run = Run([n], kv, 1, slopes=slopes)
+    got = []
+    for low in (-float("inf"), -1e30):
+        qkv = run.qkv.clone()
+        heads = qkv.view(n, kv, 3, D)
+        heads[:, :, 0, 0] = heads[:, :, 0, 0].abs() + 0.5
+        for at in (slice(0, 64), slice(70, 76), slice(190, 191)):
+            heads[at, :, 1, 0] = low
+        out, lse = run.forward(qkv)
+        got.append((out[64:n, :run.heads * D], lse[:, 64:]))
+    (out, lse), (out0, lse0) = got
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    assert torch.equal(out.view(torch.int16), out0.view(torch.int16))
+    assert torch.equal(lse, lse0)
