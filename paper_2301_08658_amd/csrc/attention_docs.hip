@@ -1125,13 +1125,22 @@ void docs_dq_kernel(BwdArgs a) {
 // ---------------------------------------------------------------------------
 // launches
 // ---------------------------------------------------------------------------
-// Forward: from two workgroups of 128 rows per CU on; below that 64 rows and two groups of
-// waves for each half of the keys.  8 heads, wide and split: one document of 4096 rows (256
-// tiles) 82 and 52 us, of 4096 and 2048 (384) 85 and 69, two of 4096 (512) 96 and 103.
-constexpr int64_t kFwdWideTiles = 512;
-// Backward: 64-row tiles below which the loops are split.  The same documents, whole and
-// split: 254 and 197 us, 258 and 235, 310 and 350.
-constexpr int64_t kBwdSplitTiles = 1024;
+// The kernels of 128 rows (64 keys for dK and dV) are taken where they leave `full_tiles`
+// 64-row tiles of all heads; below that those of 64 rows whose loops are split over two
+// groups of waves.  These halve the long loops of an emptier chip, but take twice the
+// starts, which is most of a short document's time: four tiles per CU for documents of more
+// than 2048 rows on the average, fewer for shorter ones (empty documents count).  Whole and
+// split, forward + backward, us:
+//   rows of 128: 288 tiles 11 + 25 and 14 + 36;
+//   of 520: 292 tiles 20 + 47 and 17 + 42, 584 tiles 22 + 54 and 26 + 71;
+//   of 1024: 512 tiles 27 + 75 and 24 + 68, 768 tiles 30 + 84 and 35 + 100;
+//   of 2048: 512 tiles 44 + 131 and 33 + 102, 768 tiles 48 + 140 and 49 + 154;
+//   of 4096 and 2048: 768 tiles 85 + 253 and 69 + 211; of 4096: 1024 tiles 96 + 310 and
+//   103 + 350.
+int64_t full_tiles(int64_t tokens, int n_docs) {
+    const int64_t rows = tokens / n_docs;
+    return 256 * (rows < 256 ? 1 : rows < 1024 ? 2 : rows <= 2048 ? 3 : 4);
+}
 
 void fill(Common& c, const DocsView& d, const uint16_t* qkv, int64_t ldq, int64_t tokens,
           int kv_heads, int group) {
@@ -1154,12 +1163,19 @@ void fill(Common& c, const DocsView& d, const uint16_t* qkv, int64_t ldq, int64_
 // Slots of tiles of `rows` rows: up to cu[n] / rows + n.
 int64_t slots_of(int64_t tokens, int rows, int n_docs) { return tokens / rows + n_docs; }
 
-// Divisions of a group's heads for the dK/dV kernel: as many as it takes for four
-// workgroups per CU (16 heads of two key heads, one document of 4096 rows: 317 us; for two
-// workgroups 391, for eight 349).
-int dkv_parts(int64_t tokens, int kv_heads, int group, int* heads) {
+// Divisions of a group's heads for the dK/dV kernel: as many as it takes for `tiles` of 64
+// keys.  Four per CU (16 heads of two key heads, one document of 4096 rows: 317 us; for two
+// per CU 391, for eight 349); where documents have fewer than 512 rows, what fills the chip,
+// since each division starts anew and leaves sums to be joined (backward of 36 documents
+// of 128 rows, 4 key heads of 3 query heads: 61 and 43 us; of 20 of 300, 12 heads of one key
+// head: 84 and 70; of 9 of 520 the same, with prefixes 119 and 146).
+constexpr int64_t kPartTiles = 1024;
+int64_t part_tiles(int64_t tokens, int n_docs) {
+    return tokens / n_docs < 512 ? full_tiles(tokens, n_docs) : kPartTiles;
+}
+int dkv_parts(int64_t tokens, int kv_heads, int group, int64_t most, int* heads) {
     const int64_t tiles = std::max<int64_t>(1, tokens / BM) * kv_heads;
-    const int64_t want = std::min<int64_t>(group, (kBwdSplitTiles + tiles - 1) / tiles);
+    const int64_t want = std::min<int64_t>(group, (most + tiles - 1) / tiles);
     *heads = (int)((group + want - 1) / want);
     return (group + *heads - 1) / *heads;
 }
@@ -1174,7 +1190,8 @@ void fwd(FwdArgs& a, hipStream_t s) {
 }
 template <bool CAP, bool BIAS>
 void fwd_of(FwdArgs& a, hipStream_t s) {
-    if ((a.tokens + 127) / 128 * a.kv_heads * a.group >= kFwdWideTiles) fwd<2, 1, CAP, BIAS>(a, s);
+    const int64_t tiles = (a.tokens + 127) / 128 * a.kv_heads * a.group;
+    if (2 * tiles >= full_tiles(a.tokens, a.n_docs)) fwd<2, 1, CAP, BIAS>(a, s);
     else fwd<1, 2, CAP, BIAS>(a, s);
 }
 
@@ -1182,7 +1199,8 @@ template <bool CAP, bool BIAS>
 void bwd_of(BwdArgs& a, hipStream_t s) {
     const int heads = a.kv_heads * a.group;
     const int64_t s64 = slots_of(a.tokens, 64, a.n_docs);
-    const bool split = (a.tokens + 63) / 64 * heads < kBwdSplitTiles;
+    const int64_t full = full_tiles(a.tokens, a.n_docs);
+    const bool split = (a.tokens + 63) / 64 * heads < full;
     if (split) {
         a.slots = (int)s64;
         docs_dq_kernel<1, 2, CAP, BIAS>
@@ -1194,7 +1212,7 @@ void bwd_of(BwdArgs& a, hipStream_t s) {
     }
     const int per_slot = a.kv_heads * a.parts;
     a.slots = (int)s64;
-    if ((a.tokens + 63) / 64 * per_slot < kBwdSplitTiles) {
+    if ((a.tokens + 63) / 64 * per_slot < full) {
         docs_dkv_kernel<2, CAP, BIAS><<<dim3((unsigned)(s64 * per_slot)), 2 * NTHR, 0, s>>>(a);
     } else {
         docs_dkv_kernel<1, CAP, BIAS><<<dim3((unsigned)(s64 * per_slot)), NTHR, 0, s>>>(a);
@@ -1205,7 +1223,8 @@ void bwd_of(BwdArgs& a, hipStream_t s) {
 
 int64_t docs_attention_ws_floats(int64_t tokens, int kv_heads, int group) {
     int heads;
-    const int parts = dkv_parts(tokens, kv_heads, group, &heads);
+    // for any number of documents: fewer tiles never give more parts
+    const int parts = dkv_parts(tokens, kv_heads, group, kPartTiles, &heads);
     return delta_floats(tokens, kv_heads * group) +
            (parts > 1 ? (int64_t)parts * tokens * kv_heads * 2 * D : 0);
 }
@@ -1237,7 +1256,8 @@ hipError_t launch_docs_attention_bwd(const DocsAttentionBwdProblem& p, hipStream
     a.delta = p.ws;
     a.sums = p.ws + delta_floats(p.tokens, p.kv_heads * p.group);
     a.dqkv = p.dqkv; a.lddq = p.lddq;
-    a.parts = dkv_parts(p.tokens, p.kv_heads, p.group, &a.part_heads);
+    a.parts = dkv_parts(p.tokens, p.kv_heads, p.group, part_tiles(p.tokens, p.docs.n_docs),
+                        &a.part_heads);
     a.inv_sqrt_d = 1.0f / sqrtf((float)D);
     if (p.docs.cap > 0.f) {
         if (p.docs.slopes) bwd_of<true, true>(a, s);

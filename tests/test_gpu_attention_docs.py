@@ -277,3 +277,13 @@ def test_seen_scores_of_minus_infinity_weigh_nothing(kv, n, slopes):
     assert torch.isfinite(out).all() and torch.isfinite(lse).all()
     assert torch.equal(out.view(torch.int16), out0.view(torch.int16))
     assert torch.equal(lse, lse0)
+
+
+@pytest.mark.parametrize("kv,group,kw", [(4, 3, {}), (1, 12, dict(slopes=True)),
+                                         (8, 1, dict(cap=20.0)),
+                                         (2, 5, dict(slopes=True, cap=9.0))])
+def test_many_short_documents(kv, group, kw):
+    # enough tiles for the kernels of 128 rows, though no document has many
+    lens = [1 + 37 * d % 250 for d in range(30)]
+    prefix = [0 if d % 3 else n // 2 for d, n in enumerate(lens)] if kw.get("slopes") else None
+    Run(lens, kv, group, prefix=prefix, first=2, behind=61, seed=kv, **kw).check()
