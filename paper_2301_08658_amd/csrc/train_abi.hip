@@ -172,7 +172,7 @@ atp_status check_side(const void* p, int64_t rows, int64_t cols, int64_t ld, int
                          (long long)ld, (long long)cols);
     if (ld != cols && (ld % 8 != 0 || ld > kMaxLd))
         return set_error(ATP_ERR_UNSUPPORTED,
-                         "gradient %d: ld_%s %lld of rows with gaps must be a multiple of 8 up to 4M",
+                         "gradient %d: ld_%s %lld of rows with gaps is no multiple of 8 up to 4M",
                          i, name, (long long)ld);
     return ATP_OK;
 }
