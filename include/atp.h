@@ -900,7 +900,9 @@ size_t atp_layer_norm_workspace_bytes(int64_t tokens, int64_t cols);
  * rows sees its rows j <= i, and the first prefix[d] rows (int32 [n_docs], nullable;
  * cut to [0, n]).  Scores: x = q . k / sqrt(128), with cap > 0 cap * tanh(x / cap), then
  * minus slopes[head] * |i - j| (fp32 [kv_heads * group], nullable; constants: they
- * get no gradient).  At most 65536 documents.  Lists that do not ascend or leave
+ * get no gradient).  A cap of up to 64 moves a score by up to 6 * 2^-24 of the cap beside
+ * fp32's roundings of the product, a larger one, up to 2^100, by up to 2^-18 of the
+ * score.  At most 65536 documents.  Lists that do not ascend or leave
  * the rows give undefined results, but no access outside the buffers. */
 typedef struct {
     const int32_t* cu_docs;
@@ -919,7 +921,7 @@ typedef struct {
  * row does not see hold does not reach its result.
  * Errors: INVALID_ARGUMENT for negative sizes, kv_heads or group < 1, NULL buffers,
  * a negative or non-finite cap, overlap; UNSUPPORTED for more than 2^24 tokens, the
- * limits above, 2^31 tiles of 64 rows and heads, misalignment. */
+ * limits above, a cap above 2^100, 2^31 tiles of 64 rows and heads, misalignment. */
 atp_status atp_attention_docs_fwd(int64_t tokens, int32_t kv_heads, int32_t group,
                                   const atp_attention_docs* docs, const void* qkv, int64_t ld_qkv,
                                   void* out, int64_t ld_out, float* lse, void* stream);

@@ -32,6 +32,7 @@
 // 48%, dK and dV 450 us, 35%, the waves waiting for LDS 39% of their time); one of 16384
 // rows and 8 heads 508 us and 1903, 1080 and 722 TFLOP/s.
 #include <hip/hip_runtime.h>
+#include <float.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -62,6 +63,7 @@ struct Common {
     int n_docs, kv_heads, group, slots;
     float scale_log2;                    // log2(e) / sqrt(D)
     float cap_in, cap_log2;              // 2 log2(e) / (sqrt(D) cap), cap log2(e)
+    float cap_y;                         // 1 / (sqrt(D) cap)
     float root_d;                        // sqrt(D)
 };
 
@@ -154,15 +156,26 @@ __device__ __forceinline__ bool find_tile(const Common& a, int i, Doc& doc) {
     return __builtin_amdgcn_readfirstlane(ok);
 }
 
+// How scores are capped: by 1 - 2 / (1 + e^(2 y)) alone, which is off by up to 6 u of the
+// cap however small the score is, or, for caps whose 6 u are no longer small beside the
+// weights' rounding to bf16, by that where |y| >= 1/4 and by the series of tanh below (off by
+// 2^-18 of the score).  The series takes 30% more time (20 heads of two documents of 4096
+// rows forward 211 and 271 us, backward 767 and 994), so caps of up to kSmallCap do
+// without: 6 u 64 = 2.3e-5 against the weights' 2^-9.
+enum Cap { kNoCap, kSmall, kLarge };
+constexpr float kSmallCap = 64.f;
+
 // What is done to raw products q . k.  A bias alone is what the products are added to
-// (in their units), a cap alone keeps their order, so that both keep the raw maximum; cap
-// and bias together are formed for every score before it.
-template <bool CAP, bool BIAS>
+// (in their units), a cap alone keeps their order (a large one but for its roundings), so
+// that both keep the raw maximum; cap and bias together are formed for every score before
+// it.
+template <Cap CAP, bool BIAS>
 struct Score {
     static constexpr bool kFormed = CAP && BIAS;
-    float scale, cap_in, cap_log2, slope, slope_raw;
+    float scale, cap_in, cap_log2, cap_y, slope, slope_raw;
     __device__ __forceinline__ Score(const Common& a, int head)
-        : scale(a.scale_log2), cap_in(a.cap_in), cap_log2(a.cap_log2), slope(0.f), slope_raw(0.f) {
+        : scale(a.scale_log2), cap_in(a.cap_in), cap_log2(a.cap_log2), cap_y(a.cap_y), slope(0.f),
+          slope_raw(0.f) {
         if constexpr (BIAS) {
             slope = a.slopes[head] * kLog2e;
             slope_raw = a.slopes[head] * a.root_d;
@@ -173,13 +186,23 @@ struct Score {
         if constexpr (BIAS && !CAP) return -slope_raw * __builtin_fabsf(dist);
         return 0.f;
     }
-    // tanh(y) = 1 - 2 r, r = 1 / (1 + e^(2 y)): off by 2^-23 of 1 at most, which moves a
-    // score of cap 50 by 6e-6
+    // tanh(y) = 1 - 2 r, r = 1 / (1 + e^(2 y))
     __device__ __forceinline__ float rest_of(float raw) const {
         return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(raw * cap_in));
     }
+    __device__ __forceinline__ float capped_of(float raw, float r) const {
+        const float whole = __builtin_fmaf(r, -2.f * cap_log2, cap_log2);
+        if constexpr (CAP != kLarge) return whole;
+        // tanh(y) / y to y^8: the rest is below 2^-26 up to 1/4
+        const float y = raw * cap_y, y2 = y * y;
+        float t = __builtin_fmaf(y2, 62.f / 2835.f, -17.f / 315.f);
+        t = __builtin_fmaf(y2, t, 2.f / 15.f);
+        t = __builtin_fmaf(y2, t, -1.f / 3.f);
+        t = __builtin_fmaf(y2, t, 1.f);
+        return __builtin_fabsf(y) < 0.25f ? raw * scale * t : whole;
+    }
     __device__ __forceinline__ float capped(float raw) const {
-        return __builtin_fmaf(rest_of(raw), -2.f * cap_log2, cap_log2);
+        return capped_of(raw, rest_of(raw));
     }
     __device__ __forceinline__ float bias(float x, float dist) const {
         if constexpr (kFormed) return __builtin_fmaf(-slope, __builtin_fabsf(dist), x);
@@ -194,16 +217,22 @@ struct Score {
     // 2^(score - m) of a raw (or formed) value
     __device__ __forceinline__ float weight(float v, float m) const {
         if constexpr (kFormed) return __builtin_amdgcn_exp2f(v - m);
-        if constexpr (CAP)
+        if constexpr (CAP == kLarge) return __builtin_amdgcn_exp2f(capped(v) - m);
+        if constexpr (CAP == kSmall)
             return __builtin_amdgcn_exp2f(
                 __builtin_fmaf(rest_of(v), -2.f * cap_log2, cap_log2 - m));
         return __builtin_amdgcn_exp2f(__builtin_fmaf(v, scale, -m));
     }
     // The same with the product rounded as m's was: 1 at the maximum however large the
     // scores are, where the product's own last bits, kept by a fused step, pass 2^7 from
-    // scores of 2^31 on.
+    // scores of 2^31 on.  Below m + kSlack where m is the maximum or at most so much less;
+    // large caps' roundings may pass it where the series ends.
     __device__ __forceinline__ float weight_at_top(float v, float m) const {
 #pragma clang fp contract(off)
+        if constexpr (CAP == kLarge && !BIAS) {
+            const float x = capped(v) - m;
+            return __builtin_amdgcn_exp2f(x > kSlack ? kSlack : x);    // NaN stays
+        }
         if constexpr (CAP) return weight(v, m);
         const float x = v * scale;
         return __builtin_amdgcn_exp2f(x - m);
@@ -254,7 +283,7 @@ __device__ __forceinline__ void odd_values(const uint16_t* vs, int n_first,
     }
 }
 
-template <int RB, int KG, bool CAP, bool BIAS>
+template <int RB, int KG, Cap CAP, bool BIAS>
 __global__ __launch_bounds__(NTHR * KG + (KG > 1 ? NTHR : 0), KG > 1 ? 3 : 2)
 void docs_fwd_kernel(FwdArgs a) {
     constexpr int QT = 64 * RB;
@@ -649,14 +678,17 @@ struct BwdArgs : Common {
 };
 
 // P and dS of one element from the raw score, dO . v, and the row's lse and delta.
-template <bool CAP, bool BIAS>
+template <Cap CAP, bool BIAS>
 __device__ __forceinline__ void grad_of(const Score<CAP, BIAS>& f, float raw, float dist, float l2,
                                         float dl, bool hidden, float& p, float& ds) {
     float pv, d;
     if constexpr (CAP) {
         const float r = f.rest_of(raw), r4 = 4.f * r;
-        pv = __builtin_amdgcn_exp2f(
-            f.bias(__builtin_fmaf(r, -2.f * f.cap_log2, f.cap_log2 - l2), dist));
+        if constexpr (CAP == kLarge)
+            pv = __builtin_amdgcn_exp2f(f.bias(f.capped_of(raw, r) - l2, dist));
+        else
+            pv = __builtin_amdgcn_exp2f(
+                f.bias(__builtin_fmaf(r, -2.f * f.cap_log2, f.cap_log2 - l2), dist));
         d = pv * (ds - dl) * __builtin_fmaf(-r4, r, r4);     // 1 - tanh^2 = 4 r (1 - r)
     } else {
         pv = __builtin_amdgcn_exp2f(__builtin_fmaf(raw, f.scale, -l2));
@@ -672,7 +704,7 @@ __device__ __forceinline__ void grad_of(const Score<CAP, BIAS>& f, float raw, fl
 // of 4096 rows took 100 us more with 32 keys per wave, which halve the fragments' reads
 // but leave one wave per SIMD; 25 us more with the products at a raised wave priority; and
 // 230 us more with the first transposed fragments read ahead of the weights (spills).
-template <int KG, bool CAP, bool BIAS>
+template <int KG, Cap CAP, bool BIAS>
 __global__ __launch_bounds__(NTHR * KG, 2 / KG) void docs_dkv_kernel(BwdArgs a) {
     __shared__ __attribute__((aligned(16))) uint16_t qd[KG][2][2][BM * D];   // [grp][buf][Q|dO]
     __shared__ __attribute__((aligned(16))) float rowv[KG][2][2][BM];   // [grp][buf][lse2|delta]
@@ -802,6 +834,9 @@ __global__ __launch_bounds__(NTHR * KG, 2 / KG) void docs_dkv_kernel(BwdArgs a) 
                                 rv[buf][1][ql], hidden, pv, dsv);
                         p[jj][e] = pv;
                         d[jj][e] = dsv;
+                        // two at a time: with the series of all eight more spills (1024 us)
+                        if constexpr (CAP == kLarge)
+                            if (e & 1) __builtin_amdgcn_sched_barrier(0);
                     }
                 const bf16x8 pf = pack_pair(p[0], p[1]), sf = pack_pair(d[0], d[1]);
 #pragma unroll
@@ -895,7 +930,7 @@ __global__ __launch_bounds__(256) void docs_join_kernel(BwdArgs a) {
     o.store(a.dqkv + t * a.lddq + ((int64_t)kvh * (a.group + 2) + a.group) * D + c);
 }
 
-template <int RB, int KG, bool CAP, bool BIAS>
+template <int RB, int KG, Cap CAP, bool BIAS>
 __global__ __launch_bounds__(NTHR * KG + (KG > 1 ? NTHR : 0), KG > 1 ? 3 : 2)
 void docs_dq_kernel(BwdArgs a) {
     constexpr int QT = 64 * RB;
@@ -1157,7 +1192,9 @@ void fill(Common& c, const DocsView& d, const uint16_t* qkv, int64_t ldq, int64_
     const float root = sqrtf((float)D);
     c.scale_log2 = kLog2e / root;
     c.root_d = root;
-    c.cap_in = d.cap > 0.f ? 2.f * kLog2e / (root * d.cap) : 0.f;
+    // finite for the smallest caps too: products of 0 score 0
+    c.cap_in = d.cap > 0.f ? std::min(2.f * kLog2e / (root * d.cap), FLT_MAX) : 0.f;
+    c.cap_y = d.cap > 0.f ? std::min(1.f / (root * d.cap), FLT_MAX) : 0.f;
     c.cap_log2 = d.cap * kLog2e;
 }
 // Slots of tiles of `rows` rows: up to cu[n] / rows + n.
@@ -1181,21 +1218,21 @@ int dkv_parts(int64_t tokens, int kv_heads, int group, int64_t most, int* heads)
 }
 int64_t delta_floats(int64_t tokens, int heads) { return (tokens * heads + 63) / 64 * 64; }
 
-template <int RB, int KG, bool CAP, bool BIAS>
+template <int RB, int KG, Cap CAP, bool BIAS>
 void fwd(FwdArgs& a, hipStream_t s) {
     a.slots = (int)slots_of(a.tokens, 64 * RB, a.n_docs);
     docs_fwd_kernel<RB, KG, CAP, BIAS>
         <<<dim3((unsigned)((int64_t)a.slots * a.kv_heads * a.group)), KG > 1 ? 3 * NTHR : NTHR, 0,
            s>>>(a);
 }
-template <bool CAP, bool BIAS>
+template <Cap CAP, bool BIAS>
 void fwd_of(FwdArgs& a, hipStream_t s) {
     const int64_t tiles = (a.tokens + 127) / 128 * a.kv_heads * a.group;
     if (2 * tiles >= full_tiles(a.tokens, a.n_docs)) fwd<2, 1, CAP, BIAS>(a, s);
     else fwd<1, 2, CAP, BIAS>(a, s);
 }
 
-template <bool CAP, bool BIAS>
+template <Cap CAP, bool BIAS>
 void bwd_of(BwdArgs& a, hipStream_t s) {
     const int heads = a.kv_heads * a.group;
     const int64_t s64 = slots_of(a.tokens, 64, a.n_docs);
@@ -1236,12 +1273,15 @@ hipError_t launch_docs_attention(const DocsAttentionProblem& p, hipStream_t s) {
     a.out = p.out;
     a.ldo = p.ldo;
     a.lse = p.lse;
-    if (p.docs.cap > 0.f) {
-        if (p.docs.slopes) fwd_of<true, true>(a, s);
-        else fwd_of<true, false>(a, s);
+    if (p.docs.cap > kSmallCap) {
+        if (p.docs.slopes) fwd_of<kLarge, true>(a, s);
+        else fwd_of<kLarge, false>(a, s);
+    } else if (p.docs.cap > 0.f) {
+        if (p.docs.slopes) fwd_of<kSmall, true>(a, s);
+        else fwd_of<kSmall, false>(a, s);
     } else {
-        if (p.docs.slopes) fwd_of<false, true>(a, s);
-        else fwd_of<false, false>(a, s);
+        if (p.docs.slopes) fwd_of<kNoCap, true>(a, s);
+        else fwd_of<kNoCap, false>(a, s);
     }
     return hipGetLastError();
 }
@@ -1259,12 +1299,15 @@ hipError_t launch_docs_attention_bwd(const DocsAttentionBwdProblem& p, hipStream
     a.parts = dkv_parts(p.tokens, p.kv_heads, p.group, part_tiles(p.tokens, p.docs.n_docs),
                         &a.part_heads);
     a.inv_sqrt_d = 1.0f / sqrtf((float)D);
-    if (p.docs.cap > 0.f) {
-        if (p.docs.slopes) bwd_of<true, true>(a, s);
-        else bwd_of<true, false>(a, s);
+    if (p.docs.cap > kSmallCap) {
+        if (p.docs.slopes) bwd_of<kLarge, true>(a, s);
+        else bwd_of<kLarge, false>(a, s);
+    } else if (p.docs.cap > 0.f) {
+        if (p.docs.slopes) bwd_of<kSmall, true>(a, s);
+        else bwd_of<kSmall, false>(a, s);
     } else {
-        if (p.docs.slopes) bwd_of<false, true>(a, s);
-        else bwd_of<false, false>(a, s);
+        if (p.docs.slopes) bwd_of<kNoCap, true>(a, s);
+        else bwd_of<kNoCap, false>(a, s);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.parts < 2) return e;
