@@ -208,10 +208,12 @@ struct Score {
         if constexpr (kFormed) return __builtin_fmaf(-slope, __builtin_fabsf(dist), x);
         return x;
     }
-    // base-2 score of a row's largest raw (or formed) value; -inf stays
+    // Base-2 score of a row's largest raw (or formed) value.  -inf stays but under a cap alone,
+    // where it may be a seen product's, with a score of -cap; of a row that sees nothing
+    // (whose weights are masked one by one) -cap is a reference below all scores to come.
     __device__ __forceinline__ float top(float mx) const {
         if constexpr (kFormed) return mx;
-        if constexpr (CAP) return mx == -INFINITY ? mx : capped(mx);
+        if constexpr (CAP) return capped(mx);
         return mx * scale;
     }
     // 2^(score - m) of a raw (or formed) value
@@ -502,8 +504,8 @@ void docs_fwd_kernel(FwdArgs a) {
                 rs = weights(b1, mrun[r] == -INFINITY ? 0.f : mrun[r], true);
             } else {
                 // The first tile sets the reference.  Where a row sees nothing in it (from the
-                // back) or scores of -inf alone, m stays -inf, and the next sums are infinite
-                // or NaN.
+                // back) or, without a cap, scores of -inf alone, m stays -inf, and the next
+                // sums are infinite or NaN.
                 const bool first = !BACK && i == 0;
                 if (!first) rs = weights(b0, mrun[r], false);
                 const bool over = !(rs <= kMostSum);

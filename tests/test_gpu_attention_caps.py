@@ -67,3 +67,33 @@ def test_the_smallest_and_largest_caps():
     R.check(out[:70, :D], mean, 2 * R.H * (size + mean.abs()), "means")
     with pytest.raises(atp.AtpError, match="cap"):
         Run([70], 1, 1, cap=2.0 ** 101).forward()
+
+
+@pytest.mark.parametrize("kv,n", [(2, 300), (16, 4096)])
+@pytest.mark.parametrize("cap", [2.0, 50.0, 1000.0])
+def test_seen_products_of_minus_infinity_score_minus_the_cap(kv, n, cap):
+    """Under a cap alone a product of -inf is a score of -cap, in the first tiles of a row,
+    among others and where a row sees nothing else; masked ones still weigh nothing."""
+    run = Run([n], kv, 1, cap=cap)
+    got = []
+    for low in (-float("inf"), -1e30):
+        qkv = run.qkv.clone()
+        heads = qkv.view(n, kv, 3, D)
+        heads[:, :, 0, 0] = heads[:, :, 0, 0].abs() + 0.5
+        for at in (slice(0, 130), slice(135, 141), slice(190, 191)):
+            heads[at, :, 1, 0] = low
+        out, lse = run.forward(qkv)
+        got.append((out[:n, :run.heads * D], lse))
+    (out, lse), (out0, lse0) = got
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    assert torch.equal(out.view(torch.int16), out0.view(torch.int16))
+    assert torch.equal(lse, lse0)
+    # rows that see such scores alone: their values' mean
+    rows = torch.arange(1, 131, device=out.device).double()
+    want = torch.log(rows) - cap
+    assert ((lse[:, :130] - want).abs() <= 6 * R.U * cap + 3 * R.EXP + 160 * R.U).all()
+    v = R.f64(run.qkv[:130]).view(130, kv, 3, D)[:, :, 2]
+    mean = v.cumsum(0) / rows[:, None, None]
+    size = v.abs().cumsum(0) / rows[:, None, None]
+    bound = size * (6 * R.U * cap + 2 * R.EXP + 2 * R.H + 160 * R.U) + R.H * mean.abs()
+    R.check(out[:130].reshape(130, kv, D), mean, bound, "means")
