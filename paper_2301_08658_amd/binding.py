@@ -1305,9 +1305,13 @@ class grad_list:
             self.device = s.device.index
         # a result must not land in another gradient or result
         spans.sort()
-        for (_, e0, i, a), (b1, _, j, b) in zip(spans, spans[1:]):
-            if b1 < e0 and i != j and "dst" in (a, b):
-                raise ValueError(f"{a}[{i}] and {b}[{j}] overlap")
+        reach = []                       # what ends behind the next one's begin
+        for span in spans:
+            reach = [r for r in reach if r[1] > span[0]]
+            for _, _, i, a in reach:
+                if i != span[2] and "dst" in (a, span[3]):
+                    raise ValueError(f"{a}[{i}] and {span[3]}[{span[2]}] overlap")
+            reach.append(span)
 
     @staticmethod
     def _matrix(t: torch.Tensor, name: str):
