@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence
 
 import torch
 
@@ -1268,6 +1268,34 @@ def atp_attention_docs_bwd(tokens: int, kv_heads: int, group: int, docs: attenti
         _stream(stream, dev)))
 
 
+class _Place(NamedTuple):
+    """Memory of rows `pitch` bytes apart; side and i: whose it is."""
+    begin: int
+    rows: int
+    pitch: int
+    width: int
+    i: int
+    side: str
+
+    @property
+    def end(self) -> int:
+        return self.begin + (self.rows - 1) * self.pitch + self.width
+
+    def meets(self, other: "_Place") -> bool:
+        """Whether a byte belongs to both (columns of one matrix interleave without)."""
+        if self.rows > 1 and other.rows > 1 and self.pitch != other.pitch:
+            a, b = (self, other) if self.rows <= other.rows else (other, self)
+            return any(a._replace(begin=a.begin + k * a.pitch, rows=1).meets(b)
+                       for k in range(a.rows))
+        # row k + j of this one meets row j of the other where k pitch is inside the rows'
+        # widths of their distance
+        pitch = self.pitch if self.rows > 1 else other.pitch
+        far = other.begin - self.begin
+        least = max((far - self.width) // pitch + 1, 1 - other.rows)
+        most = min(-((-far - other.width) // pitch) - 1, self.rows - 1)
+        return least <= most
+
+
 class grad_list:
     """Gradients and where their clipped values go (an array of atp_grad; keeps the
     tensors alive).  src: float32 or bf16 tensors, contiguous or 2-D with gaps between
@@ -1299,18 +1327,18 @@ class grad_list:
                 setattr(g, "ld_" + side, t.stride(0) if gaps else cols)
                 setattr(g, side + "_dtype", _float_code(t, f"{side}[{i}]"))
                 if t.numel():
-                    end = (rows - 1) * getattr(g, "ld_" + side) + cols
-                    spans.append((t.data_ptr(), t.data_ptr() + end * t.element_size(), i, side))
+                    pitch = getattr(g, "ld_" + side) * t.element_size()
+                    spans.append(_Place(t.data_ptr(), rows, pitch, cols * t.element_size(), i, side))
             g.rows, g.cols = rows, cols
             self.device = s.device.index
         # a result must not land in another gradient or result
         spans.sort()
         reach = []                       # what ends behind the next one's begin
         for span in spans:
-            reach = [r for r in reach if r[1] > span[0]]
-            for _, _, i, a in reach:
-                if i != span[2] and "dst" in (a, span[3]):
-                    raise ValueError(f"{a}[{i}] and {span[3]}[{span[2]}] overlap")
+            reach = [r for r in reach if r.end > span.begin]
+            for r in reach:
+                if r.i != span.i and "dst" in (r.side, span.side) and r.meets(span):
+                    raise ValueError(f"{r.side}[{r.i}] and {span.side}[{span.i}] overlap")
             reach.append(span)
 
     @staticmethod

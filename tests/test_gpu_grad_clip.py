@@ -183,3 +183,13 @@ def test_more_than_the_caches_hold(st, dt):
         before = [s.clone() for s in src]
         check_clip(src, None, before, 0.5, 1.0)
         assert all(torch.equal(w[:, c:], k) for w, k, (_, c) in zip(wide, gaps, shapes))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+def test_columns_of_one_matrix_in_place(dtype):
+    # a fused matrix' gradient, listed by its columns
+    m = rand((37, 192), 21, dtype)
+    before = m.clone()
+    cut = [(0, 64), (64, 72), (72, 168)]
+    check_clip([m[:, a:b] for a, b in cut], None, [before[:, a:b] for a, b in cut], 1.0, 2.0)
+    assert torch.equal(m[:, 168:], before[:, 168:])

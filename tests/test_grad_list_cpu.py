@@ -53,3 +53,50 @@ def test_against_every_pair_of_values():
         meet = any(i != j and values(dst[i]) & (values(src[j]) | values(dst[j]))
                    for i in range(n) for j in range(n))
         assert refused(src, dst) == meet
+
+
+def test_columns_of_one_matrix():
+    m = torch.zeros(8, 128)
+    assert not refused([m[:, :64], m[:, 64:]])            # in place, side by side
+    assert not refused([m[:, :32], m[:, 40:72], m[:, 72:]])
+    assert not refused([torch.zeros(8, 64), torch.zeros(8, 64)], [m[:, :64], m[:, 64:]])
+    assert not refused([m[:, 64:], torch.zeros(8, 64)], [torch.zeros(8, 64), m[:, :64]])
+    assert refused([m[:, :72], m[:, 64:]]) and refused([m[:, :64], m[:, 56:]])
+    assert not refused([m[:4, :72], m[4:, 64:]])
+    # a run between two rows, and one that reaches into the next
+    flat = m.view(-1)
+    assert not refused([m[:, :64], flat[64:128]]) and refused([m[:, :64], flat[64:129]])
+    assert not refused([m[:, 64:], flat[:64]]) and refused([m[:, 64:], flat[60:200]])
+    # rows of another length over the same memory
+    w = flat.view(4, 256)
+    assert not refused([m[:, :64], w[:, 64:128]]) and not refused([m[:, :64], w[:, 192:]])
+    assert refused([m[:, :64], w[:, 64:136]]) and refused([m[:, :64], w[:, 100:200]])
+    # types of other sizes
+    half = m.view(torch.bfloat16)                         # rows of 256
+    assert not refused([m[:, :64], half[:, 128:]]) and refused([m[:, :64], half[:, 120:]])
+
+
+def test_rows_against_every_pair_of_values():
+    rng = random.Random(8)
+    store = torch.zeros(600)
+
+    def view():
+        if rng.random() < 0.3:
+            n = rng.randrange(1, 40)
+            return store[(a := rng.randrange(0, 601 - n)):a + n]
+        ld = rng.choice((16, 16, 16, 24, 40))
+        rows, cols = rng.randrange(1, 600 // ld), rng.randrange(1, ld)
+        return store.as_strided((rows, cols), (ld, 1), rng.randrange(0, 600 - rows * ld))
+
+    def values(t):
+        if t.dim() == 1:
+            return set(range(t.storage_offset(), t.storage_offset() + t.numel()))
+        return {t.storage_offset() + r * t.stride(0) + c for r in range(t.size(0))
+                for c in range(t.size(1))}
+    seen = set()
+    for _ in range(2000):
+        a, b = view(), view()
+        meet = bool(values(a) & values(b))
+        assert refused([a, b]) == meet, (a.shape, a.stride(), b.shape, b.stride())
+        seen.add(meet)
+    assert seen == {True, False}
