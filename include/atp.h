@@ -939,7 +939,8 @@ atp_status atp_attention_docs_bwd(int64_t tokens, int32_t kv_heads, int32_t grou
                                   const void* out, int64_t ld_out, const float* lse,
                                   const void* d_out, int64_t ld_dout, void* d_qkv, int64_t ld_dqkv,
                                   void* workspace, size_t ws_bytes, void* stream);
-/* 0 for sizes that the call refuses (and for 0 tokens). */
+/* 0 for sizes that the call refuses (and for 0 tokens); what is enough for a number of
+ * tokens is enough for fewer. */
 size_t atp_attention_docs_workspace_bytes(int64_t tokens, int32_t kv_heads, int32_t group);
 
 /* One gradient: src [rows, cols], fp32 or bf16 (ld_src elements between rows; for one

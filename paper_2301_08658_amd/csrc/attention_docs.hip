@@ -1260,12 +1260,18 @@ void bwd_of(BwdArgs& a, hipStream_t s) {
 
 }  // namespace
 
+// Enough for any number of documents (fewer tiles never give more parts) and for every
+// smaller number of rows: the sums of more divisions of fewer rows may be the larger ones, so
+// each number of divisions counts with the most rows that take it.
 int64_t docs_attention_ws_floats(int64_t tokens, int kv_heads, int group) {
-    int heads;
-    // for any number of documents: fewer tiles never give more parts
-    const int parts = dkv_parts(tokens, kv_heads, group, kPartTiles, &heads);
-    return delta_floats(tokens, kv_heads * group) +
-           (parts > 1 ? (int64_t)parts * tokens * kv_heads * 2 * D : 0);
+    int64_t sums = 0;
+    for (int want = 2; want <= group; ++want) {
+        const int most = (int)(kPartTiles - 1) / (want - 1) / kv_heads;   // tiles of 64 rows
+        if (most < 1) break;
+        const int heads = (group + want - 1) / want, parts = (group + heads - 1) / heads;
+        sums = std::max(sums, parts * std::min<int64_t>(tokens, (int64_t)BM * most + BM - 1));
+    }
+    return delta_floats(tokens, kv_heads * group) + sums * kv_heads * 2 * D;
 }
 
 hipError_t launch_docs_attention(const DocsAttentionProblem& p, hipStream_t s) {

@@ -236,3 +236,29 @@ def test_binding_checks_sizes_and_devices():
         atp.attention_docs(torch.zeros(0, dtype=torch.int32))
     with pytest.raises(ValueError, match="GPU"):
         atp.grad_list([torch.zeros(8)])
+
+
+def _docs_need(t, kv, group, most):
+    """Bytes of a backward of t rows whose heads are divided for `most` tiles."""
+    want = min(group, -(-most // (max(1, t // 64) * kv)))
+    heads = -(-group // want)
+    parts = -(-group // heads)
+    return 4 * (-(-t * kv * group // 64) * 64 + (parts * t * kv * 256 if parts > 1 else 0))
+
+
+@pytest.mark.parametrize("kv,group", [(2, 8), (1, 64), (4, 3), (1, 12), (20, 1), (3, 7), (700, 2)])
+def test_attention_workspace_of_the_largest_batch(kv, group):
+    # what is enough for a batch is enough for every smaller one, however it is divided
+    sizes, t = [], 1
+    while t < 1 << 18:
+        sizes.append((t, atp.atp_attention_docs_workspace_bytes(t, kv, group)))
+        t += 1 if t < 130 else 63 + t // 50
+    for (_, a), (_, b) in zip(sizes, sizes[1:]):
+        assert a <= b
+    largest = 0
+    for t, have in sizes:
+        largest = max(largest, _docs_need(t, kv, group, 1024))
+        assert have >= largest
+    # not more than the largest of them and the last one's row values
+    assert sizes[-1][1] <= max(_docs_need(t, kv, group, 1024) for t in range(1, 70000, 7)) * 1.02 \
+        + _docs_need(sizes[-1][0], kv, group, 1)
