@@ -828,7 +828,8 @@ atp_status atp_embedding_bwd(int64_t tokens, const int32_t* ids, int64_t vocab_l
                              int64_t vocab_off, int64_t cols, const void* dy, int64_t ld_dy,
                              float scale, float* dtable, int64_t ld_dtable, int32_t accumulate,
                              void* workspace, size_t ws_bytes, void* stream);
-/* 0 for sizes that the call refuses (and for 0 tokens). */
+/* 0 for sizes that the call refuses (and for 0 tokens); what is enough for a number of
+ * tokens is enough for fewer. */
 size_t atp_embedding_workspace_bytes(int64_t tokens, int64_t vocab_loc, int64_t cols);
 
 /* Layer norm of rows: y = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) o weight

@@ -442,18 +442,38 @@ struct Plan {
 };
 int bit_length(uint64_t v) { return v ? 64 - __builtin_clzll(v) : 0; }
 
+// Tokens of a chunk.  Short chunks fill the chip, long ones leave fewer runs that cross an
+// end.  Gradients with chunks of 8, 16, 32 and 64 tokens, us: 1024 x 2048 values 20, 24, 32,
+// 50; 4096 x 4096 33, 32, 37, 54; 4096 x 20480 172, 174, 164, 185; 65536 x 2048 242, 184, 183,
+// 168.  No more than kMostChunks, which one run may cross.
+constexpr int kMostChunks = 2048;
+struct ChunkRule {
+    int64_t values;                      // of gradients of fewer values than this
+    int chunk;
+};
+constexpr ChunkRule kChunks[] = {{1 << 22, 8}, {1 << 25, 16}, {1 << 27, 32}, {INT64_MAX, 64}};
+int64_t chunk_of(int64_t values) {
+    for (const ChunkRule& r : kChunks)
+        if (values < r.values) return r.chunk;
+    return 0;
+}
+// Rows of partial sums that any gradient of up to n tokens leaves: longer chunks leave fewer,
+// so each rule counts with its most tokens.
+int64_t most_chunks(int64_t n, int64_t cols) {
+    int64_t most = 0;
+    for (const ChunkRule& r : kChunks) {
+        const int64_t k = std::min(n, (r.values - 1) / cols);
+        most = std::max(most, std::min<int64_t>(kMostChunks, (k + r.chunk - 1) / r.chunk));
+    }
+    return most;
+}
+
 Plan plan_of(int64_t n, int64_t vocab, int64_t cols) {
     Plan p = {};
     p.key_bits = bit_length((uint64_t)vocab);
     p.few = n <= kCountMax;
     p.tiles = (int)((n + kTile - 1) / kTile);
-    // Short chunks fill the chip, long ones leave fewer runs that cross an end.  Gradients
-    // with chunks of 8, 16, 32 and 64 tokens, us: 1024 x 2048 values 20, 24, 32, 50; 4096 x
-    // 4096 33, 32, 37, 54; 4096 x 20480 172, 174, 164, 185; 65536 x 2048 242, 184, 183, 168.
-    // No more than 2048 chunks, which one run may cross.
-    const int64_t values = n * cols;
-    const int64_t chunk = values < 1 << 22 ? 8 : values < 1 << 25 ? 16 : values < 1 << 27 ? 32 : 64;
-    p.chunk = (int)std::max(chunk, ((n + 2047) / 2048 + 7) / 8 * 8);
+    p.chunk = (int)std::max(chunk_of(n * cols), ((n + kMostChunks - 1) / kMostChunks + 7) / 8 * 8);
     p.chunks = (int)((n + p.chunk - 1) / p.chunk);
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
@@ -468,7 +488,7 @@ Plan plan_of(int64_t n, int64_t vocab, int64_t cols) {
         p.order2 = take(4 * n);
         p.hist = take(4 * (int64_t)kDigits * p.tiles);
     }
-    p.part = take((int64_t)p.chunks * 2 * cols * 4);
+    p.part = take(most_chunks(n, cols) * 2 * cols * 4);
     p.bytes = at;
     return p;
 }

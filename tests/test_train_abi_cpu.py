@@ -262,3 +262,29 @@ def test_attention_workspace_of_the_largest_batch(kv, group):
     # not more than the largest of them and the last one's row values
     assert sizes[-1][1] <= max(_docs_need(t, kv, group, 1024) for t in range(1, 70000, 7)) * 1.02 \
         + _docs_need(sizes[-1][0], kv, group, 1)
+
+
+@pytest.mark.parametrize("cols", [8, 64, 520, 2048, 4096, 20480, 1 << 20])
+def test_embedding_workspace_of_the_largest_batch(cols):
+    # lists of sorted tokens, and two rows of sums for each chunk of tokens
+    def need(t):
+        values = t * cols
+        chunk = 8 if values < 1 << 22 else 16 if values < 1 << 25 else 32 if values < 1 << 27 else 64
+        chunk = max(chunk, -(-(-(-t // 2048)) // 8) * 8)
+        lists = 8 * t if t <= 16384 else 16 * t + 1024 * -(-t // 8192)
+        return lists + -(-t // chunk) * 2 * cols * 4
+    sizes, t = [], 1
+    while t <= 1 << 24:
+        sizes.append((t, atp.atp_embedding_workspace_bytes(t, 50000, cols)))
+        t += 1 if t < 40 else 7 + t // 90
+    for edge in (1 << 22, 1 << 25, 1 << 27):               # where the chunks change
+        t = edge // cols
+        sizes += [(k, atp.atp_embedding_workspace_bytes(k, 50000, cols))
+                  for k in (t - 1, t, t + 1) if 1 <= k <= 1 << 24]
+    sizes.sort()
+    largest = 0
+    for (_, a), (t, b) in zip([(0, 0)] + sizes, sizes):
+        largest = max(largest, need(t))
+        assert a <= b and largest <= b
+    # a row of sums above the largest batch's, and the lists' alignment
+    assert sizes[-1][1] <= largest + 8 * sizes[-1][0] + 8 * cols * 64
