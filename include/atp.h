@@ -892,7 +892,8 @@ atp_status atp_layer_norm_bwd_sums(int64_t tokens, int64_t cols, int32_t dtype,
                                    const atp_layer_norm* norm, const void* x, int64_t ldx,
                                    const float* mean, const float* rstd, const void* dy,
                                    int64_t ld_dy, float* sums, void* stream);
-/* 0 for sizes that the call refuses (and for 0 tokens). */
+/* 0 for sizes that the call refuses (and for 0 tokens); what is enough for a number of
+ * tokens is enough for fewer. */
 size_t atp_layer_norm_workspace_bytes(int64_t tokens, int64_t cols);
 
 /* Documents of packed rows.  Rows [cu_docs[d], cu_docs[d + 1]) are document d (int32

@@ -553,13 +553,19 @@ __global__ __launch_bounds__(kSumThreads) void column_sum_kernel(const float* pa
 // Workgroups of the backward: enough to fill the chip, each with four rows at least (eight
 // where its waves hold one each), since it leaves a row of partial sums, 8 bytes a
 // column against the 8 to 14 of a row, and all with the same number of visits.
-int64_t bwd_groups(int64_t tokens, int64_t cols) {
+struct Groups {
+    int64_t rows, most, visits;          // rows at a time, workgroups at most, visits at least
+};
+Groups groups_of(int64_t cols) {
     const Shape sh = shape_of(cols);
-    const int64_t rows = sh.one ? kRowsPerGroup : 1;
-    const int64_t most = 256 * (sh.one ? 4 : std::max(1, 1024 / sh.threads));
+    return Groups{sh.one ? kRowsPerGroup : 1,
+                  256 * (sh.one ? 4 : std::max(1, 1024 / sh.threads)), sh.one ? 2 : 4};
+}
+int64_t bwd_groups(int64_t tokens, int64_t cols) {
+    const Groups g = groups_of(cols);
     const int64_t visits =
-        std::max<int64_t>((tokens + most * rows - 1) / (most * rows), sh.one ? 2 : 4);
-    return (tokens + visits * rows - 1) / (visits * rows);
+        std::max((tokens + g.most * g.rows - 1) / (g.most * g.rows), g.visits);
+    return (tokens + visits * g.rows - 1) / (visits * g.rows);
 }
 
 template <class T, int NV, bool ONE>
@@ -616,8 +622,11 @@ void bwd_of(const Shape& sh, const BwdArgs& a, int64_t grid, hipStream_t s) {
 
 }  // namespace
 
+// Enough for every smaller number of tokens too: one visit more for all leaves fewer
+// workgroups, so what counts is the most that there are with the fewest visits.
 int64_t layer_norm_ws_floats(int64_t tokens, int64_t cols) {
-    return bwd_groups(tokens, cols) * 2 * cols;
+    const Groups g = groups_of(cols);
+    return std::min(g.most, (tokens + g.visits * g.rows - 1) / (g.visits * g.rows)) * 2 * cols;
 }
 
 hipError_t launch_layer_norm(const LayerNormProblem& p, hipStream_t s) {

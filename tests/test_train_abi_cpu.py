@@ -288,3 +288,24 @@ def test_embedding_workspace_of_the_largest_batch(cols):
         assert a <= b and largest <= b
     # a row of sums above the largest batch's, and the lists' alignment
     assert sizes[-1][1] <= largest + 8 * sizes[-1][0] + 8 * cols * 64
+
+
+@pytest.mark.parametrize("cols", [8, 512, 1024, 2048, 2056, 5120, 10240, 20480, 32768])
+def test_layer_norm_workspace_of_the_largest_batch(cols):
+    # two rows of sums for each workgroup
+    vecs = cols // 8
+    one = vecs <= 256
+    nv = 2 if vecs <= 1280 else 4
+    most = 1024 if one else 256 * max(1, 1024 // (64 * -(-vecs // (64 * nv))))
+    rows = 4 if one else 1
+
+    def need(t):
+        visits = max(-(-t // (most * rows)), 2 if one else 4)
+        return -(-t // (visits * rows)) * 2 * cols * 4
+    largest, last, t = 0, 0, 1
+    while t <= 1 << 24:
+        have = atp.atp_layer_norm_workspace_bytes(t, cols)
+        largest = max(largest, need(t))
+        assert last <= have and largest <= have
+        last, t = have, t + (1 if t < 30000 else t // 90)
+    assert last == largest
