@@ -296,8 +296,8 @@ atp_status atp_embedding_fwd(int64_t tokens, const int32_t* ids, int64_t vocab_l
 }
 
 size_t atp_embedding_workspace_bytes(int64_t tokens, int64_t vocab_loc, int64_t cols) {
-    if (tokens < 0 || tokens > kMaxTokens || vocab_loc < 1 || vocab_loc > kMaxVocab || cols < 1 ||
-        cols > kMaxLd)
+    if (tokens < 0 || tokens > kMaxTokens || vocab_loc < 1 || vocab_loc > kMaxVocab || cols < 8 ||
+        cols % 8 != 0 || cols > kMaxLd)
         return 0;
     return (size_t)atp::embedding_ws_bytes(tokens, vocab_loc, cols);
 }

@@ -309,3 +309,9 @@ def test_layer_norm_workspace_of_the_largest_batch(cols):
         assert last <= have and largest <= have
         last, t = have, t + (1 if t < 30000 else t // 90)
     assert last == largest
+
+
+def test_workspaces_of_refused_columns():
+    for cols in (1, 4, 12, 1 << 22 | 8):
+        assert emb_bwd(c=cols, ldy=1 << 22, ldw=1 << 22) == UNS
+        assert atp.atp_embedding_workspace_bytes(5, 100, cols) == 0
