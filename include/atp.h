@@ -923,7 +923,8 @@ typedef struct {
  * row does not see hold does not reach its result.
  * Errors: INVALID_ARGUMENT for negative sizes, kv_heads or group < 1, NULL buffers,
  * a negative or non-finite cap, overlap; UNSUPPORTED for more than 2^24 tokens, the
- * limits above, a cap above 2^100, 2^31 tiles of 64 rows and heads, misalignment. */
+ * limits above, a cap above 2^100, 2^24 tiles of 64 rows of all documents (empty ones count
+ * one) and heads, misalignment. */
 atp_status atp_attention_docs_fwd(int64_t tokens, int32_t kv_heads, int32_t group,
                                   const atp_attention_docs* docs, const void* qkv, int64_t ld_qkv,
                                   void* out, int64_t ld_out, float* lse, void* stream);

@@ -1227,19 +1227,26 @@ void fwd(FwdArgs& a, hipStream_t s) {
         <<<dim3((unsigned)((int64_t)a.slots * a.kv_heads * a.group)), KG > 1 ? 3 * NTHR : NTHR, 0,
            s>>>(a);
 }
+// Whether the kernels that split their loops, of `threads` threads, can be launched: empty
+// documents have slots too.
+bool split_fits(const Common& a, int64_t heads, int threads) {
+    return fits_launch(slots_of(a.tokens, 64, a.n_docs) * heads, threads);
+}
 template <Cap CAP, bool BIAS>
 void fwd_of(FwdArgs& a, hipStream_t s) {
     const int64_t tiles = (a.tokens + 127) / 128 * a.kv_heads * a.group;
-    if (2 * tiles >= full_tiles(a.tokens, a.n_docs)) fwd<2, 1, CAP, BIAS>(a, s);
+    if (2 * tiles >= full_tiles(a.tokens, a.n_docs) ||
+        !split_fits(a, a.kv_heads * a.group, 3 * NTHR))
+        fwd<2, 1, CAP, BIAS>(a, s);
     else fwd<1, 2, CAP, BIAS>(a, s);
 }
 
 template <Cap CAP, bool BIAS>
-void bwd_of(BwdArgs& a, hipStream_t s) {
+hipError_t bwd_of(BwdArgs& a, hipStream_t s) {
     const int heads = a.kv_heads * a.group;
     const int64_t s64 = slots_of(a.tokens, 64, a.n_docs);
     const int64_t full = full_tiles(a.tokens, a.n_docs);
-    const bool split = (a.tokens + 63) / 64 * heads < full;
+    const bool split = (a.tokens + 63) / 64 * heads < full && split_fits(a, heads, 3 * NTHR);
     if (split) {
         a.slots = (int)s64;
         docs_dq_kernel<1, 2, CAP, BIAS>
@@ -1249,13 +1256,16 @@ void bwd_of(BwdArgs& a, hipStream_t s) {
         docs_dq_kernel<2, 1, CAP, BIAS>
             <<<dim3((unsigned)((int64_t)a.slots * heads)), NTHR, 0, s>>>(a);
     }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     const int per_slot = a.kv_heads * a.parts;
     a.slots = (int)s64;
-    if ((a.tokens + 63) / 64 * per_slot < full) {
+    if ((a.tokens + 63) / 64 * per_slot < full && split_fits(a, per_slot, 2 * NTHR)) {
         docs_dkv_kernel<2, CAP, BIAS><<<dim3((unsigned)(s64 * per_slot)), 2 * NTHR, 0, s>>>(a);
     } else {
         docs_dkv_kernel<1, CAP, BIAS><<<dim3((unsigned)(s64 * per_slot)), NTHR, 0, s>>>(a);
     }
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -1307,17 +1317,17 @@ hipError_t launch_docs_attention_bwd(const DocsAttentionBwdProblem& p, hipStream
     a.parts = dkv_parts(p.tokens, p.kv_heads, p.group, part_tiles(p.tokens, p.docs.n_docs),
                         &a.part_heads);
     a.inv_sqrt_d = 1.0f / sqrtf((float)D);
+    hipError_t e;
     if (p.docs.cap > kSmallCap) {
-        if (p.docs.slopes) bwd_of<kLarge, true>(a, s);
-        else bwd_of<kLarge, false>(a, s);
+        if (p.docs.slopes) e = bwd_of<kLarge, true>(a, s);
+        else e = bwd_of<kLarge, false>(a, s);
     } else if (p.docs.cap > 0.f) {
-        if (p.docs.slopes) bwd_of<kSmall, true>(a, s);
-        else bwd_of<kSmall, false>(a, s);
+        if (p.docs.slopes) e = bwd_of<kSmall, true>(a, s);
+        else e = bwd_of<kSmall, false>(a, s);
     } else {
-        if (p.docs.slopes) bwd_of<kNoCap, true>(a, s);
-        else bwd_of<kNoCap, false>(a, s);
+        if (p.docs.slopes) e = bwd_of<kNoCap, true>(a, s);
+        else e = bwd_of<kNoCap, false>(a, s);
     }
-    hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.parts < 2) return e;
     docs_join_kernel<<<dim3((unsigned)((p.tokens * p.kv_heads + 7) / 8)), 256, 0, s>>>(a);
     return hipGetLastError();

@@ -19,7 +19,6 @@ using atp::set_error;
 
 constexpr int64_t kMaxVocab = 1 << 24;
 constexpr int32_t kMaxDocs = 1 << 16;
-constexpr int64_t kMaxGrid = 0x7fffffff;
 constexpr float kMaxCap = 0x1p100f;         // its reciprocal and base-2 score stay normal numbers
 
 atp_status overlap(const char* a, const char* b) {
@@ -251,9 +250,10 @@ atp_status check_docs(const atp_attention_docs* d, int64_t tokens, int32_t kv_he
     if (!(d->cap >= 0.f) || isinf(d->cap))
         return set_error(ATP_ERR_INVALID_ARGUMENT, "cap must be finite and not negative");
     if (d->cap > kMaxCap) return set_error(ATP_ERR_UNSUPPORTED, "cap %g: at most 2^100", d->cap);
-    if ((tokens / 64 + d->n_docs) * kv_heads * group > kMaxGrid)
-        return set_error(ATP_ERR_UNSUPPORTED, "%lld tokens of %d documents and %lld heads: above "
-                         "2^31 tiles", (long long)tokens, d->n_docs, (long long)kv_heads * group);
+    if (!atp::fits_launch((tokens / 64 + d->n_docs) * kv_heads * group, 256))
+        return set_error(ATP_ERR_UNSUPPORTED, "%lld tokens of %d documents and %lld heads: 2^24 "
+                         "tiles or more", (long long)tokens, d->n_docs,
+                         (long long)kv_heads * group);
     if (d->n_docs == 0) return ATP_OK;
     ATP_CHECK(check_vector(d->cu_docs, "cu_docs"));
     ATP_CHECK(check_optional(d->prefix, "prefix"));

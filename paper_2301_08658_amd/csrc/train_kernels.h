@@ -10,6 +10,12 @@
 
 namespace atp {
 
+// Threads of a launch are fewer than 2^32 (a limit of HIP).
+constexpr int64_t kLaunchThreads = (int64_t)1 << 32;
+inline bool fits_launch(int64_t groups, int64_t threads) {
+    return groups < kLaunchThreads / threads;
+}
+
 struct EmbeddingProblem {
     const int32_t* ids;
     int64_t tokens, vocab, off, cols;    // rows of this device's table, its first token

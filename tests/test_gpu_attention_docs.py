@@ -287,3 +287,10 @@ def test_many_short_documents(kv, group, kw):
     lens = [1 + 37 * d % 250 for d in range(30)]
     prefix = [0 if d % 3 else n // 2 for d, n in enumerate(lens)] if kw.get("slopes") else None
     Run(lens, kv, group, prefix=prefix, first=2, behind=61, seed=kv, **kw).check()
+
+
+@pytest.mark.parametrize("kv,cap", [(86, 0.0), (86, 20.0), (255, 0.0)])
+def test_lists_padded_to_the_most_documents(kv, cap):
+    # 65536 documents, nearly all empty: more tiles than the kernels of 768 threads can have
+    lens = [60] + [0] * 40000 + [1, 0, 67] + [0] * 25532
+    Run(lens, kv, 1, cap=cap, seed=4).check()

@@ -315,3 +315,10 @@ def test_workspaces_of_refused_columns():
     for cols in (1, 4, 12, 1 << 22 | 8):
         assert emb_bwd(c=cols, ldy=1 << 22, ldw=1 << 22) == UNS
         assert atp.atp_embedding_workspace_bytes(5, 100, cols) == 0
+
+
+@pytest.mark.parametrize("call", [att, att_bwd])
+def test_attention_tiles_of_one_launch(call):
+    # 65538 tiles of 256 heads, in workgroups of 256 threads: a launch of 2^32
+    wide = dict(t=128, kv=256, ldx=256 * 384, ldo=256 * 128, d=docs(n=65536))
+    assert call(**wide) == UNS and "tiles" in B.last_error()
