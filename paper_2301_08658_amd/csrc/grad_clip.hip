@@ -29,6 +29,8 @@ constexpr int kThreads = 256;
 // of 16384 990).
 constexpr int kSumValues = 16384, kClipValues = 4096;
 constexpr int64_t kMaxRun = 1 << 30;                 // values of a run; longer ones are cut
+constexpr int64_t kMaxRowBlocks = 1 << 23;           // workgroups of rows with gaps, likewise
+static_assert(kMaxRun / kClipValues <= kMaxRowBlocks && kClipValues <= kSumValues, "pieces");
 // Gradients of more bytes go past the caches, which hold no value from the sum to the
 // clipping then.  Sum and clipping into other memory, cached and past the caches: of
 // 128 MiB 65 and 71 us, of 256 MiB 154 and 134, of 1 GiB 572 and 526.
@@ -286,10 +288,17 @@ bool is_run(const GradView& g, bool with_dst) {
 int64_t row_blocks(int64_t rows, int64_t cols, int group) {
     return (rows * ((cols + 7) / 8) + group / 8 - 1) / (group / 8);
 }
+// Rows with gaps that one entry takes.
+int64_t piece_rows(int64_t cols, int group) { return kMaxRowBlocks * (group / 8) / ((cols + 7) / 8); }
 int64_t blocks_of(const GradView& g) {
     if (g.rows == 0 || g.cols == 0) return 0;
-    if (!is_run(g, false)) return row_blocks(g.rows, g.cols, kSumValues);
     int64_t blocks = 0;
+    if (!is_run(g, false)) {
+        const int64_t most = piece_rows(g.cols, kSumValues);
+        for (int64_t left = g.rows; left > 0; left -= most)
+            blocks += row_blocks(std::min(left, most), g.cols, kSumValues);
+        return blocks;
+    }
     for (int64_t left = g.rows * g.cols; left > 0; left -= kMaxRun)
         blocks += row_blocks(1, std::min(left, kMaxRun), kSumValues);
     return blocks;
@@ -301,7 +310,8 @@ bool past_caches(int n, const GradView* g) {
     return bytes > kCachedBytes;
 }
 
-// Collects entries of one kind and calls f(list, workgroups) for every full one.
+// Collects entries of one kind and calls f(list, workgroups) for every full one; a launch has
+// fewer than 2^32 threads (HIP drops the rest of a larger one without an error).
 template <class L, class F>
 struct Launches {
     L list;
@@ -316,7 +326,7 @@ struct Launches {
     }
     // the next entry's place; b: its workgroups
     int next(int64_t b) {
-        if (list.n == L::kMost || blocks + b > 0x7fffffff) flush();
+        if (list.n == L::kMost || !fits_launch(blocks + b, kThreads)) flush();
         list.first[list.n] = (int32_t)blocks;
         blocks += b;
         return list.n++;
@@ -344,13 +354,20 @@ hipError_t in_launches(int n, const GradView* g, bool with_dst, F f) {
             }
             continue;
         }
-        const int t = rows.next(row_blocks(g[i].rows, g[i].cols, group));
-        rows.list.src[t] = src | (g[i].src_f32 ? 1 : 0);
-        rows.list.dst[t] = dst | (g[i].dst_f32 ? 1 : 0);
-        rows.list.cols[t] = g[i].cols;
-        rows.list.rows[t] = (int32_t)g[i].rows;
-        rows.list.ld_src[t] = (int32_t)g[i].ld_src;
-        rows.list.ld_dst[t] = (int32_t)g[i].ld_dst;
+        const int64_t most = piece_rows(g[i].cols, group);
+        for (int64_t at = 0; at < g[i].rows; at += most) {
+            const int64_t n_rows = std::min(g[i].rows - at, most);
+            const int t = rows.next(row_blocks(n_rows, g[i].cols, group));
+            rows.list.src[t] =
+                (src + at * g[i].ld_src * (g[i].src_f32 ? 4 : 2)) | (g[i].src_f32 ? 1 : 0);
+            if (with_dst)
+                rows.list.dst[t] =
+                    (dst + at * g[i].ld_dst * (g[i].dst_f32 ? 4 : 2)) | (g[i].dst_f32 ? 1 : 0);
+            rows.list.cols[t] = g[i].cols;
+            rows.list.rows[t] = (int32_t)n_rows;
+            rows.list.ld_src[t] = (int32_t)g[i].ld_src;
+            rows.list.ld_dst[t] = (int32_t)g[i].ld_dst;
+        }
     }
     runs.flush();
     if (runs.e != hipSuccess) return runs.e;

@@ -193,3 +193,22 @@ def test_columns_of_one_matrix_in_place(dtype):
     cut = [(0, 64), (64, 72), (72, 168)]
     check_clip([m[:, a:b] for a, b in cut], None, [before[:, a:b] for a, b in cut], 1.0, 2.0)
     assert torch.equal(m[:, 168:], before[:, 168:])
+
+
+def test_more_values_than_one_launch_takes():
+    # 2^36 values in place: 2^24 workgroups of 256 threads, more than HIP launches at once
+    torch.cuda.empty_cache()
+    n = (1 << 36) + 8
+    if torch.cuda.mem_get_info()[0] < 2 * n + (8 << 30):
+        pytest.skip("needs 136 GiB of device memory")
+    g = torch.zeros(n, dtype=BF, device=DEV)
+    at = torch.tensor([0, (1 << 30) - 1, 1 << 35, (1 << 36) - 1, 1 << 36, n - 1], device=DEV)
+    g[at] = 3.0
+    grads = atp.grad_list([g])
+    total, norm = total_of(grads), torch.empty(2, device=DEV)
+    assert float(total) == 54.0
+    atp.atp_grad_clip(grads, [total], norm, max_norm=1.0)
+    assert (g[at].cpu() == torch.tensor(3.0 / 54 ** 0.5).to(BF)).all()
+    assert abs(float(norm[0]) - 54 ** 0.5) <= 2 * R.U * 54 ** 0.5
+    del g, grads
+    torch.cuda.empty_cache()
