@@ -808,8 +808,8 @@ size_t atp_attention_cache_workspace_bytes(int32_t kv_heads, int32_t group, int3
  * bf16 [tokens, cols].
  * Errors: INVALID_ARGUMENT for negative sizes, vocab_loc or cols < 1, a negative
  * vocab_off, a non-finite scale, NULL buffers, out sharing memory with table;
- * UNSUPPORTED for more than 2^24 tokens or rows, cols not a multiple of 8,
- * misalignment. */
+ * UNSUPPORTED for more than 2^24 tokens or rows, 2^37 values of out, cols not a multiple
+ * of 8, misalignment. */
 atp_status atp_embedding_fwd(int64_t tokens, const int32_t* ids, int64_t vocab_loc,
                              int64_t vocab_off, int64_t cols, const void* table, int64_t ld_table,
                              float scale, void* out, int32_t out_dtype, int64_t ld_out,
@@ -856,8 +856,9 @@ typedef struct {
  * Errors: INVALID_ARGUMENT for negative sizes, cols < 1, a bad dtype, a negative or
  * non-finite eps, NULL buffers, add without x_out or with stats, buffers that
  * overlap otherwise than above, red_size < 1; UNSUPPORTED for more than 2^24
- * tokens or 32768 columns, cols not a multiple of 8, misalignment, red_size above
- * ATP_MAX_GROUP. */
+ * tokens or 32768 columns, 2^32 threads of 16 to 32 columns each in the two calls below
+ * (13.4 million rows of 4104 columns), cols not a multiple of 8, misalignment, red_size
+ * above ATP_MAX_GROUP. */
 atp_status atp_layer_norm_fwd(int64_t tokens, int64_t cols, int32_t dtype,
                               const atp_layer_norm* norm, const void* x, int64_t ldx,
                               const void* add, int64_t ld_add, void* x_out, int64_t ld_xout,

@@ -38,6 +38,10 @@ struct FwdArgs {
 
 constexpr int kFwdVecs = 4;              // vectors per thread
 
+int64_t fwd_groups(int64_t tokens, int64_t cols) {
+    return (tokens * (cols / 8) + 256 * kFwdVecs - 1) / (256 * kFwdVecs);
+}
+
 // A workgroup copies a run of kFwdVecs * 256 vectors of the output, rows in order.
 template <class T>
 __global__ __launch_bounds__(256) void embed_kernel(FwdArgs A) {
@@ -517,6 +521,10 @@ int64_t embedding_ws_bytes(int64_t tokens, int64_t vocab, int64_t cols) {
     return plan_of(tokens, vocab, cols).bytes;
 }
 
+bool embedding_fits(int64_t tokens, int64_t cols) {
+    return fits_launch(fwd_groups(tokens, cols), 256);
+}
+
 hipError_t launch_embedding(const EmbeddingProblem& p, hipStream_t s) {
     if (p.tokens == 0) return hipSuccess;
     FwdArgs a;
@@ -528,8 +536,7 @@ hipError_t launch_embedding(const EmbeddingProblem& p, hipStream_t s) {
     a.table = p.table; a.ldt = p.ldt;
     a.scale = p.scale;
     a.out = p.out; a.ldo = p.ldo;
-    const int64_t grid = (p.tokens * a.vecs + 256 * kFwdVecs - 1) / (256 * kFwdVecs);
-    if (grid > 0x7fffffff) return hipErrorInvalidValue;
+    const int64_t grid = fwd_groups(p.tokens, p.cols);
     if (p.out_f32) embed_kernel<float><<<dim3((unsigned)grid), 256, 0, s>>>(a);
     else embed_kernel<uint16_t><<<dim3((unsigned)grid), 256, 0, s>>>(a);
     return hipGetLastError();

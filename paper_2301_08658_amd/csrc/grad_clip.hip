@@ -310,8 +310,8 @@ bool past_caches(int n, const GradView* g) {
     return bytes > kCachedBytes;
 }
 
-// Collects entries of one kind and calls f(list, workgroups) for every full one; a launch has
-// fewer than 2^32 threads (HIP drops the rest of a larger one without an error).
+// Collects entries of one kind and calls f(list, workgroups) for every full one, or one that
+// fills a launch.
 template <class L, class F>
 struct Launches {
     L list;

@@ -629,6 +629,10 @@ int64_t layer_norm_ws_floats(int64_t tokens, int64_t cols) {
     return std::min(g.most, (tokens + g.visits * g.rows - 1) / (g.visits * g.rows)) * 2 * cols;
 }
 
+bool layer_norm_fits(int64_t tokens, int64_t cols) {
+    return fits_launch(tokens, shape_of(cols).threads);
+}
+
 hipError_t launch_layer_norm(const LayerNormProblem& p, hipStream_t s) {
     if (p.tokens == 0) return hipSuccess;
     Args a = {};

@@ -101,6 +101,9 @@ atp_status check_sum(const NormSum& s) {
     ATP_CHECK(check_tokens(s.tokens));
     ATP_CHECK(check_cols(s.cols, atp::kMaxNormCols));
     ATP_CHECK(check_dtype(s.dtype, "dtype"));
+    if (!atp::layer_norm_fits(s.tokens, s.cols))
+        return set_error(ATP_ERR_UNSUPPORTED, "%lld rows of %lld columns: 2^32 threads or more",
+                         (long long)s.tokens, (long long)s.cols);
     ATP_CHECK(check_matrix(s.x, s.tokens, s.ldx, s.cols, "x"));
     if (!s.add != !s.x_out)
         return set_error(ATP_ERR_INVALID_ARGUMENT, "add and x_out go together");
@@ -276,6 +279,9 @@ atp_status atp_embedding_fwd(int64_t tokens, const int32_t* ids, int64_t vocab_l
     ATP_CHECK(check_matrix(table, vocab_loc, ld_table, cols, "table"));
     ATP_CHECK(check_matrix(out, tokens, ld_out, cols, "out"));
     if (tokens == 0) return ATP_OK;
+    if (!atp::embedding_fits(tokens, cols))
+        return set_error(ATP_ERR_UNSUPPORTED, "%lld tokens of %lld columns: 2^37 values or more",
+                         (long long)tokens, (long long)cols);
     const int64_t z = size_of(out_dtype);
     if (share(buf(table, vocab_loc, ld_table, cols), buf(out, tokens, ld_out, cols, z)))
         return overlap("out", "table");

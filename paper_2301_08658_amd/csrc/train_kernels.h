@@ -10,7 +10,7 @@
 
 namespace atp {
 
-// Threads of a launch are fewer than 2^32 (a limit of HIP).
+// Threads of a launch are fewer than 2^32: HIP drops the rest of a larger one without an error.
 constexpr int64_t kLaunchThreads = (int64_t)1 << 32;
 inline bool fits_launch(int64_t groups, int64_t threads) {
     return groups < kLaunchThreads / threads;
@@ -23,6 +23,7 @@ struct EmbeddingProblem {
     float scale;
     void* out; int64_t ldo; bool out_f32;
 };
+bool embedding_fits(int64_t tokens, int64_t cols);       // one launch
 hipError_t launch_embedding(const EmbeddingProblem& p, hipStream_t s);
 
 struct EmbeddingBwdProblem {
@@ -54,6 +55,7 @@ struct LayerNormProblem {
     uint16_t* y; int64_t ldy;
     float *mean, *rstd;
 };
+bool layer_norm_fits(int64_t tokens, int64_t cols);      // one launch
 hipError_t launch_layer_norm(const LayerNormProblem& p, hipStream_t s);
 
 struct LayerNormBwdProblem {

@@ -322,3 +322,13 @@ def test_attention_tiles_of_one_launch(call):
     # 65538 tiles of 256 heads, in workgroups of 256 threads: a launch of 2^32
     wide = dict(t=128, kv=256, ldx=256 * 384, ldo=256 * 128, d=docs(n=65536))
     assert call(**wide) == UNS and "tiles" in B.last_error()
+
+
+def test_rows_of_one_launch():
+    # 2^32 threads: HIP drops what a launch has beyond them without an error
+    most = 1 << 24
+    assert emb(t=most, c=8192, ldw=8192, ldo=8192, w=1 << 46) == UNS
+    assert "2^37" in B.last_error()
+    for t, c in ((most, 4096), (13421773, 5120), (6710887, 20480), (1 << 22, 32768)):
+        for call in (stats, fwd):
+            assert call(t=t, c=c, ldx=c, add=None, xo=None) == UNS and "rows" in B.last_error()
