@@ -50,7 +50,7 @@ Shape shape_of(int64_t cols) {
 struct Args {
     int64_t tokens;
     int cols, nparts;
-    float inv_cols, inv_total, eps, part_cols;
+    float inv_total, eps, part_cols;
     const void* x; int64_t ldx;
     const uint16_t* add; int64_t ldadd;
     void* x_out; int64_t ldxo;
@@ -146,7 +146,8 @@ __global__ __launch_bounds__(ONE ? 64 * kRowsPerGroup : 1024) void norm_fwd_kern
     }
     float mean = 0.f, m2 = 0.f;
     if (A.nparts == 0) {
-        mean = row_sum<ONE>(sum, red[0], waves) * A.inv_cols;
+        // divided, not by a rounded reciprocal: rows of one value have it as their mean
+        mean = row_sum<ONE>(sum, red[0], waves) / A.part_cols;
         float sq = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -639,7 +640,6 @@ hipError_t launch_layer_norm(const LayerNormProblem& p, hipStream_t s) {
     a.tokens = p.tokens;
     a.cols = (int)p.cols;
     a.nparts = p.nparts;
-    a.inv_cols = 1.f / (float)p.cols;
     a.inv_total = 1.f / (float)(p.cols * std::max(1, p.nparts));
     a.part_cols = (float)p.cols;
     a.eps = p.eps;

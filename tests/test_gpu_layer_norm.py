@@ -220,3 +220,22 @@ def test_no_rows():
     dw, db = torch.full((c,), 9.0, device=DEV), torch.full((c,), 9.0, device=DEV)
     atp.atp_layer_norm_bwd(0, norm, none, empty, empty, none, none, dweight=dw, dbias=db)
     assert (dw == 0).all() and (db == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, BF])
+@pytest.mark.parametrize("c", [24, 520, 1000, 2056, 5120, 12288, 20480])
+def test_rows_of_one_value_give_the_bias(c, dtype):
+    # their sums are exact (multiples of 8 below 2^27), so the mean is the value itself and
+    # nothing is left of it, whatever 1 / sqrt(eps) would make of a rounding
+    t, values = 3, torch.tensor([1000.0, -24.0, 1656.0])
+    x = values.to(dtype).to(DEV)[:, None].expand(t, c).contiguous()
+    b = (torch.arange(c) % 7 - 3).to(BF).to(DEV)
+    y, mean, rstd = torch.empty((t, c), dtype=BF, device=DEV), *(
+        torch.empty(t, device=DEV) for _ in range(2))
+    for bias in (None, b):
+        atp.atp_layer_norm_fwd(t, atp.layer_norm(None, bias), x, y, mean, rstd)
+        assert torch.equal(mean.cpu(), values)
+        assert torch.equal(y, torch.zeros_like(y) if bias is None else b.expand(t, c))
+    stats = torch.empty((t, 2), device=DEV)
+    atp.atp_layer_norm_stats(t, x, stats)
+    assert torch.equal(stats[:, 0].cpu(), values) and (stats[:, 1] == 0).all()
