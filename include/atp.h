@@ -807,7 +807,7 @@ size_t atp_attention_cache_workspace_bytes(int32_t kv_heads, int32_t group, int3
  * ids: int32 [tokens], any value.  table: bf16 [vocab_loc, cols].  out: fp32 or
  * bf16 [tokens, cols].
  * Errors: INVALID_ARGUMENT for negative sizes, vocab_loc or cols < 1, a negative
- * vocab_off, a non-finite scale, NULL buffers, out sharing memory with table;
+ * vocab_off, a non-finite scale, NULL buffers, out sharing memory with table or ids;
  * UNSUPPORTED for more than 2^24 tokens or rows, 2^37 values of out, cols not a multiple
  * of 8, misalignment. */
 atp_status atp_embedding_fwd(int64_t tokens, const int32_t* ids, int64_t vocab_loc,
@@ -823,7 +823,7 @@ atp_status atp_embedding_fwd(int64_t tokens, const int32_t* ids, int64_t vocab_l
  * it and rows without tokens are not touched (a table that is the output
  * layer's weight too).  workspace: atp_embedding_workspace_bytes() bytes,
  * scratch.  Errors as atp_embedding_fwd; INVALID_ARGUMENT for another accumulate,
- * a short workspace, dtable sharing memory with dy. */
+ * a short workspace, dtable or the workspace sharing memory with another buffer. */
 atp_status atp_embedding_bwd(int64_t tokens, const int32_t* ids, int64_t vocab_loc,
                              int64_t vocab_off, int64_t cols, const void* dy, int64_t ld_dy,
                              float scale, float* dtable, int64_t ld_dtable, int32_t accumulate,

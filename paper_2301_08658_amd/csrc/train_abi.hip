@@ -32,7 +32,33 @@ struct Buf {
 Buf buf(const void* p, int64_t rows, int64_t ld, int64_t cols, int64_t size = 2) {
     return Buf{p, p ? extent(rows, ld, cols, size) : 0};
 }
+Buf vec(const void* p, int64_t n, int64_t size = 4) { return Buf{p, p ? n * size : 0}; }
 bool share(const Buf& a, const Buf& b) { return share_bytes(a.p, a.bytes, b.p, b.bytes); }
+
+// What a call writes must share no memory with what it reads or writes elsewhere.
+struct Named {
+    Buf b;
+    const char* name;
+};
+template <int N, int M>
+atp_status check_apart(const Named (&out)[N], const Named (&in)[M]) {
+    for (int i = 0; i < N; ++i) {
+        for (int j = 0; j < M; ++j)
+            if (share(out[i].b, in[j].b)) return overlap(out[i].name, in[j].name);
+        for (int j = 0; j < i; ++j)
+            if (share(out[i].b, out[j].b)) return overlap(out[i].name, out[j].name);
+    }
+    return ATP_OK;
+}
+template <int N>
+atp_status check_parts_apart(const Named (&out)[N], int n, const float* const* parts,
+                             int64_t tokens, const char* name) {
+    for (int j = 0; j < n; ++j) {
+        const Named part[] = {{vec(parts[j], 2 * tokens), name}};
+        ATP_CHECK(check_apart(out, part));
+    }
+    return ATP_OK;
+}
 
 atp_status check_dtype(int32_t dtype, const char* name) {
     if (dtype != ATP_F32 && dtype != ATP_BF16)
@@ -262,6 +288,12 @@ atp_status check_docs(const atp_attention_docs* d, int64_t tokens, int32_t kv_he
     ATP_CHECK(check_optional(d->prefix, "prefix"));
     return check_optional(d->slopes, "slopes");
 }
+template <int N>
+atp_status check_lists_apart(const Named (&out)[N], const atp_attention_docs* d, int64_t heads) {
+    const Named lists[] = {{vec(d->cu_docs, d->n_docs + (int64_t)1), "cu_docs"},
+                           {vec(d->prefix, d->n_docs), "prefix"}, {vec(d->slopes, heads), "slopes"}};
+    return check_apart(out, lists);
+}
 atp::DocsView view(const atp_attention_docs* d) {
     return atp::DocsView{d->cu_docs, d->prefix, d->slopes, d->n_docs, d->cap};
 }
@@ -283,8 +315,9 @@ atp_status atp_embedding_fwd(int64_t tokens, const int32_t* ids, int64_t vocab_l
         return set_error(ATP_ERR_UNSUPPORTED, "%lld tokens of %lld columns: 2^37 values or more",
                          (long long)tokens, (long long)cols);
     const int64_t z = size_of(out_dtype);
-    if (share(buf(table, vocab_loc, ld_table, cols), buf(out, tokens, ld_out, cols, z)))
-        return overlap("out", "table");
+    const Named to[] = {{buf(out, tokens, ld_out, cols, z), "out"}};
+    const Named from[] = {{buf(table, vocab_loc, ld_table, cols), "table"}, {vec(ids, tokens), "ids"}};
+    ATP_CHECK(check_apart(to, from));
     atp::EmbeddingProblem p = {};
     p.ids = ids;
     p.tokens = tokens;
@@ -317,10 +350,12 @@ atp_status atp_embedding_bwd(int64_t tokens, const int32_t* ids, int64_t vocab_l
         return set_error(ATP_ERR_INVALID_ARGUMENT, "accumulate %d is neither 0 nor 1", accumulate);
     ATP_CHECK(check_matrix(dy, tokens, ld_dy, cols, "dy"));
     ATP_CHECK(check_matrix(dtable, vocab_loc, ld_dtable, cols, "dtable"));
-    ATP_CHECK(check_workspace(workspace, ws_bytes,
-                              atp_embedding_workspace_bytes(tokens, vocab_loc, cols)));
-    if (share(buf(dy, tokens, ld_dy, cols), buf(dtable, vocab_loc, ld_dtable, cols, 4)))
-        return overlap("dtable", "dy");
+    const size_t need = atp_embedding_workspace_bytes(tokens, vocab_loc, cols);
+    ATP_CHECK(check_workspace(workspace, ws_bytes, need));
+    const Named out[] = {{buf(dtable, vocab_loc, ld_dtable, cols, 4), "dtable"},
+                         {vec(workspace, (int64_t)need, 1), "workspace"}};
+    const Named in[] = {{buf(dy, tokens, ld_dy, cols), "dy"}, {vec(ids, tokens), "ids"}};
+    ATP_CHECK(check_apart(out, in));
     atp::EmbeddingBwdProblem p = {};
     p.ids = ids;
     p.tokens = tokens;
@@ -345,12 +380,17 @@ atp_status atp_layer_norm_stats(int64_t tokens, int64_t cols, int32_t dtype, con
     ATP_CHECK(check_sum(sum));
     if (tokens == 0) return ATP_OK;
     ATP_CHECK(check_vector(stats, "stats"));
+    const int64_t z = size_of(dtype);
+    const Named out[] = {{vec(stats, 2 * tokens), "stats"}};
+    const Named in[] = {{buf(x, tokens, ldx, cols, z), "x"}, {buf(add, tokens, ld_add, cols), "add"},
+                        {buf(x_out, tokens, ld_xout, cols, z), "x_out"}};
+    ATP_CHECK(check_apart(out, in));
     atp::LayerNormProblem p = problem(sum);
     p.stats_out = stats;
     const double el = (double)tokens * cols;
     hipStream_t s = stream_of(stream);
     return run_timed("layer_norm_stats", 5.0 * el,
-                     el * (size_of(dtype) + (add ? 2 + size_of(dtype) : 0)), s,
+                     el * (z + (add ? 2 + z : 0)), s,
                      [&] { return atp::launch_layer_norm(p, s); });
 }
 
@@ -373,10 +413,16 @@ atp_status atp_layer_norm_fwd(int64_t tokens, int64_t cols, int32_t dtype,
     ATP_CHECK(check_vector(mean, "mean"));
     ATP_CHECK(check_vector(rstd, "rstd"));
     const int64_t z = size_of(dtype);
-    const Buf o = buf(y, tokens, ld_y, cols);
-    if (share(o, buf(x, tokens, ldx, cols, z))) return overlap("y", "x");
-    if (share(o, buf(x_out, tokens, ld_xout, cols, z))) return overlap("y", "x_out");
-    if (share(o, buf(add, tokens, ld_add, cols))) return overlap("y", "add");
+    const Named sum_out[] = {{buf(x_out, tokens, ld_xout, cols, z), "x_out"}};
+    const Named params[] = {{vec(norm->weight, cols, 2), "weight"}, {vec(norm->bias, cols, 2), "bias"}};
+    const Named out[] = {{buf(y, tokens, ld_y, cols), "y"}, {vec(mean, tokens), "mean"},
+                         {vec(rstd, tokens), "rstd"}};
+    const Named in[] = {{buf(x, tokens, ldx, cols, z), "x"}, {buf(add, tokens, ld_add, cols), "add"}};
+    ATP_CHECK(check_apart(out, in));
+    ATP_CHECK(check_apart(out, params));
+    ATP_CHECK(check_apart(out, sum_out));
+    ATP_CHECK(check_apart(sum_out, params));
+    ATP_CHECK(check_parts_apart(out, stats ? red_size : 0, stats, tokens, "stats"));
     atp::LayerNormProblem p = problem(sum);
     p.weight = bits(norm->weight);
     p.bias = bits(norm->bias);
@@ -399,6 +445,11 @@ atp_status atp_layer_norm_bwd_sums(int64_t tokens, int64_t cols, int32_t dtype,
     ATP_CHECK(check_norm_bwd(tokens, cols, dtype, norm, x, ldx, mean, rstd, dy, ld_dy));
     if (tokens == 0) return ATP_OK;
     ATP_CHECK(check_vector(sums, "sums"));
+    const Named out[] = {{vec(sums, 2 * tokens), "sums"}};
+    const Named in[] = {{buf(x, tokens, ldx, cols, size_of(dtype)), "x"},
+                        {buf(dy, tokens, ld_dy, cols), "dy"}, {vec(mean, tokens), "mean"},
+                        {vec(rstd, tokens), "rstd"}, {vec(norm->weight, cols, 2), "weight"}};
+    ATP_CHECK(check_apart(out, in));
     atp::LayerNormBwdProblem p =
         bwd_problem(tokens, cols, dtype, norm, x, ldx, mean, rstd, dy, ld_dy);
     p.sums_out = sums;
@@ -430,20 +481,22 @@ atp_status atp_layer_norm_bwd(int64_t tokens, int64_t cols, int32_t dtype,
     ATP_CHECK(check_optional(dweight, "dweight"));
     ATP_CHECK(check_optional(dbias, "dbias"));
     const bool weights = dweight || dbias;
-    if (weights)
-        ATP_CHECK(check_workspace(workspace, ws_bytes,
-                                  atp_layer_norm_workspace_bytes(tokens, cols)));
+    const size_t need = weights ? atp_layer_norm_workspace_bytes(tokens, cols) : 0;
+    ATP_CHECK(check_workspace(workspace, ws_bytes, need));
     if (tokens == 0 && !weights) return ATP_OK;
     const int64_t z = size_of(dtype);
-    const Buf bx = buf(x, tokens, ldx, cols, z), bdy = buf(dy, tokens, ld_dy, cols),
-              bres = buf(d_res, tokens, ld_dres, cols, z), bdx = buf(dx, tokens, ld_dx, cols, z),
-              badd = buf(d_add, tokens, ld_dadd, cols);
-    if (share(bdx, bx)) return overlap("dx", "x");
-    if (share(bdx, bdy)) return overlap("dx", "dy");
-    if (!(dx == d_res && ld_dx == ld_dres) && share(bdx, bres))
+    const Buf bres = buf(d_res, tokens, ld_dres, cols, z), bdx = buf(dx, tokens, ld_dx, cols, z);
+    const bool in_place = dx == d_res && ld_dx == ld_dres;
+    if (!in_place && share(bdx, bres))
         return set_error(ATP_ERR_INVALID_ARGUMENT, "dx must be d_res itself or not overlap it");
-    if (share(badd, bx) || share(badd, bdy) || share(badd, bres) || share(badd, bdx))
-        return overlap("d_add", "x, dy, d_res or dx");
+    const Named out[] = {{bdx, "dx"}, {buf(d_add, tokens, ld_dadd, cols), "d_add"},
+                         {vec(dweight, cols), "dweight"}, {vec(dbias, cols), "dbias"},
+                         {vec(weights ? workspace : nullptr, (int64_t)need, 1), "workspace"}};
+    const Named in[] = {{buf(x, tokens, ldx, cols, z), "x"}, {buf(dy, tokens, ld_dy, cols), "dy"},
+                        {in_place ? Buf{} : bres, "d_res"}, {vec(mean, tokens), "mean"},
+                        {vec(rstd, tokens), "rstd"}, {vec(norm->weight, cols, 2), "weight"}};
+    ATP_CHECK(check_apart(out, in));
+    ATP_CHECK(check_parts_apart(out, sums ? red_size : 0, sums, tokens, "sums"));
     atp::LayerNormBwdProblem p =
         bwd_problem(tokens, cols, dtype, norm, x, ldx, mean, rstd, dy, ld_dy);
     p.nparts = sums ? red_size : 0;
@@ -512,8 +565,11 @@ atp_status atp_attention_docs_fwd(int64_t tokens, int32_t kv_heads, int32_t grou
     ATP_CHECK(check_matrix(out, tokens, ld_out, ocols, "out"));
     if (tokens == 0 || docs->n_docs == 0) return ATP_OK;
     ATP_CHECK(check_vector(lse, "lse"));
-    if (share(buf(qkv, tokens, ld_qkv, cols), buf(out, tokens, ld_out, ocols)))
-        return overlap("out", "qkv");
+    const Named to[] = {{buf(out, tokens, ld_out, ocols), "out"},
+                        {vec(lse, tokens * kv_heads * group), "lse"}};
+    const Named from[] = {{buf(qkv, tokens, ld_qkv, cols), "qkv"}};
+    ATP_CHECK(check_apart(to, from));
+    ATP_CHECK(check_lists_apart(to, docs, (int64_t)kv_heads * group));
     atp::DocsAttentionProblem p = {};
     p.docs = view(docs);
     p.tokens = tokens;
@@ -549,12 +605,16 @@ atp_status atp_attention_docs_bwd(int64_t tokens, int32_t kv_heads, int32_t grou
     ATP_CHECK(check_matrix(d_qkv, tokens, ld_dqkv, cols, "d_qkv"));
     if (tokens == 0 || docs->n_docs == 0) return ATP_OK;
     ATP_CHECK(check_vector(lse, "lse"));
-    ATP_CHECK(check_workspace(workspace, ws_bytes,
-                              atp_attention_docs_workspace_bytes(tokens, kv_heads, group)));
-    const Buf d = buf(d_qkv, tokens, ld_dqkv, cols);
-    if (share(d, buf(qkv, tokens, ld_qkv, cols))) return overlap("d_qkv", "qkv");
-    if (share(d, buf(out, tokens, ld_out, ocols))) return overlap("d_qkv", "out");
-    if (share(d, buf(d_out, tokens, ld_dout, ocols))) return overlap("d_qkv", "d_out");
+    const size_t need = atp_attention_docs_workspace_bytes(tokens, kv_heads, group);
+    ATP_CHECK(check_workspace(workspace, ws_bytes, need));
+    const Named to[] = {{buf(d_qkv, tokens, ld_dqkv, cols), "d_qkv"},
+                        {vec(workspace, (int64_t)need, 1), "workspace"}};
+    const Named from[] = {{buf(qkv, tokens, ld_qkv, cols), "qkv"},
+                          {buf(out, tokens, ld_out, ocols), "out"},
+                          {buf(d_out, tokens, ld_dout, ocols), "d_out"},
+                          {vec(lse, tokens * kv_heads * group), "lse"}};
+    ATP_CHECK(check_apart(to, from));
+    ATP_CHECK(check_lists_apart(to, docs, (int64_t)kv_heads * group));
     atp::DocsAttentionBwdProblem p = {};
     p.docs = view(docs);
     p.tokens = tokens;

@@ -332,3 +332,50 @@ def test_rows_of_one_launch():
     for t, c in ((most, 4096), (13421773, 5120), (6710887, 20480), (1 << 22, 32768)):
         for call in (stats, fwd):
             assert call(t=t, c=c, ldx=c, add=None, xo=None) == UNS and "rows" in B.last_error()
+
+
+def test_written_memory_is_apart():
+    """Buffers far from each other but for the named pair."""
+    at = {k: (i + 1) << 32 for i, k in enumerate("ids w out dy dw ws x add xo y m r st p b res dx da "
+                                                 "db su qkv o z do cu pre sl".split())}
+
+    def pairs(call, base, written, read):
+        for a in written:
+            for b in list(written) + list(read):
+                if a == b:
+                    continue
+                assert call(**{**base, a: base[b]}) == INV, (a, b)
+                assert "overlap" in B.last_error(), (a, b)
+    pairs(emb, dict(ids=at["ids"], w=at["w"], out=at["out"]), ["out"], ["ids", "w"])
+    pairs(emb_bwd, dict(ids=at["ids"], dy=at["dy"], dw=at["dw"], ws=at["ws"]), ["dw", "ws"],
+          ["ids", "dy"])
+    lone = {k: at[k] for k in ("x", "y", "m", "r")}
+    pairs(fwd, dict(lone, add=None, xo=None, p=norm(at["p"], at["b"])), ["y", "m", "r"], ["x"])
+    both = dict(lone, add=at["add"], xo=at["xo"], p=norm(at["p"], at["b"]))
+    pairs(fwd, both, ["y", "m", "r"], ["x", "add", "xo"])
+    for k in ("y", "m", "r", "xo"):
+        for q in ("p", "b"):
+            assert fwd(**{**both, k: at[q]}) == INV and "overlap" in B.last_error(), (k, q)
+        if k != "xo":
+            assert fwd(**{**lone, k: at["st"]}, add=None, xo=None, n=2, p=norm(at["p"], at["b"]),
+                       st=[at["su"], at["st"]]) == INV and "overlap" in B.last_error()
+    pairs(stats, {k: at[k] for k in ("x", "add", "xo", "st")}, ["st"], ["x", "add", "xo"])
+    back = dict(x=at["x"], m=at["m"], r=at["r"], dy=at["dy"], p=norm(at["p"], at["b"]))
+    pairs(sums, dict(back, su=at["su"]), ["su"], ["x", "m", "r", "dy"])
+    assert sums(**back, su=at["p"]) == INV and "overlap" in B.last_error()
+    back.update(res=at["res"], dx=at["dx"], da=at["da"], dw=at["dw"], db=at["db"], ws=at["ws"])
+    pairs(bwd, back, ["da", "dw", "db", "ws"], ["x", "m", "r", "dy", "res", "dx"])
+    pairs(bwd, back, ["dx"], ["x", "m", "r", "dy"])          # dx may be res
+    for k in ("dx", "da", "dw", "db", "ws"):
+        assert bwd(**{**back, k: at["p"]}) == INV and "overlap" in B.last_error()
+        assert bwd(**{**back, k: at["su"]}, n=2, su=[at["st"], at["su"]]) == INV
+        assert "overlap" in B.last_error()
+    lists = docs(cu=at["cu"], pre=at["pre"], sl=at["sl"])
+    fore = dict(x=at["qkv"], o=at["o"], z=at["z"], d=lists)
+    pairs(att, fore, ["o", "z"], ["x"])
+    aft = dict(fore, do=at["do"], dx=at["dx"], ws=at["ws"])
+    pairs(att_bwd, aft, ["dx", "ws"], ["x", "o", "z", "do"])
+    for call, base, written in ((att, fore, "oz"), (att_bwd, aft, ("dx", "ws"))):
+        for k in written:
+            for q in ("cu", "pre", "sl"):
+                assert call(**{**base, k: at[q]}) == INV and "overlap" in B.last_error()
