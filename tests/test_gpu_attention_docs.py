@@ -294,3 +294,58 @@ def test_lists_padded_to_the_most_documents(kv, cap):
     # 65536 documents, nearly all empty: more tiles than the kernels of 768 threads can have
     lens = [60] + [0] * 40000 + [1, 0, 67] + [0] * 25532
     Run(lens, kv, 1, cap=cap, seed=4).check()
+
+
+def bits(t):
+    return t.contiguous().view(torch.int16 if t.dtype is BF else torch.int32)
+
+
+@pytest.mark.parametrize("kv,group,lens", [(2, 2, [70, 200, 129]), (4, 8, [700, 130, 1100])])
+@pytest.mark.parametrize("kw", [{}, dict(cap=30.0), dict(slopes=True, prefix=True),
+                                dict(cap=30.0, slopes=True, prefix=True)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf"), 3e38])
+def test_documents_keep_their_bits_beside_others(kv, group, lens, kw, bad):
+    """Whatever other documents and padding rows hold, a document's results have the same bits,
+    forward and backward."""
+    kw = dict(kw, prefix=[5, 100, 0] if kw.get("prefix") else None)
+    r = Run(lens, kv, group, first=10, behind=20, **kw)
+    w, c = r.qkv.shape[1], r.heads * D
+    out, lse, d_qkv = r.buffers()
+    r.forward(buf=(out, lse, d_qkv))
+    r.backward(out, lse, d_qkv)
+    for d in range(len(lens)):
+        rows = slice(r.cu[d], r.cu[d + 1])
+        qkv, d_out = torch.full_like(r.qkv, bad), torch.full_like(r.d_out, bad)
+        qkv[rows], d_out[rows] = r.qkv[rows], r.d_out[rows]
+        o, z, g = r.buffers()
+        r.forward(qkv, (o, z, g))
+        r.backward(o, z, g, qkv, d_out)
+        assert torch.equal(bits(o[rows, :c]), bits(out[rows, :c])), d
+        assert torch.equal(bits(z[:, rows]), bits(lse[:, rows])), d
+        assert torch.equal(bits(g[rows, :w]), bits(d_qkv[rows, :w])), d
+        assert torch.isfinite(g[rows, :w]).all()
+
+
+@pytest.mark.parametrize("kv,group", [(1, 2), (16, 2)])
+def test_long_lists_that_are_wrong_stay_inside(kv, group):
+    """More than 64 documents that leave the rows or do not ascend: nothing outside the
+    buffers is touched, and rows behind stay as they were."""
+    r = Run([300], kv, group, behind=1000)
+    c, w = r.heads * D, r.qkv.shape[1]
+    g = torch.Generator().manual_seed(2)
+    wild = torch.randint(-2 ** 31, 2 ** 31, (90,), generator=g).tolist()
+    near = torch.randint(-100, 1500, (90,), generator=g).tolist()
+    for cu in (wild, near, sorted(near)[::-1], [1300] * 45 + [0] * 45, [-2 ** 31] * 90,
+               [2 ** 31 - 1] * 90, [0] * 89 + [2 ** 31 - 1]):
+        prefix = torch.randint(-2 ** 31, 2 ** 31, (89,), generator=g).tolist()
+        docs = atp.attention_docs(ints(cu), prefix=ints(prefix))
+        out, lse, d_qkv = r.buffers()
+        atp.atp_attention_docs_fwd(r.t, kv, group, docs, r.qkv, out[:r.t, :c], lse)
+        n = atp.atp_attention_docs_workspace_bytes(r.t, kv, group)
+        ws = torch.zeros(n + 64, dtype=torch.uint8, device=DEV)
+        atp.atp_attention_docs_bwd(r.t, kv, group, docs, r.qkv, out[:r.t, :c], lse, r.d_out,
+                                   d_qkv[:r.t, :w], ws[:n])
+        torch.cuda.synchronize()
+        assert torch.isnan(out[r.t]).all() and torch.isnan(d_qkv[r.t]).all()
+        assert torch.isnan(out[:, c:]).all() and torch.isnan(d_qkv[:, w:]).all()
+        assert (ws[n:] == 0).all()

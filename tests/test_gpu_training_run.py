@@ -358,3 +358,34 @@ def test_gradients_of_billions_of_values():
     atp.atp_grad_clip(grads, [total], norm, max_norm=1.0)
     want = torch.tensor(3.0 / 54 ** 0.5).to(BF)
     assert (g[at].cpu() == want).all() and int((g != 0).sum()) == 6
+
+
+def _bits(t):
+    return t.contiguous().view({2: torch.int16, 4: torch.int32, 8: torch.int64}[t.element_size()])
+
+
+@pytest.mark.parametrize("stream", [F32, BF])
+def test_replays_have_the_bits_of_eager_steps(stream):
+    """As above, but every value counts, also beside a NaN."""
+    s = Step(400, 256, 1, 4, 300, 6, stream)
+    eager = Step(400, 256, 1, 4, 300, 6, stream)
+    s.batch([100, 50, 0, 200, 1, 9], 1)
+    s.run()                                               # warm
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        s.run()
+    for k, lens in enumerate(([9, 1, 200, 0, 50, 100], [400, 0, 0, 0, 0, 0], [1, 2, 3, 4, 5, 6],
+                              [64, 64, 64, 64, 64, 80], [9, 1, 200, 0, 50, 100])):
+        for b in (s, eager):
+            b.batch(lens, 20 + k)
+            for n in ("attn", "d_turned", "lse"):
+                b.a[n].zero_()
+        graph.replay()
+        eager.run()
+        torch.cuda.synchronize()
+        got, want = s.outputs(), eager.outputs()
+        for n in want:
+            assert torch.equal(_bits(got[n]), _bits(want[n])), (lens, n)
+        assert torch.isfinite(want["norm"]).all()
