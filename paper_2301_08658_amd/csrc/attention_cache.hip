@@ -37,6 +37,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "attention_tiles.h"
 #include "cache_kernels.h"
 #include "cache_plan.h"
 #include "lds_dma.h"
@@ -44,53 +45,17 @@
 namespace atp {
 namespace {
 
-constexpr int D = kHead;
-constexpr int NWAVE = 4;
-constexpr int NTHR = 64 * NWAVE;
+using namespace tiles;
+static_assert(D == kHead, "head dimension");
 constexpr int KT = 32;                 // keys of a wave's tile
 using plan::kGroups;
 using plan::kLeast;
 constexpr int kXcds = 8;
 constexpr float kLn2 = 0.69314718055994530942f;
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef short i16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 // lists that the kernel never writes: uniform reads go through the scalar cache
 typedef const __attribute__((address_space(4))) int32_t* const_ints;
 
-// 16-byte chunk c of tile row n is kept at these places (distinct banks for the
-// fragment reads and for the transposing reads)
-__device__ __forceinline__ int kpos(int n, int c) { return c ^ (n & 15); }
-__device__ __forceinline__ int vpos(int n, int c) { return c ^ (2 * (n & 3) + 8 * ((n >> 2) & 1)); }
-
-// maximum and sum over the four lanes l, l ^ 16, l ^ 32, l ^ 48, the same bits in each
-__device__ __forceinline__ float row_max4(float x) {
-    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
-                                                    false);
-    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
-                                                    false);
-    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float row_sum4(float x) {
-    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
-                                                    false);
-    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
-                                                    false);
-    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
-}
-__device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {   // round to nearest even
-    const f32x2 v = {a, b};
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
-}
 __device__ __forceinline__ float weight_of(float m, float top) {   // exp2(m - top), 0 for m = -inf
     return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
 }
@@ -393,13 +358,6 @@ __device__ __forceinline__ bool has_odd(uint32_t seen) {    // in any lane
     return __builtin_amdgcn_ballot_w64((seen & 0x80008000u) != 0) != 0;
 }
 
-// V^T's fragment of a 32-key slice: two transposing reads 16 rows apart.
-__device__ __forceinline__ bf16x8 v_fragment(const uint16_t* p) {
-    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p);
-    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 16 * D));
-    const i16x8 vv = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-    return __builtin_bit_cast(bf16x8, vv);
-}
 // Infinities and NaN of a 32-key slice of V where not every row sees them: 0 times them
 // would reach the other rows' sums in a matrix product, so what the rows do see is
 // added here, key by key, o(row lane % 16, value 16 dt + 4 g + e) += p(row, key) v(key,
@@ -705,7 +663,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_kernel(Args a) {
             }
 #pragma unroll
             for (int dt = 0; dt < 8; ++dt) {
-                const bf16x8 vf = v_fragment(vt + vread[dt]);
+                const bf16x8 vf = frag_tr_at(vt + vread[dt]);
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
                     o[r][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r], o[r][dt], 0, 0, 0);
@@ -986,7 +944,7 @@ __global__ __launch_bounds__(NTHR, 2) void attention_cache_wide_kernel(Args a) {
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
                     vf[i & 1][d] =
-                        v_fragment(vt + 32 * (i >> 1) * D + vread[4 * (i & 1) + d]);
+                        frag_tr_at(vt + 32 * (i >> 1) * D + vread[4 * (i & 1) + d]);
             };
 #pragma unroll
             for (int r = 0; r < RB; ++r) {

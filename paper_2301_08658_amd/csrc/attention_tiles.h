@@ -27,6 +27,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 
+// 16-byte chunk c of tile row n is kept at these places: distinct banks for the fragment
+// reads (both) and for the transposing reads (vpos).
 __device__ __forceinline__ int kpos(int n, int c) { return c ^ (n & 15); }
 __device__ __forceinline__ int vpos(int n, int c) { return c ^ (2 * (n & 3) + 8 * ((n >> 2) & 1)); }
 
