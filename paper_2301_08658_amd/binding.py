@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import NamedTuple, Optional, Sequence
+from typing import Optional, Sequence
 
 import torch
 
@@ -1268,32 +1268,20 @@ def atp_attention_docs_bwd(tokens: int, kv_heads: int, group: int, docs: attenti
         _stream(stream, dev)))
 
 
-class _Place(NamedTuple):
-    """Memory of rows `pitch` bytes apart; side and i: whose it is."""
-    begin: int
-    rows: int
-    pitch: int
-    width: int
-    i: int
-    side: str
-
-    @property
-    def end(self) -> int:
-        return self.begin + (self.rows - 1) * self.pitch + self.width
-
-    def meets(self, other: "_Place") -> bool:
-        """Whether a byte belongs to both (columns of one matrix interleave without)."""
-        if self.rows > 1 and other.rows > 1 and self.pitch != other.pitch:
-            a, b = (self, other) if self.rows <= other.rows else (other, self)
-            return any(a._replace(begin=a.begin + k * a.pitch, rows=1).meets(b)
-                       for k in range(a.rows))
-        # row k + j of this one meets row j of the other where k pitch is inside the rows'
-        # widths of their distance
-        pitch = self.pitch if self.rows > 1 else other.pitch
-        far = other.begin - self.begin
-        least = max((far - self.width) // pitch + 1, 1 - other.rows)
-        most = min(-((-far - other.width) // pitch) - 1, self.rows - 1)
-        return least <= most
+# a, b: memory of rows `pitch` bytes apart, (begin, end, rows, pitch, width, ...).
+def _meet(a, b) -> bool:
+    """Whether a byte belongs to both (columns of one matrix interleave without)."""
+    begin, _, rows, pitch, width = a[:5]
+    if rows > 1 and b[2] > 1 and pitch != b[3]:
+        if rows > b[2]:
+            return _meet(b, a)
+        return any(_meet((begin + k * pitch, 0, 1, pitch, width), b) for k in range(rows))
+    # row k + j of a meets row j of b where k pitch is inside the rows' widths of their distance
+    pitch = pitch if rows > 1 else b[3]
+    far = b[0] - begin
+    least = max((far - width) // pitch + 1, 1 - b[2])
+    most = min(-((-far - b[4]) // pitch) - 1, rows - 1)
+    return least <= most
 
 
 class grad_list:
@@ -1327,19 +1315,22 @@ class grad_list:
                 setattr(g, "ld_" + side, t.stride(0) if gaps else cols)
                 setattr(g, side + "_dtype", _float_code(t, f"{side}[{i}]"))
                 if t.numel():
-                    pitch = getattr(g, "ld_" + side) * t.element_size()
-                    spans.append(_Place(t.data_ptr(), rows, pitch, cols * t.element_size(), i, side))
+                    begin, size = t.data_ptr(), t.element_size()
+                    pitch, width = getattr(g, "ld_" + side) * size, cols * size
+                    spans.append((begin, begin + (rows - 1) * pitch + width, rows, pitch, width,
+                                  i, side))
             g.rows, g.cols = rows, cols
             self.device = s.device.index
         # a result must not land in another gradient or result
         spans.sort()
-        reach = []                       # what ends behind the next one's begin
+        reach, last = [], 0              # what ends behind the next one's begin
         for span in spans:
-            reach = [r for r in reach if r.end > span.begin]
+            reach = [r for r in reach if r[1] > span[0]] if span[0] < last else []
             for r in reach:
-                if r.i != span.i and "dst" in (r.side, span.side) and r.meets(span):
-                    raise ValueError(f"{r.side}[{r.i}] and {span.side}[{span.i}] overlap")
+                if r[5] != span[5] and "dst" in (r[6], span[6]) and _meet(r, span):
+                    raise ValueError(f"{r[6]}[{r[5]}] and {span[6]}[{span[5]}] overlap")
             reach.append(span)
+            last = max(last, span[1])
 
     @staticmethod
     def _matrix(t: torch.Tensor, name: str):
