@@ -876,8 +876,8 @@ atp_status atp_layer_norm_stats(int64_t tokens, int64_t cols, int32_t dtype, con
  * d_res: the gradient that reaches x_out past the norm (`dtype`, nullable).  dx:
  * `dtype`, may be d_res itself (same pointer and ld); it is the gradient of x and of
  * add.  d_add (nullable): dx rounded to bf16 from fp32, for the linear that add came
- * from.  dweight, dbias: fp32 [cols], nullable; they need a workspace of
- * atp_layer_norm_workspace_bytes(tokens, cols) bytes.
+ * from.  dweight, dbias: fp32 [cols], nullable, overwritten (batches are added up by the
+ * caller); they need a workspace of atp_layer_norm_workspace_bytes(tokens, cols) bytes.
  * Rows on several devices: sums is the table of the devices' two row sums (fp32
  * [tokens][2]: g and g o xh over the local columns), each written by
  * atp_layer_norm_bwd_sums.  Errors as atp_layer_norm_fwd; INVALID_ARGUMENT for a
@@ -935,9 +935,11 @@ atp_status atp_attention_docs_fwd(int64_t tokens, int32_t kv_heads, int32_t grou
  * layout and must not overlap qkv, out or d_out.  dk and dv are summed in fp32 over the
  * group's query heads.  The weights are formed again from lse, whose last bit moves
  * them by |lse| 2^-23 of themselves; scores of 2^30 and more have no defined gradient.
- * An infinity or NaN in a document may reach all gradients of that document, and no other.  workspace: atp_attention_docs_workspace_bytes() bytes,
- * scratch.  Errors as atp_attention_docs_fwd; INVALID_ARGUMENT for a short
- * workspace. */
+ * Weights are rounded to bf16 for dv's product with d_out, and the scores' gradients
+ * for those with k and q that give dq and dk.  An infinity or NaN in a document may
+ * reach all gradients of that document, and no other.  workspace:
+ * atp_attention_docs_workspace_bytes() bytes, scratch.  Errors as
+ * atp_attention_docs_fwd; INVALID_ARGUMENT for a short workspace. */
 atp_status atp_attention_docs_bwd(int64_t tokens, int32_t kv_heads, int32_t group,
                                   const atp_attention_docs* docs, const void* qkv, int64_t ld_qkv,
                                   const void* out, int64_t ld_out, const float* lse,
@@ -977,12 +979,13 @@ size_t atp_grad_workspace_bytes(int32_t n, const atp_grad* grads);
  *   dst = factor * src, rounded once, for each gradient.
  * scale: what the gradients are to be multiplied by in any case (1 / loss scale, 1 /
  * number of accumulated batches).  norm: fp32 [2], 8-byte aligned, receives norm and
- * factor.  An infinite norm gives factor 0 (NaN where the gradient is infinite), a NaN
- * one NaN everywhere: look at norm before using dst.  A dst must be its src itself
- * (type and leading dimension too) or overlap no src, and no other dst (the call
- * looks at pairs of one gradient alone).  Errors as atp_grad_sq_sum; INVALID_ARGUMENT
- * for scale or max_norm not positive (max_norm may be infinite), red_size < 1;
- * UNSUPPORTED for red_size above ATP_MAX_GROUP. */
+ * factor.  An infinite norm gives factor 0 (NaN where the gradient is infinite) unless
+ * max_norm is infinite too, a NaN one NaN everywhere: look at norm before using dst.
+ * A dst must be its src itself (type and leading dimension too) or overlap no src, and
+ * no other dst (the call looks at pairs of one gradient alone, from the first value to
+ * the last).  Errors as atp_grad_sq_sum; INVALID_ARGUMENT for scale or max_norm not
+ * positive (max_norm may be infinite), red_size < 1; UNSUPPORTED for red_size above
+ * ATP_MAX_GROUP. */
 atp_status atp_grad_clip(int32_t n, const atp_grad* grads, int32_t red_size,
                          const double* const* sums, float scale, float max_norm, float* norm,
                          void* stream);

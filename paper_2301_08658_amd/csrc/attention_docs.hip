@@ -26,11 +26,18 @@
 // heads of its key head; where that leaves too few workgroups the heads are divided
 // over several, which leave fp32 sums that are added in order.
 //
-// Bound by the matrix cores and the vector instructions together, as the causal core is: 20
-// heads of two documents of 4096 rows forward 186 us, 927 TFLOP/s of the visible pairs'
-// products (matrix cores busy 43% of the cycles), backward 680 us, 632 TFLOP/s (dQ 260 us,
-// 48%, dK and dV 450 us, 35%, the waves waiting for LDS 39% of their time); one of 16384
-// rows and 8 heads 508 us and 1903, 1080 and 722 TFLOP/s.
+// The weights P are rounded to bf16 for the products with V and dO, and dS for those with K
+// and Q: the matrix instructions that take 32 bits have a sixteenth of the rate.  A rounding is
+// off by 2^-9 of the value at most, so that outputs and gradients are off by up to 2^-9 of the
+// sums of their terms' magnitudes (on unit-normal inputs 0.24% of the results' norm, of
+// which the results' own rounding to bf16 is 0.17); sums, maxima, lse and delta are fp32.
+//
+// Kernels of 20 heads of two documents of 4096 rows, one profile: forward 194 us, 886 TFLOP/s of
+// the visible pairs' products (matrix cores busy 43% of the cycles, vector units 44%: the two
+// together), dQ 264 us (48% and 39%), dK and dV 478 us, where no unit is full (35%, 32%, LDS
+// 39%) and the waves wait for LDS, copies and barriers 39% of their time; 579 TFLOP/s for the
+// backward's five products.  Calls in a row on one document of 16384 rows and 8 heads: 503 to
+// 525 us forward and 1880 to 1950 backward, 1050 to 1090 and 700 to 730 TFLOP/s.
 #include <hip/hip_runtime.h>
 #include <float.h>
 #include <math.h>
@@ -1205,9 +1212,13 @@ int64_t slots_of(int64_t tokens, int rows, int n_docs) { return tokens / rows + 
 // Divisions of a group's heads for the dK/dV kernel: as many as it takes for `tiles` of 64
 // keys.  Four per CU (16 heads of two key heads, one document of 4096 rows: 317 us; for two
 // per CU 391, for eight 349); where documents have fewer than 512 rows, what fills the chip,
-// since each division starts anew and leaves sums to be joined (backward of 36 documents
-// of 128 rows, 4 key heads of 3 query heads: 61 and 43 us; of 20 of 300, 12 heads of one key
-// head: 84 and 70; of 9 of 520 the same, with prefixes 119 and 146).
+// since each division starts anew and leaves sums to be joined.  Backward by both rules, what
+// fills the chip and four per CU, us, ragged documents of an average of
+//   128 rows, heads of 4 x 3: 62 and 75; 1 x 12: 79 and 68; 4 x 5: 108 and 132;
+//   256: 80 and 74; 84 and 88; 151 and 156;      350: 85 and 79; 90 and 95; 163 and 171;
+//   450: 98 and 86; 101 and 102; 193 and 198;    512: 125 and 101; 118 and 119; 231 and 202;
+//   650: 126 and 100; 122 and 111; 253 and 238;  1024: 158 and 128; 168 and 168; 297 and 296.
+// Between 200 and 500 the layouts differ in which is faster, by up to 13%.
 constexpr int64_t kPartTiles = 1024;
 int64_t part_tiles(int64_t tokens, int n_docs) {
     return tokens / n_docs < 512 ? full_tiles(tokens, n_docs) : kPartTiles;

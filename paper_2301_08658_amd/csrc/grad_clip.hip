@@ -289,7 +289,9 @@ int64_t row_blocks(int64_t rows, int64_t cols, int group) {
     return (rows * ((cols + 7) / 8) + group / 8 - 1) / (group / 8);
 }
 // Rows with gaps that one entry takes.
-int64_t piece_rows(int64_t cols, int group) { return kMaxRowBlocks * (group / 8) / ((cols + 7) / 8); }
+int64_t piece_rows(int64_t cols, int group) {
+    return kMaxRowBlocks * (group / 8) / ((cols + 7) / 8);
+}
 int64_t blocks_of(const GradView& g) {
     if (g.rows == 0 || g.cols == 0) return 0;
     int64_t blocks = 0;

@@ -291,7 +291,8 @@ atp_status check_docs(const atp_attention_docs* d, int64_t tokens, int32_t kv_he
 template <int N>
 atp_status check_lists_apart(const Named (&out)[N], const atp_attention_docs* d, int64_t heads) {
     const Named lists[] = {{vec(d->cu_docs, d->n_docs + (int64_t)1), "cu_docs"},
-                           {vec(d->prefix, d->n_docs), "prefix"}, {vec(d->slopes, heads), "slopes"}};
+                           {vec(d->prefix, d->n_docs), "prefix"},
+                           {vec(d->slopes, heads), "slopes"}};
     return check_apart(out, lists);
 }
 atp::DocsView view(const atp_attention_docs* d) {
@@ -316,7 +317,8 @@ atp_status atp_embedding_fwd(int64_t tokens, const int32_t* ids, int64_t vocab_l
                          (long long)tokens, (long long)cols);
     const int64_t z = size_of(out_dtype);
     const Named to[] = {{buf(out, tokens, ld_out, cols, z), "out"}};
-    const Named from[] = {{buf(table, vocab_loc, ld_table, cols), "table"}, {vec(ids, tokens), "ids"}};
+    const Named from[] = {{buf(table, vocab_loc, ld_table, cols), "table"},
+                          {vec(ids, tokens), "ids"}};
     ATP_CHECK(check_apart(to, from));
     atp::EmbeddingProblem p = {};
     p.ids = ids;
@@ -382,7 +384,8 @@ atp_status atp_layer_norm_stats(int64_t tokens, int64_t cols, int32_t dtype, con
     ATP_CHECK(check_vector(stats, "stats"));
     const int64_t z = size_of(dtype);
     const Named out[] = {{vec(stats, 2 * tokens), "stats"}};
-    const Named in[] = {{buf(x, tokens, ldx, cols, z), "x"}, {buf(add, tokens, ld_add, cols), "add"},
+    const Named in[] = {{buf(x, tokens, ldx, cols, z), "x"},
+                        {buf(add, tokens, ld_add, cols), "add"},
                         {buf(x_out, tokens, ld_xout, cols, z), "x_out"}};
     ATP_CHECK(check_apart(out, in));
     atp::LayerNormProblem p = problem(sum);
@@ -414,10 +417,12 @@ atp_status atp_layer_norm_fwd(int64_t tokens, int64_t cols, int32_t dtype,
     ATP_CHECK(check_vector(rstd, "rstd"));
     const int64_t z = size_of(dtype);
     const Named sum_out[] = {{buf(x_out, tokens, ld_xout, cols, z), "x_out"}};
-    const Named params[] = {{vec(norm->weight, cols, 2), "weight"}, {vec(norm->bias, cols, 2), "bias"}};
+    const Named params[] = {{vec(norm->weight, cols, 2), "weight"},
+                            {vec(norm->bias, cols, 2), "bias"}};
     const Named out[] = {{buf(y, tokens, ld_y, cols), "y"}, {vec(mean, tokens), "mean"},
                          {vec(rstd, tokens), "rstd"}};
-    const Named in[] = {{buf(x, tokens, ldx, cols, z), "x"}, {buf(add, tokens, ld_add, cols), "add"}};
+    const Named in[] = {{buf(x, tokens, ldx, cols, z), "x"},
+                        {buf(add, tokens, ld_add, cols), "add"}};
     ATP_CHECK(check_apart(out, in));
     ATP_CHECK(check_apart(out, params));
     ATP_CHECK(check_apart(out, sum_out));
